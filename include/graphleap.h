@@ -425,6 +425,99 @@ gl_status gl_vig_stack(gl_lookahead_t h, const void* x0, int B, int H, int W, in
                        gl_dtype dt, gl_schedule schedule, void* ws, size_t ws_bytes,
                        void* x_out);
 
+/* ===========================================================================
+ * Layer norm and 8-bit layers (the normalisation units of Sec. IV-D, and the
+ * dense layers of a block on 8-bit integers).
+ *
+ * These calls take rows of any width, stride and alignment of their elements:
+ * x is [R, C] in dt with rows `ldx` elements apart (ldx >= C; ldx == C for
+ * contiguous rows, anything for R == 1), aligned to its element.  Vectors
+ * (gamma, beta, bias) are in dt, statistics, scales and weight gradients fp32.
+ * Sums are fp32 (int32 in products) in an order that depends on the sizes
+ * alone: a call repeats its bits.
+ *
+ * 8-bit rows: int8 q [R, Kp] with Kp = gl_q8_row_bytes(K) (K rounded up to 16),
+ * 16-byte aligned, its bytes K .. Kp-1 zero, and a scale [R] fp32; the values
+ * are q[r, k] * scale[r].  gl_quantize_rows and gl_layer_norm_q8 write such
+ * rows; weights [Cout, K] become them once, with one scale per output channel.
+ * ========================================================================= */
+
+/* ---------------------------------------------------------------------------
+ * gl_layer_norm -- per row, over its C channels:
+ *   mean = sum x / C;  var = sum (x - mean)^2 / C;  rstd = 1 / sqrt(var + eps)
+ *   out  = (x - mean) rstd gamma + beta          (fp32, rounded once to dt)
+ *   gamma, beta [C] (dt) or NULL for ones and zeros; eps >= 0.
+ *   out [R, C] (dt), contiguous.  mean, rstd [R] fp32 or NULL: what
+ *   gl_layer_norm_backward needs.  Outputs must not overlap x, gamma or beta.
+ * A row with a NaN or an infinity is NaN.
+ * Limits: R, C >= 1; R * C < 2^40.
+ * Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype), GL_ERR_BAD_SHAPE (sizes,
+ * ldx < C, eps negative or not finite), GL_ERR_ALIGNMENT, GL_ERR_ALIAS, GL_ERR_HIP.
+ * -------------------------------------------------------------------------*/
+gl_status gl_layer_norm(const void* x, int R, int C, long long ldx, const void* gamma,
+                        const void* beta, float eps, gl_dtype dt, void* out, float* mean,
+                        float* rstd, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * gl_layer_norm_backward -- the gradients of gl_layer_norm from the output's,
+ * with xh = (x - mean) rstd and h = dy gamma:
+ *   dx     = rstd (h - avg_c h - xh avg_c(h xh))
+ *   dgamma = sum_r dy xh;   dbeta = sum_r dy
+ *   dy, x [R, C] (dt), rows lddy and ldx apart; mean, rstd [R] from the forward
+ *   pass; gamma [C] (dt) or NULL for ones.
+ *   dx [R, C] (dt), contiguous; dgamma, dbeta [C] fp32.  Any of the three may
+ *   be NULL (not all): it is then not computed.
+ *   workspace: gl_layer_norm_backward_workspace_bytes(R, C, dt) bytes, 16-byte
+ *   aligned, disjoint from every other argument; not needed (NULL) when dgamma
+ *   and dbeta are NULL.
+ * Outputs must not overlap inputs or each other.  Limits and errors as
+ * gl_layer_norm, and GL_ERR_WORKSPACE.
+ * -------------------------------------------------------------------------*/
+size_t gl_layer_norm_backward_workspace_bytes(int R, int C, gl_dtype dt);
+gl_status gl_layer_norm_backward(const void* dy, long long lddy, const void* x, long long ldx, int R,
+                                 int C, const float* mean, const float* rstd, const void* gamma,
+                                 gl_dtype dt, void* dx, float* dgamma, float* dbeta,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of one 8-bit row of K values: K rounded up to 16 (0 when K is outside
+ * [1, GL_MAX_Q8_K], the longest row whose products' sums fit 32 bits). */
+#define GL_MAX_Q8_K 131071
+int gl_q8_row_bytes(int K);
+
+/* ---------------------------------------------------------------------------
+ * gl_quantize_rows -- rows to 8 bits, symmetric, each with its own scale:
+ *   top = max_k |x[r, k]|;  scale[r] = top / 127;  q[r, k] = rne(127 x[r, k] / top)
+ * (the correctly rounded fp32 quotient, ties to even).  A row with top < 2^-118
+ * counts as zero: q = 0, scale = 0.  A row with a NaN or an infinity has q = 0
+ * and scale = NaN, so that what is computed from it is NaN.
+ *   x [R, K] (dt), rows ldx apart; q [R, Kp] int8, scale [R] fp32; neither may
+ *   overlap x or the other.
+ * Limits: 1 <= K <= GL_MAX_Q8_K.  Errors as gl_layer_norm.
+ * -------------------------------------------------------------------------*/
+gl_status gl_quantize_rows(const void* x, int R, int K, long long ldx, gl_dtype dt, int8_t* q,
+                           float* scale, hipStream_t stream);
+
+/* gl_layer_norm_q8 -- gl_layer_norm and gl_quantize_rows in one pass: the
+ * normalised row stays in fp32 until it is brought to 8 bits. */
+gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const void* gamma,
+                           const void* beta, float eps, gl_dtype dt, int8_t* q, float* scale,
+                           hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * gl_linear_q8 -- one fully connected layer on 8-bit rows:
+ *   out[r, o] = act_out( (sum_k q[r, k] Wq[o, k]) scale[r] w_scale[o] + bias[o] )
+ *               + residual[r, o]
+ * The sum is exact (int32); the rest is fp32, rounded once to dt.
+ *   q [R, Kp], scale [R]: 8-bit rows of K values; Wq [Cout, Kp], w_scale [Cout]:
+ *   the weights likewise.  bias [Cout] (dt) or NULL; residual [R, Cout] (dt) or
+ *   NULL, and may be `out` itself; out [R, Cout] (dt), must not overlap the
+ *   other arguments.  Any whole number of -128 .. 127 is taken as a value.
+ * Limits: R, Cout >= 1; 1 <= K <= GL_MAX_Q8_K.
+ * -------------------------------------------------------------------------*/
+gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const int8_t* Wq,
+                       const float* w_scale, const void* bias, int Cout, gl_act act_out,
+                       const void* residual, gl_dtype dt, void* out, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

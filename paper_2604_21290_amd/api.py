@@ -23,12 +23,14 @@ GL_SCHED_LOOKAHEAD, GL_SCHED_STANDARD, GL_SCHED_LOOKAHEAD_FUSED = 0, 1, 2
 GL_TIME_BUILD, GL_TIME_UPDATE, GL_TIME_FUSED, GL_TIME_LINEAR = 0, 1, 2, 3
 GL_ACT_NONE, GL_ACT_GELU = 0, 1
 GL_MAX_KD, GL_MAX_M, GL_MAX_K = 64, 4096, 64
+GL_MAX_Q8_K = 131071
 
 STATUS = {0: "GL_OK", 1: "GL_ERR_NULL_PTR", 2: "GL_ERR_BAD_SHAPE", 3: "GL_ERR_BAD_K",
           4: "GL_ERR_UNSUPPORTED", 5: "GL_ERR_ALIGNMENT", 6: "GL_ERR_ALIAS", 7: "GL_ERR_HIP",
           8: "GL_ERR_BAD_HANDLE", 9: "GL_ERR_WORKSPACE"}
 
 _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+_ll = ctypes.c_longlong
 
 VIG_PARAMS = ("W_in", "b_in", "W_upd", "b_upd", "W_out", "b_out", "W_1", "b_1", "W_2", "b_2")
 
@@ -63,6 +65,14 @@ SIGNATURES = {
                      _sz, _vp, _vp, _i, _vp],
     "gl_vig_stack": [_vp, _vp, _i, _i, _i, _i, _i, _i, _i, ctypes.POINTER(_i),
                      ctypes.POINTER(VigParams), _i, _i, _vp, _sz, _vp],
+    "gl_layer_norm": [_vp, _i, _i, _ll, _vp, _vp, _f, _i, _vp, _vp, _vp, _vp],
+    "gl_layer_norm_backward_workspace_bytes": [_i, _i, _i],
+    "gl_layer_norm_backward": [_vp, _ll, _vp, _ll, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp,
+                               _sz, _vp],
+    "gl_q8_row_bytes": [_i],
+    "gl_quantize_rows": [_vp, _i, _i, _ll, _i, _vp, _vp, _vp],
+    "gl_layer_norm_q8": [_vp, _i, _i, _ll, _vp, _vp, _f, _i, _vp, _vp, _vp],
+    "gl_linear_q8": [_vp, _vp, _i, _i, _vp, _vp, _vp, _i, _i, _vp, _i, _vp, _vp],
     "gl_status_string": [_i],
     "gl_last_error": [],
     "gl_version": [],
@@ -70,6 +80,7 @@ SIGNATURES = {
 RESTYPES = {"gl_status_string": ctypes.c_char_p, "gl_last_error": ctypes.c_char_p,
             "gl_vig_workspace_bytes": ctypes.c_size_t, "gl_mrconv_workspace_bytes": ctypes.c_size_t,
             "gl_mrconv_heads_workspace_bytes": ctypes.c_size_t,
+            "gl_layer_norm_backward_workspace_bytes": ctypes.c_size_t,
             "gl_graphleap_workspace_bytes": ctypes.c_size_t}
 
 _lib = None
@@ -253,6 +264,216 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None,
         out = torch.empty(x.shape[:-1] + (Cout,), dtype=x.dtype, device=x.device)
     _call("gl_linear", _p(x), R, K, _p(W), _p(bias), Cout, act_in, act_out, _p(residual), _dt(x),
           _p(out), _s(stream))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# layer norm and 8-bit layers
+# ---------------------------------------------------------------------------
+class Q8Rows:
+    """8-bit rows (gl_quantize_rows): q [..., Kp] int8, whose last Kp - K bytes
+    are zero, scale [...] float32 and the rows' length K; the values are
+    q[..., :K] * scale[..., None]."""
+    __slots__ = ("q", "scale", "K")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, K: int):
+        self.q, self.scale, self.K = q, scale, K
+
+    @property
+    def shape(self):
+        return self.q.shape[:-1] + (self.K,)
+
+    def dequantize(self, dtype=torch.float32) -> torch.Tensor:
+        return (self.q[..., : self.K].float() * self.scale[..., None]).to(dtype)
+
+
+def q8_row_bytes(K: int) -> int:
+    """Bytes of one 8-bit row of K values (K rounded up to 16)."""
+    n = lib().gl_q8_row_bytes(K)
+    if not n:
+        raise GraphLeapError("gl_q8_row_bytes", 2, f"K={K} outside [1, {GL_MAX_Q8_K}]")
+    return n
+
+
+def _rows(x: torch.Tensor):
+    """(R, C, ld) of a device tensor whose leading axes are rows a uniform stride apart."""
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("rows must be a device tensor")
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {x.device}, the current device is {torch.cuda.current_device()}")
+    C = x.shape[-1]
+    if x.is_contiguous():
+        return (x.numel() // C if C else 0), C, C
+    sh, st = x.shape, x.stride()
+    if C > 1 and st[-1] != 1:
+        raise ValueError("the last axis of rows must be contiguous")
+    ld = rows = None
+    for n, d in zip(reversed(sh[:-1]), reversed(st[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld, rows = d, n
+        elif d == ld * rows:
+            rows *= n
+        else:
+            raise ValueError(f"rows of shape {tuple(sh)} and strides {st} are not a uniform stride apart")
+    return x.numel() // C if C else 0, C, C if ld is None else ld
+
+
+def _like(name: str, t, shape, dtype, x: torch.Tensor):
+    """An argument that must be contiguous and have this shape and type, on x's device."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != x.device
+                          or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
+                         f"{x.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def _new(shape, dtype, x: torch.Tensor, stream):
+    """A tensor to write on `stream` (the current one if None)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=x.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=x.device)
+
+
+def _hold(stream, *ts):
+    """Tensors of other streams that `stream` uses are not handed out again before it has."""
+    if stream is not None:
+        for t in ts:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None,
+               beta: torch.Tensor | None = None, eps: float = 1e-5, stats: bool = False,
+               out: torch.Tensor | None = None, stream=None):
+    """(x - mean) * rstd * gamma + beta over the last axis (gl_layer_norm).  x may
+    be a slice of wider rows.  stats: return (out, mean, rstd), the row statistics
+    in float32 that layer_norm_backward takes."""
+    R, C, ld = _rows(x)
+    _like("gamma", gamma, (C,), x.dtype, x)
+    _like("beta", beta, (C,), x.dtype, x)
+    if out is None:
+        out = _new(x.shape, x.dtype, x, stream)
+    else:
+        _like("out", out, x.shape, x.dtype, x)
+    mean = rstd = None
+    if stats:
+        mean = _new(x.shape[:-1], torch.float32, x, stream)
+        rstd = _new(x.shape[:-1], torch.float32, x, stream)
+    _hold(stream, x, gamma, beta, out)
+    _call("gl_layer_norm", x.data_ptr(), R, C, ld, _ptr(gamma), _ptr(beta), eps, _dt(x),
+          out.data_ptr(), _ptr(mean), _ptr(rstd), _s(stream))
+    return (out, mean, rstd) if stats else out
+
+
+def layer_norm_backward_workspace(x: torch.Tensor) -> Workspace:
+    """Workspace of gl_layer_norm_backward for rows shaped like x."""
+    R, C, _ = _rows(x)
+    return Workspace(lib().gl_layer_norm_backward_workspace_bytes(R, C, _dt(x)), x.device)
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        gamma: torch.Tensor | None = None, need=(True, True, True),
+                        ws: Workspace | None = None, stream=None):
+    """(dx, dgamma, dbeta) of layer_norm from its output's gradient dy, its input
+    and the row statistics it returned (gl_layer_norm_backward); dgamma and dbeta
+    are float32 sums over all rows.  need: which of the three to compute (None
+    for the others).  ws: the call's workspace (allocated here when not given)."""
+    R, C, ldx = _rows(x)
+    Rd, Cd, lddy = _rows(dy)
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError(f"dy {dy.dtype} {tuple(dy.shape)} does not match x {x.dtype} {tuple(x.shape)}")
+    _like("mean", mean, x.shape[:-1], torch.float32, x)
+    _like("rstd", rstd, x.shape[:-1], torch.float32, x)
+    _like("gamma", gamma, (C,), x.dtype, x)
+    dx = _new(x.shape, x.dtype, x, stream) if need[0] else None
+    dgamma = _new((C,), torch.float32, x, stream) if need[1] else None
+    dbeta = _new((C,), torch.float32, x, stream) if need[2] else None
+    wp, wn = None, 0
+    if need[1] or need[2]:
+        if ws is None:
+            wn = lib().gl_layer_norm_backward_workspace_bytes(R, C, _dt(x))
+            buf = _new((wn,), torch.uint8, x, stream)
+            wp = buf.data_ptr()
+        else:
+            wp, wn = ws.ptr, ws.nbytes
+            if stream is not None:
+                ws.record_stream(stream)
+    _hold(stream, dy, x, mean, rstd, gamma)
+    _call("gl_layer_norm_backward", dy.data_ptr(), lddy, x.data_ptr(), ldx, R, C, mean.data_ptr(),
+          rstd.data_ptr(), _ptr(gamma), _dt(x), _ptr(dx), _ptr(dgamma), _ptr(dbeta), wp, wn,
+          _s(stream))
+    return dx, dgamma, dbeta
+
+
+def _q8_out(x: torch.Tensor, R: int, K: int, out: Q8Rows | None, stream) -> Q8Rows:
+    Kp = (K + 15) // 16 * 16
+    if out is None:
+        return Q8Rows(_new(x.shape[:-1] + (Kp,), torch.int8, x, stream),
+                      _new(x.shape[:-1], torch.float32, x, stream), K)
+    if out.K != K:
+        raise ValueError(f"out holds rows of {out.K} values, x has {K}")
+    _like("out.q", out.q, x.shape[:-1] + (Kp,), torch.int8, x)
+    _like("out.scale", out.scale, x.shape[:-1], torch.float32, x)
+    _hold(stream, out.q, out.scale)
+    return out
+
+
+def quantize_rows(x: torch.Tensor, out: Q8Rows | None = None, stream=None) -> Q8Rows:
+    """x's rows (its last axis) as 8-bit integers with a scale each
+    (gl_quantize_rows): activations per token, or a weight per output channel."""
+    R, K, ld = _rows(x)
+    out = _q8_out(x, R, K, out, stream)
+    _hold(stream, x)
+    _call("gl_quantize_rows", x.data_ptr(), R, K, ld, _dt(x), out.q.data_ptr(), out.scale.data_ptr(),
+          _s(stream))
+    return out
+
+
+def layer_norm_q8(x: torch.Tensor, gamma: torch.Tensor | None = None,
+                  beta: torch.Tensor | None = None, eps: float = 1e-5, out: Q8Rows | None = None,
+                  stream=None) -> Q8Rows:
+    """layer_norm and quantize_rows in one pass (gl_layer_norm_q8)."""
+    R, K, ld = _rows(x)
+    _like("gamma", gamma, (K,), x.dtype, x)
+    _like("beta", beta, (K,), x.dtype, x)
+    out = _q8_out(x, R, K, out, stream)
+    _hold(stream, x, gamma, beta)
+    _call("gl_layer_norm_q8", x.data_ptr(), R, K, ld, _ptr(gamma), _ptr(beta), eps, _dt(x),
+          out.q.data_ptr(), out.scale.data_ptr(), _s(stream))
+    return out
+
+
+def linear_q8(x: Q8Rows, W: Q8Rows, bias: torch.Tensor | None = None, act_out: int = GL_ACT_NONE,
+              residual: torch.Tensor | None = None, dtype=torch.bfloat16,
+              out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """out[..., Cout] = act_out(x W^T + bias) + residual of 8-bit rows x and weights
+    W [Cout, K] (gl_linear_q8); bias, residual and out are in `dtype`."""
+    R, Kp, _ = _rows(x.q)
+    if W.q.dim() != 2 or x.K != W.K:
+        raise ValueError(f"linear_q8: rows {tuple(x.shape)} do not match weights {tuple(W.shape)}")
+    Cout, lead = W.q.shape[0], x.q.shape[:-1]
+    want = (x.K + 15) // 16 * 16
+    _like("x.q", x.q, lead + (want,), torch.int8, x.q)
+    _like("x.scale", x.scale, lead, torch.float32, x.q)
+    _like("W.q", W.q, (Cout, want), torch.int8, x.q)
+    _like("W.scale", W.scale, (Cout,), torch.float32, x.q)
+    _like("bias", bias, (Cout,), dtype, x.q)
+    _like("residual", residual, lead + (Cout,), dtype, x.q)
+    if out is None:
+        out = _new(lead + (Cout,), dtype, x.q, stream)
+    else:
+        _like("out", out, lead + (Cout,), dtype, x.q)
+    _hold(stream, x.q, x.scale, W.q, W.scale, bias, residual, out)
+    _call("gl_linear_q8", x.q.data_ptr(), x.scale.data_ptr(), R, x.K, W.q.data_ptr(),
+          W.scale.data_ptr(), _ptr(bias), Cout, act_out, _ptr(residual), _dt(out), out.data_ptr(),
+          _s(stream))
     return out
 
 

@@ -1202,3 +1202,211 @@ extern "C" gl_status gl_mrconv_noalloc(const void* x, int B, int N, int C, const
                                    dt == GL_BF16, rt, ws, stream);
   return e == hipSuccess ? GL_OK : hip_fail(e, "mrconv launch");
 }
+
+// ---------------------------------------------------------------------------
+// layer norm and 8-bit layers
+// ---------------------------------------------------------------------------
+namespace {
+
+// Bytes from the first element of R strided rows to the end of the last one.
+size_t span(int R, int C, long long ld, size_t es) { return ((size_t)(R - 1) * ld + C) * es; }
+
+gl_status check_rows(const char* who, const void* x, int R, int C, long long ld, gl_dtype dt) {
+  if (!dtype_ok(dt)) return fail(GL_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, (int)dt);
+  if (R < 1 || C < 1 || !size_ok(R, 1, C))
+    return fail(GL_ERR_BAD_SHAPE, "%s: bad shape R=%d C=%d", who, R, C);
+  if (R > 1 && (ld < C || ld > (1LL << 40) / R))
+    return fail(GL_ERR_BAD_SHAPE, "%s: rows of %d channels %lld elements apart", who, C, ld);
+  if (!aligned(x, esize(dt))) return fail(GL_ERR_ALIGNMENT, "%s: rows need their elements' alignment", who);
+  return GL_OK;
+}
+
+// The arguments that gl_layer_norm and gl_layer_norm_q8 share.
+gl_status check_norm(const char* who, const void* x, int R, int C, long long ldx, const void* gamma,
+                     const void* beta, float eps, gl_dtype dt) {
+  gl_status s = check_rows(who, x, R, C, ldx, dt);
+  if (s != GL_OK) return s;
+  if (!(eps >= 0.f) || eps > 3.4e38f) return fail(GL_ERR_BAD_SHAPE, "%s: bad eps %g", who, eps);
+  if ((gamma && !aligned(gamma, esize(dt))) || (beta && !aligned(beta, esize(dt))))
+    return fail(GL_ERR_ALIGNMENT, "%s: gamma and beta need their elements' alignment", who);
+  return GL_OK;
+}
+
+using Range = std::pair<const void*, size_t>;
+
+// No output may overlap an input or another output.
+gl_status check_apart(const char* who, std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    for (const Range& i : ins)
+      if (overlap(o->first, o->second, i.first, i.second))
+        return fail(GL_ERR_ALIAS, "%s: an output overlaps an input", who);
+    for (auto p = o + 1; p != outs.end(); ++p)
+      if (overlap(o->first, o->second, p->first, p->second))
+        return fail(GL_ERR_ALIAS, "%s: two outputs overlap", who);
+  }
+  return GL_OK;
+}
+
+gl_status check_q8_rows(const char* who, const int8_t* q, const float* scale, int K) {
+  if (K < 1 || K > GL_MAX_Q8_K)
+    return fail(GL_ERR_BAD_SHAPE, "%s: K=%d outside [1, %d]", who, K, GL_MAX_Q8_K);
+  if (!aligned(q, 16) || !aligned(scale, 4))
+    return fail(GL_ERR_ALIGNMENT, "%s: 8-bit rows need 16-byte, scales 4-byte alignment", who);
+  return GL_OK;
+}
+
+gl::RowArgs row_args(const void* x, int R, int C, long long ldx, const void* gamma, const void* beta,
+                     float eps) {
+  gl::RowArgs a{};
+  a.x = x;
+  a.ldx = ldx;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.R = R;
+  a.C = C;
+  a.eps = eps;
+  a.inv_c = (float)(1.0 / C);
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+gl_status gl_layer_norm(const void* x, int R, int C, long long ldx, const void* gamma,
+                        const void* beta, float eps, gl_dtype dt, void* out, float* mean,
+                        float* rstd, hipStream_t stream) {
+  if (!x || !out) return fail(GL_ERR_NULL_PTR, "layer_norm: x and out are required");
+  gl_status s = check_norm("layer_norm", x, R, C, ldx, gamma, beta, eps, dt);
+  if (s != GL_OK) return s;
+  const size_t es = esize(dt);
+  if (!aligned(out, es) || (mean && !aligned(mean, 4)) || (rstd && !aligned(rstd, 4)))
+    return fail(GL_ERR_ALIGNMENT, "layer_norm: outputs need their elements' alignment");
+  if ((s = check_apart("layer_norm",
+                       {{out, (size_t)R * C * es}, {mean, (size_t)R * 4}, {rstd, (size_t)R * 4}},
+                       {{x, span(R, C, ldx, es)}, {gamma, C * es}, {beta, C * es}})) != GL_OK)
+    return s;
+  gl::RowArgs a = row_args(x, R, C, ldx, gamma, beta, eps);
+  a.out = out;
+  a.mean = mean;
+  a.rstd = rstd;
+  hipError_t e = gl::launch_layer_norm(a, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, "layer_norm launch");
+}
+
+size_t gl_layer_norm_backward_workspace_bytes(int R, int C, gl_dtype dt) {
+  if (!dtype_ok(dt) || R < 1 || C < 1 || !size_ok(R, 1, C)) return 0;
+  return gl::norm_grad_ws_bytes(R, C, dt == GL_BF16);
+}
+
+gl_status gl_layer_norm_backward(const void* dy, long long lddy, const void* x, long long ldx, int R,
+                                 int C, const float* mean, const float* rstd, const void* gamma,
+                                 gl_dtype dt, void* dx, float* dgamma, float* dbeta,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const char* who = "layer_norm_backward";
+  if (!dy || !x || !mean || !rstd || (!dx && !dgamma && !dbeta))
+    return fail(GL_ERR_NULL_PTR, "%s: dy, x, mean, rstd and an output are required", who);
+  gl_status s = check_rows(who, x, R, C, ldx, dt);
+  if (s != GL_OK || (s = check_rows(who, dy, R, C, lddy, dt)) != GL_OK) return s;
+  const size_t es = esize(dt), xb = span(R, C, ldx, es), yb = span(R, C, lddy, es),
+               rb = (size_t)R * 4, cb = (size_t)C * 4, ob = (size_t)R * C * es;
+  if (!aligned(mean, 4) || !aligned(rstd, 4) || (gamma && !aligned(gamma, es)) ||
+      (dx && !aligned(dx, es)) || (dgamma && !aligned(dgamma, 4)) || (dbeta && !aligned(dbeta, 4)))
+    return fail(GL_ERR_ALIGNMENT, "%s: tensors need their elements' alignment", who);
+  if ((s = check_apart(who, {{dx, ob}, {dgamma, cb}, {dbeta, cb}},
+                       {{x, xb}, {dy, yb}, {mean, rb}, {rstd, rb}, {gamma, C * es}})) != GL_OK)
+    return s;
+  if (dgamma || dbeta) {
+    s = check_ws(who, gl::norm_grad_ws_bytes(R, C, dt == GL_BF16), workspace, workspace_bytes,
+                 {{x, xb}, {dy, yb}, {mean, rb}, {rstd, rb}, {gamma, gamma ? C * es : 0},
+                  {dx, dx ? ob : 0}, {dgamma, dgamma ? cb : 0}, {dbeta, dbeta ? cb : 0}});
+    if (s != GL_OK) return s;
+  }
+  gl::NormGradArgs a{};
+  a.dy = dy;
+  a.x = x;
+  a.lddy = lddy;
+  a.ldx = ldx;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.gamma = gamma;
+  a.dx = dx;
+  a.dgamma = dgamma;
+  a.dbeta = dbeta;
+  a.part = static_cast<float*>(workspace);
+  a.R = R;
+  a.C = C;
+  a.inv_c = (float)(1.0 / C);
+  hipError_t e = gl::launch_norm_grad(a, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, "layer_norm_backward launch");
+}
+
+int gl_q8_row_bytes(int K) { return K < 1 || K > GL_MAX_Q8_K ? 0 : (int)gl::q8_row_bytes(K); }
+
+static gl_status rows_q8(const char* who, bool norm, const void* x, int R, int C, long long ldx,
+                         const void* gamma, const void* beta, float eps, gl_dtype dt, int8_t* q,
+                         float* scale, hipStream_t stream) {
+  if (!x || !q || !scale) return fail(GL_ERR_NULL_PTR, "%s: x, q and scale are required", who);
+  gl_status s = check_norm(who, x, R, C, ldx, gamma, beta, eps, dt);
+  if (s != GL_OK || (s = check_q8_rows(who, q, scale, C)) != GL_OK) return s;
+  const size_t es = esize(dt);
+  gl::RowArgs a = row_args(x, R, C, ldx, gamma, beta, eps);
+  a.q = q;
+  a.scale = scale;
+  a.Kp = (int)gl::q8_row_bytes(C);
+  if ((s = check_apart(who, {{q, (size_t)R * a.Kp}, {scale, (size_t)R * 4}},
+                       {{x, span(R, C, ldx, es)}, {gamma, C * es}, {beta, C * es}})) != GL_OK)
+    return s;
+  hipError_t e = norm ? gl::launch_layer_norm_q8(a, dt == GL_BF16, stream)
+                      : gl::launch_quantize_rows(a, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, who);
+}
+
+gl_status gl_quantize_rows(const void* x, int R, int K, long long ldx, gl_dtype dt, int8_t* q,
+                           float* scale, hipStream_t stream) {
+  return rows_q8("quantize_rows", false, x, R, K, ldx, nullptr, nullptr, 0.f, dt, q, scale, stream);
+}
+
+gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const void* gamma,
+                           const void* beta, float eps, gl_dtype dt, int8_t* q, float* scale,
+                           hipStream_t stream) {
+  return rows_q8("layer_norm_q8", true, x, R, C, ldx, gamma, beta, eps, dt, q, scale, stream);
+}
+
+gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const int8_t* Wq,
+                       const float* w_scale, const void* bias, int Cout, gl_act act_out,
+                       const void* residual, gl_dtype dt, void* out, hipStream_t stream) {
+  const char* who = "linear_q8";
+  if (!q || !scale || !Wq || !w_scale || !out)
+    return fail(GL_ERR_NULL_PTR, "%s: q, scale, Wq, w_scale and out are required", who);
+  if (!dtype_ok(dt)) return fail(GL_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, (int)dt);
+  if (act_out != GL_ACT_NONE && act_out != GL_ACT_GELU)
+    return fail(GL_ERR_UNSUPPORTED, "%s: unknown activation", who);
+  gl_status s = check_q8_rows(who, q, scale, K);
+  if (s != GL_OK || (s = check_q8_rows(who, Wq, w_scale, K)) != GL_OK) return s;
+  if (R < 1 || Cout < 1 || !size_ok(R, 1, K) || !size_ok(R, 1, Cout) || !size_ok(Cout, 1, K))
+    return fail(GL_ERR_BAD_SHAPE, "%s: bad shape R=%d K=%d Cout=%d", who, R, K, Cout);
+  const size_t es = esize(dt), ob = (size_t)R * Cout * es, kp = gl::q8_row_bytes(K);
+  if (!aligned(out, es) || (bias && !aligned(bias, es)) || (residual && !aligned(residual, es)))
+    return fail(GL_ERR_ALIGNMENT, "%s: bias, residual and out need their elements' alignment", who);
+  if ((s = check_apart(who, {{out, ob}},
+                       {{q, R * kp}, {scale, (size_t)R * 4}, {Wq, Cout * kp}, {w_scale, (size_t)Cout * 4},
+                        {bias, Cout * es}, {residual == out ? nullptr : residual, ob}})) != GL_OK)
+    return s;
+  gl::GemmQ8Args a{};
+  a.A = q;
+  a.W = Wq;
+  a.sa = scale;
+  a.sw = w_scale;
+  a.bias = bias;
+  a.residual = residual;
+  a.out = out;
+  a.R = R;
+  a.Kp = (int)kp;
+  a.Cout = Cout;
+  a.act_out = act_out;
+  hipError_t e = gl::launch_gemm_q8(a, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, "linear_q8 launch");
+}
+
+}  // extern "C"

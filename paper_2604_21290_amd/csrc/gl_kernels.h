@@ -61,6 +61,42 @@ struct MlpArgs {
   int R, C;
 };
 
+// Layer norm and 8-bit rows: x [R, C], rows ldx elements apart.
+struct RowArgs {
+  const void* x;
+  long long ldx;
+  const void *gamma, *beta;  // [C] or null
+  void* out;                 // [R, C] (layer norm)
+  float *mean, *rstd;        // [R] or null
+  int8_t* q;                 // [R, Kp] (8-bit rows, Kp = q8_row_bytes(C))
+  float* scale;              // [R]
+  int R, C, Kp;
+  float eps, inv_c;          // inv_c = 1 / C
+};
+
+struct NormGradArgs {
+  const void *dy, *x;
+  long long lddy, ldx;
+  const float *mean, *rstd;  // [R]
+  const void* gamma;         // [C] or null
+  void* dx;                  // [R, C] or null
+  float *dgamma, *dbeta;     // [C] or null
+  float* part;               // workspace: the workgroups' sums
+  int R, C;
+  float inv_c;
+};
+
+// out[R, Cout] = act_out((A W^T) sa sw + bias) + residual, A and W 8-bit rows of Kp bytes.
+struct GemmQ8Args {
+  const int8_t *A, *W;
+  const float *sa, *sw;  // [R], [Cout]
+  const void* bias;      // [Cout] or null
+  const void* residual;  // [R, Cout] or null (may be `out` itself)
+  void* out;
+  int R, Kp, Cout;
+  int act_out;
+};
+
 // Workgroups are dispatched round-robin over the 8 XCDs (workgroup id mod 8).
 // Map dispatch ids so that consecutive logical ids (neighbouring tiles of the
 // same image, which share key rows) land on the same XCD and its L2.
@@ -172,5 +208,15 @@ hipError_t launch_block_gather(const KnnArgs& ka, const MrArgs& ma, void* xcat,
 // reduction) of the H x W node grid.
 hipError_t launch_pool(const void* x, void* keys, int B, int H, int W, int C, int r, int dt_bf16,
                        hipStream_t stream, bool max_pool = false);
+
+// Rows of any width, stride and alignment (norm.hip, norm_grad.hip).
+hipError_t launch_layer_norm(const RowArgs& a, int dt_bf16, hipStream_t stream);
+hipError_t launch_layer_norm_q8(const RowArgs& a, int dt_bf16, hipStream_t stream);
+hipError_t launch_quantize_rows(const RowArgs& a, int dt_bf16, hipStream_t stream);
+size_t norm_grad_ws_bytes(int R, int C, int dt_bf16);
+hipError_t launch_norm_grad(const NormGradArgs& a, int dt_bf16, hipStream_t stream);
+// Bytes of an 8-bit row of K values: whole 16-byte vectors.
+constexpr long long q8_row_bytes(long long K) { return (K + 15) / 16 * 16; }
+hipError_t launch_gemm_q8(const GemmQ8Args& a, int dt_bf16, hipStream_t stream);
 
 }  // namespace gl

@@ -1,0 +1,162 @@
+// Device helpers of the kernels that work on whole rows of channels (layer norm,
+// its gradient, the 8-bit rows): a row in chunks of 16 bytes, sums and maxima over
+// the lanes that share a row, and the rounding to 8 bits.
+#pragma once
+
+#include "gl_device.h"
+
+namespace gl {
+
+// ---------------------------------------------------------------------------
+// chunks: 8 bf16 or 4 fp32 values, 16 bytes at any element's place.  A row of C
+// channels is covered by ceil(C / E) of them; where C is not a whole number of
+// chunks the last one is moved back to end with the row, and its first `skip`
+// values, which the chunk before it has too, are left out of sums.  So every
+// access lies inside the row and no width or alignment needs a loop over single
+// values (rows shorter than one chunk aside).
+// ---------------------------------------------------------------------------
+template <int DT>
+struct Chunk;  // DT 1: bf16, 0: fp32
+
+typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4), may_alias));
+
+template <>
+struct Chunk<1> {
+  static constexpr int E = 8;
+  static constexpr size_t kSize = 2;
+  __device__ __forceinline__ static void load(const void* p, size_t i, float* f) {
+    unpack_bf16x8(load16_any(static_cast<const uint16_t*>(p) + i), f);
+  }
+  __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
+    store16_any(static_cast<uint16_t*>(p) + i, pack_bf16x8(f));
+  }
+  __device__ __forceinline__ static float load1(const void* p, size_t i) {
+    return bf16_bits_to_f32(static_cast<const uint16_t*>(p)[i]);
+  }
+  __device__ __forceinline__ static void store1(void* p, size_t i, float f) {
+    static_cast<uint16_t*>(p)[i] = (uint16_t)f32_to_bf16_bits(f);
+  }
+};
+
+template <>
+struct Chunk<0> {
+  static constexpr int E = 4;
+  static constexpr size_t kSize = 4;
+  __device__ __forceinline__ static void load(const void* p, size_t i, float* f) {
+    const u32x4_any4 v = *reinterpret_cast<const u32x4_any4*>(static_cast<const float*>(p) + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(v[j]);
+  }
+  __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
+    u32x4_any4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(f[j]);
+    *reinterpret_cast<u32x4_any4*>(static_cast<float*>(p) + i) = v;
+  }
+  __device__ __forceinline__ static float load1(const void* p, size_t i) {
+    return static_cast<const float*>(p)[i];
+  }
+  __device__ __forceinline__ static void store1(void* p, size_t i, float f) {
+    static_cast<float*>(p)[i] = f;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// sums and maxima over the LPR lanes (16, 64, or a workgroup's LPR / 64 waves) of
+// one row; every lane of the group gets the result, in the same order always.
+// `slot`: LPR / 64 words of LDS for this reduction alone (workgroup rows).
+// ---------------------------------------------------------------------------
+struct AddF {
+  __device__ __forceinline__ static uint32_t of(uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }
+};
+struct MaxU {
+  __device__ __forceinline__ static uint32_t of(uint32_t a, uint32_t b) { return max(a, b); }
+};
+
+template <class Op>
+__device__ __forceinline__ uint32_t reduce16(uint32_t v) {
+  v = Op::of(v, dpp_mov<0xB1>(v));   // quad_perm [1,0,3,2]
+  v = Op::of(v, dpp_mov<0x4E>(v));   // quad_perm [2,3,0,1]
+  v = Op::of(v, dpp_mov<0x141>(v));  // half-row mirror: the other quad of eight
+  return Op::of(v, dpp_mov<0x140>(v));  // row mirror: the other eight
+}
+
+template <class Op, int LPR>
+__device__ __forceinline__ uint32_t reduce_row(uint32_t v, uint32_t* slot) {
+  v = reduce16<Op>(v);
+  if (LPR == 16) return v;
+  const uint32_t a = Op::of(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16));
+  const uint32_t b = Op::of(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48));
+  v = Op::of(a, b);
+  if (LPR == 64) return v;
+  constexpr int NW = LPR / 64;
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = slot[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) v = Op::of(v, slot[w]);
+  return v;
+}
+
+template <int LPR>
+__device__ __forceinline__ float sum_row(float v, uint32_t* slot) {
+  return __uint_as_float(reduce_row<AddF, LPR>(__float_as_uint(v), slot));
+}
+// of the bits of magnitudes: an infinity ranks above every number, a NaN above it
+template <int LPR>
+__device__ __forceinline__ uint32_t max_row(uint32_t v, uint32_t* slot) {
+  return reduce_row<MaxU, LPR>(v, slot);
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit rows: q = rne(127 x / top), scale = top / 127, top the row's largest
+// magnitude.  The quotient is the correctly rounded one (for bf16 it then ties
+// exactly where 127 x / top does): x is taken times 127 2^-e, exact for bf16,
+// with e top's exponent, so nothing over- or underflows that matters; a product
+// with the reciprocal is corrected once by its remainder.  Adding 1.5 2^23
+// rounds to the nearest even whole number and leaves it in the low byte.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kTopMin = 0x04800000u;  // 2^-118: a row below it counts as zero
+
+struct RowQ8 {
+  float c, a, inv, scale;
+  __device__ __forceinline__ explicit RowQ8(uint32_t top) {
+    const bool zero = top < kTopMin, bad = top >= 0x7f800000u;  // an infinity or a NaN in the row
+    const uint32_t t = zero || bad ? 0x3f800000u : top;
+    a = __uint_as_float((t & 0x7fffffu) | 0x3f800000u);  // in [1, 2)
+    const float r = __builtin_amdgcn_rcpf(a);
+    inv = fmaf(fmaf(-a, r, 1.f), r, r);
+    // 127 2^-e; 0 brings every value to 0
+    c = zero || bad ? 0.f : __uint_as_float(((133u + 127u - (t >> 23)) << 23) | 0x7e0000u);
+    const float f = __uint_as_float(t), s = f * (1.f / 127.f);
+    scale = zero ? 0.f : bad ? __uint_as_float(0x7fc00000u)
+                             : fmaf(fmaf(-127.f, s, f), 1.f / 127.f, s);
+    nan = bad;
+  }
+  bool nan;
+  // the quotient's whole number in the low byte
+  __device__ __forceinline__ uint32_t bits(float x) const {
+    const float t = (nan ? 0.f : x) * c;
+    const float q = t * inv;
+    return __float_as_uint(fmaf(fmaf(-q, a, t), inv, q) + 12582912.f);
+  }
+  __device__ __forceinline__ uint32_t pack4(const float* f) const {
+    const uint32_t lo = __builtin_amdgcn_perm(bits(f[1]), bits(f[0]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(bits(f[3]), bits(f[2]), 0x04000c0cu);
+    return lo | hi;
+  }
+};
+
+typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
+typedef uint32_t u32x2_any1 __attribute__((ext_vector_type(2), aligned(1), may_alias));
+
+// E values of a chunk to 8 bits at any place
+template <int E>
+__device__ __forceinline__ void store_q8(int8_t* p, const RowQ8& q, const float* f) {
+  if (E == 8) *reinterpret_cast<u32x2_any1*>(p) = u32x2_any1{q.pack4(f), q.pack4(f + 4)};
+  else *reinterpret_cast<u32_any*>(p) = q.pack4(f);
+}
+
+}  // namespace gl

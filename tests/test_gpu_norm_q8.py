@@ -1,0 +1,472 @@
+"""GPU parity of layer norm, its gradient and the 8-bit layers against the float64
+oracle: widths around every tile's edge, rows shorter than a vector, strided and
+unaligned rows, a single row, zero and constant rows, rows that are not finite,
+offsets past 32 bits, other streams, replayed graphs.
+
+Bounds (u = 2^-8 bf16, 2^-24 fp32 for one rounding to the stored type; e = 2^-24;
+D = 80 + C / 256 fp32 additions at most between a term and its row's sum):
+  mean    D e avg|x|
+  rstd    (D + 8) e rstd: squares, their sum, the product with 1/C, eps, the root
+  y       |gamma| rstd (mean's + |d| (D + 12) e) + 3 e (|y| + |beta|), then u |y|
+  dx      rstd (4 e |h| + (D + 4) e (avg|h| + |xh| avg|h xh|) + 4 e |xh| avg|h xh|), u |dx|
+  dgamma  (R / 16 + 256) e sum|dy xh| + 3 e sum|dy xh|; dbeta alike: a lane adds at
+          most R / 16 rows, then the workgroups' sums are added
+  8 bits  of stored rows: equal.  Of a norm: half a step, and y's bound in steps
+  layer   3 e |sum| + e |y|, through the GELU 1.13 times that and 3e-7 |y|; u |out|"""
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import from_dev, require_gpu
+from oracle import norm_q8_ref as Q
+
+pytestmark = pytest.mark.gpu
+
+E32 = 2.0 ** -24
+U = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _api():
+    require_gpu()
+    from paper_2604_21290_amd import api
+    return api
+
+
+def _say(*a):
+    print("[gpu-test]", *a, flush=True)
+
+
+def _f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _rows(g, R, C, dtype, gap=0, shift=0):
+    """R rows of C channels, C + gap elements apart, the first one `shift` in."""
+    spread = np.exp(0.5 * g.standard_normal(C))
+    x = (g.standard_normal((R, C)) * spread + 0.5 * g.standard_normal(C)) * np.exp(0.3 * g.standard_normal((R, 1)))
+    buf = torch.full((shift + R * (C + gap),), float("nan"), dtype=dtype, device="cuda")
+    t = buf[shift:].view(R, C + gap)[:, :C]
+    t.copy_(torch.from_numpy(x).to(dtype))
+    return t
+
+
+def _vec(g, n, dtype, about=0.0):
+    return torch.from_numpy(about + 0.3 * g.standard_normal(n)).to(dtype).cuda()
+
+
+def _y_bound(x, y, mean, rstd, gamma, beta):
+    C = x.shape[-1]
+    D = 80 + C / 256
+    gam = 1.0 if gamma is None else np.abs(gamma)
+    bet = 0.0 if beta is None else np.abs(beta)
+    dm = D * E32 * np.abs(x).mean(-1, keepdims=True)
+    d = np.abs(x - mean[:, None])
+    return gam * rstd[:, None] * (dm + d * (D + 12) * E32) + 3 * E32 * (np.abs(y) + bet)
+
+
+def _within(name, got, ref, bound):
+    assert np.isfinite(got).all(), name
+    over = np.abs(got - ref) > bound
+    assert not over.any(), (name, np.argwhere(over)[:4], float((np.abs(got - ref) / np.maximum(bound, 1e-300)).max()))
+
+
+def _edges(dt):
+    E = 8 if dt == "bf16" else 4
+    out = {1, 2, 3, E - 1, E, E + 1, 80, 192}
+    for n in (16, 32, 64, 128, 256, 512, 1024, 2048):
+        out |= {n * E, n * E + 1} if n > 64 else {n * E - 1, n * E, n * E + 1}
+    return sorted(out)
+
+
+NORM_CASES = [(dt, C, (1, 3, 37)[i % 3], (0, 0, 5)[i % 3], i % 2, i % 4 != 3)
+              for dt in ("bf16", "f32") for i, C in enumerate(_edges(dt))]
+NORM_CASES += [("bf16", 80, 4099, 0, 0, True), ("f32", 192, 1000, 0, 0, True), ("bf16", 640, 2051, 3, 1, True),
+               ("bf16", 33, 20001, 0, 1, True), ("f32", 16, 65537, 0, 0, False), ("bf16", 2560, 700, 0, 0, True)]
+
+
+@pytest.mark.parametrize("dt,C,R,gap,shift,affine", NORM_CASES)
+def test_layer_norm_and_gradient(dt, C, R, gap, shift, affine):
+    api = _api()
+    _say("norm", dt, C, R, gap, shift, affine)
+    dtype = DT[dt]
+    g = np.random.default_rng(C * 7 + R)
+    x, dy = _rows(g, R, C, dtype, gap, shift), _rows(g, R, C, dtype, gap, shift)
+    gamma = _vec(g, C, dtype, 1.0) if affine else None
+    beta = _vec(g, C, dtype) if affine else None
+    y, mean, rstd = api.layer_norm(x, gamma, beta, 1e-5, stats=True)
+    y2 = api.layer_norm(x, gamma, beta, 1e-5)
+    dx, dg, db = api.layer_norm_backward(dy, x, mean, rstd, gamma)
+    dx2, none, db2 = api.layer_norm_backward(dy, x, mean, rstd, gamma, need=(True, False, True))
+    dx3 = api.layer_norm_backward(dy, x, mean, rstd, gamma, need=(True, False, False))[0]
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(dx, dx3)
+    assert none is None and torch.equal(db, db2)
+    xf, dyf = _f64(x), _f64(dy)
+    gam, bet = (None, None) if not affine else (_f64(gamma), _f64(beta))
+    ry, rm, rr = Q.layer_norm_ref(xf, gam, bet, float(np.float32(1e-5)))
+    D = 80 + C / 256
+    _within("mean", _f64(mean), rm, D * E32 * np.abs(xf).mean(-1) + E32 * np.abs(rm))
+    _within("rstd", _f64(rstd), rr, (D + 8) * E32 * rr
+            + rr ** 3 * (D * E32 * np.abs(xf).mean(-1)) ** 2)
+    _within("y", _f64(y), ry, _y_bound(xf, ry, rm, rr, gam, bet) + U[dtype] * np.abs(ry))
+    # the gradient is that of the statistics it is given
+    m, s = _f64(mean), _f64(rstd)
+    rdx, rdg, rdb = Q.layer_norm_backward_ref(dyf, xf, m, s, gam)
+    xh = (xf - m[:, None]) * s[:, None]
+    h = dyf if gam is None else dyf * gam
+    ah, ahx = np.abs(h).mean(-1, keepdims=True), np.abs(h * xh).mean(-1, keepdims=True)
+    b = s[:, None] * (4 * E32 * np.abs(h) + (D + 4) * E32 * (ah + np.abs(xh) * ahx) + 4 * E32 * np.abs(xh) * ahx)
+    _within("dx", _f64(dx), rdx, b + U[dtype] * np.abs(rdx))
+    n = R / 16 + 259
+    _within("dgamma", _f64(dg), rdg, n * E32 * np.abs(dyf * xh).sum(0))
+    _within("dbeta", _f64(db), rdb, n * E32 * np.abs(dyf).sum(0))
+
+
+@pytest.mark.parametrize("dt,C,R,gap,shift,affine", NORM_CASES)
+def test_rows_to_8_bits(dt, C, R, gap, shift, affine):
+    api = _api()
+    _say("q8", dt, C, R, gap, shift)
+    dtype = DT[dt]
+    g = np.random.default_rng(C * 11 + R)
+    x = _rows(g, R, C, dtype, gap, shift)
+    if R > 2:
+        x[1] = 0
+        x[2] = x[2] * 2.0 ** -60
+    gamma = _vec(g, C, dtype, 1.0) if affine else None
+    beta = _vec(g, C, dtype) if affine else None
+    a = api.quantize_rows(x)
+    b = api.layer_norm_q8(x, gamma, beta, 1e-5)
+    torch.cuda.synchronize()
+    Kp = api.q8_row_bytes(C)
+    for r in (a, b):
+        assert r.q.shape == (R, Kp) and r.scale.shape == (R,) and r.K == C
+        assert not r.q[:, C:].any(), "the bytes after a row are zero"
+    xf = _f64(x)
+    rq, rs = Q.quantize_rows_ref(xf)
+    if dt == "f32":  # the definition's fp32 quotient
+        x32 = xf.astype(np.float32)
+        top = np.abs(x32).max(-1, keepdims=True)
+        rq = np.rint(x32 * np.float32(127) / np.where(top > 0, top, np.float32(1))).astype(np.int64)
+    assert (a.q[:, :C].cpu().numpy() == rq).all()
+    assert (np.abs(_f64(a.scale) - rs) <= 2 * E32 * rs).all()
+    gam, bet = (None, None) if not affine else (_f64(gamma), _f64(beta))
+    ry, rm, rr = Q.layer_norm_ref(xf, gam, bet, float(np.float32(1e-5)))
+    by = _y_bound(xf, ry, rm, rr, gam, bet)
+    top, btop = np.abs(ry).max(-1, keepdims=True), by.max(-1, keepdims=True)
+    some = top[:, 0] > 4 * btop[:, 0]  # a row whose norm is zero has rounding alone
+    steps = 127 / np.where(top > 0, top, 1)
+    lim = 0.5 + steps * (by + btop) * 1.01 + 127 * 4 * E32
+    off = np.abs(b.q[:, :C].cpu().numpy() - ry * steps)
+    assert (off <= lim)[some].all(), float((off - lim)[some].max())
+    assert (np.abs(_f64(b.scale) - top[:, 0] / 127) <= (btop[:, 0] + 2 * E32 * top[:, 0]) / 127)[some].all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_8_bit_ties_and_all_values(dt):
+    """Every bf16 magnitude of two binades against several tops: ties go to even."""
+    api = _api()
+    m = torch.arange(128, 256, dtype=torch.float64)
+    for top in (1.0, 254.0, 129.0, 255.0, 2.0 ** -100, 3 * 2.0 ** 120):
+        row = torch.cat([m / 256, m / 512, -m / 256, torch.tensor([1.0], dtype=torch.float64)]) * top
+        x = row.to(DT[dt]).cuda().reshape(1, -1)
+        a = api.quantize_rows(x)
+        torch.cuda.synchronize()
+        xf = _f64(x)
+        q = np.rint(xf * 127 / np.abs(xf).max())
+        assert (a.q[:, : x.shape[1]].cpu().numpy() == q).all(), top
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [3, 80, 640, 5000])
+def test_rows_that_are_not_finite(dt, C):
+    api = _api()
+    dtype = DT[dt]
+    g = np.random.default_rng(C)
+    x = _rows(g, 6, C, dtype)
+    clean = x.clone()
+    x[1, C - 1] = float("nan")
+    x[3, 0] = float("inf")
+    x[4, C // 2] = float("-inf")
+    bad = [1, 3, 4]
+    good = [0, 2, 5]
+    for t in (api.layer_norm(x), api.quantize_rows(x), api.layer_norm_q8(x)):
+        torch.cuda.synchronize()
+        if isinstance(t, torch.Tensor):
+            assert torch.isnan(t[bad]).all()
+            assert torch.equal(t[good], api.layer_norm(clean)[good])
+        else:
+            assert torch.isnan(t.scale[bad]).all() and not t.q[bad].any()
+            assert torch.isfinite(t.scale[good]).all()
+    # what is computed from such rows is NaN, and nothing else is
+    W = api.quantize_rows(_rows(g, 5, C, dtype))
+    out = api.linear_q8(api.quantize_rows(x), W, dtype=dtype)
+    ref = api.linear_q8(api.quantize_rows(clean), W, dtype=dtype)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[bad]).all() and torch.equal(out[good], ref[good])
+
+
+def test_constant_and_zero_rows():
+    api = _api()
+    x = torch.zeros((4, 192), device="cuda")
+    x[1] = 3.0
+    x[2] = -1e-30
+    x[3] = 2.0 ** -119
+    y, mean, rstd = api.layer_norm(x, None, None, 1e-5, stats=True)
+    a = api.quantize_rows(x)
+    torch.cuda.synchronize()
+    assert (y[0] == 0).all() and rstd[0].item() == pytest.approx(1e-5 ** -0.5, rel=1e-6)
+    # a constant row: the deviations are the mean's rounding
+    assert y[1].abs().max().item() <= 3.0 * 80 * E32 * 320
+    assert (a.q[0] == 0).all() and a.scale[0] == 0
+    assert (a.q[1] == 127).all() and (a.q[2] == -127).all()
+    assert (a.q[3] == 0).all() and a.scale[3] == 0
+
+
+LAYER_CASES = [
+    # R, K, Cout, gelu, residual, bias
+    (1, 1, 1, False, False, True), (1, 16, 8, False, True, True), (1, 640, 2560, True, False, True),
+    (2, 15, 7, False, True, False), (3, 17, 33, True, True, True), (7, 130, 250, False, False, True),
+    (16, 64, 64, False, True, True), (17, 128, 16, True, False, True), (31, 4665, 72, False, True, True),
+    (33, 257, 129, False, True, True), (64, 2560, 640, False, True, True), (65, 63, 65, False, False, False),
+    (128, 1024, 128, False, True, True), (129, 129, 129, True, True, True), (196, 192, 768, True, False, True),
+    (777, 1001, 333, False, False, True), (1000, 80, 320, True, False, True), (1025, 1040, 1025, False, True, True),
+    (4100, 320, 80, False, True, True), (6272, 192, 768, True, False, True), (12544, 72, 641, False, True, True),
+    (20000, 96, 24, False, True, True), (2049, 4096, 515, False, False, True), (5, 131071, 9, False, False, True),
+    (8192, 640, 2048, True, True, True), (3000, 16, 4000, False, True, True),
+]
+
+
+def _layer(g, api, R, K, Cout, dtype, gelu, residual, bias):
+    q = torch.zeros((R, api.q8_row_bytes(K)), dtype=torch.int8, device="cuda")
+    q[:, :K] = torch.from_numpy(g.integers(-127, 128, (R, K), dtype=np.int8))
+    w = torch.zeros((Cout, api.q8_row_bytes(K)), dtype=torch.int8, device="cuda")
+    w[:, :K] = torch.from_numpy(g.integers(-128, 128, (Cout, K), dtype=np.int8))
+    # scales of one dense layer: outputs of order one
+    xs = torch.from_numpy(np.exp(0.4 * g.standard_normal(R)) / 73).float().cuda()
+    ws = torch.from_numpy(np.exp(0.4 * g.standard_normal(Cout)) / (73 * K ** 0.5)).float().cuda()
+    b = _vec(g, Cout, dtype) if bias else None
+    res = _rows(g, R, Cout, dtype) if residual else None
+    return api.Q8Rows(q, xs, K), api.Q8Rows(w, ws, K), b, res
+
+
+def _check_layer(x, W, b, res, gelu, out, rows=None):
+    q, s = x.q[:, : x.K].cpu().numpy(), _f64(x.scale)
+    o, r = out, res
+    if rows is not None:
+        q, s, o, r = q[rows], s[rows], out[rows], None if res is None else res[rows]
+    wq, ws = W.q[:, : W.K].cpu().numpy(), _f64(W.scale)
+    bf, rf = None if b is None else _f64(b), None if r is None else _f64(r)
+    lin = Q.linear_q8_ref(q, s, wq, ws)
+    y = lin if bf is None else lin + bf
+    ref = Q.linear_q8_ref(q, s, wq, ws, bf, gelu, rf)
+    bound = 3 * E32 * np.abs(lin) + E32 * np.abs(y)
+    if gelu:
+        bound = 1.13 * bound + 3e-7 * np.abs(y)
+    if rf is not None:
+        bound = bound + E32 * (np.abs(ref) + np.abs(rf))
+    _within("layer", _f64(o), ref, bound + U[out.dtype] * np.abs(ref) + 1e-37)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("R,K,Cout,gelu,residual,bias", LAYER_CASES)
+def test_linear_q8(dt, R, K, Cout, gelu, residual, bias):
+    api = _api()
+    _say("linear_q8", dt, R, K, Cout, gelu, residual, bias)
+    g = np.random.default_rng(R + 3 * K + 5 * Cout)
+    x, W, b, res = _layer(g, api, R, K, Cout, DT[dt], gelu, residual, bias)
+    act = api.GL_ACT_GELU if gelu else api.GL_ACT_NONE
+    out = api.linear_q8(x, W, b, act, res, DT[dt])
+    again = api.linear_q8(x, W, b, act, res, DT[dt])
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
+    _check_layer(x, W, b, res, gelu, out)
+    if res is not None:  # the residual updated in place
+        api.linear_q8(x, W, b, act, res, DT[dt], out=res)
+        torch.cuda.synchronize()
+        assert torch.equal(res, out)
+
+
+@pytest.mark.parametrize("R,Cout,shift", [(5, 64, 1), (300, 257, 3), (5000, 640, 5), (20000, 81, 7)])
+def test_linear_q8_unaligned_output(R, Cout, shift):
+    api = _api()
+    g = np.random.default_rng(R)
+    x, W, b, _ = _layer(g, api, R, 200, Cout, torch.bfloat16, False, False, True)
+    buf = torch.full((shift + R * Cout + 8,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[shift: shift + R * Cout].view(R, Cout)
+    api.linear_q8(x, W, b, out=out)
+    torch.cuda.synchronize()
+    assert (buf[:shift] == 7).all() and (buf[shift + R * Cout:] == 7).all(), "outside the output"
+    _check_layer(x, W, b, None, False, out)
+
+
+def test_linear_q8_extremes_are_exact():
+    """The longest rows of the largest products: the sum is near 2^31 and exact."""
+    api = _api()
+    K = api.GL_MAX_Q8_K
+    q = torch.zeros((3, api.q8_row_bytes(K)), dtype=torch.int8, device="cuda")
+    w = torch.zeros((2, api.q8_row_bytes(K)), dtype=torch.int8, device="cuda")
+    q[:, :K], w[0, :K], w[1, :K] = -128, -128, 127
+    q[1, 5], q[2, :K] = 127, 1
+    one = torch.ones(3, device="cuda")
+    out = api.linear_q8(api.Q8Rows(q, one, K), api.Q8Rows(w, one[:2].clone(), K), dtype=torch.float32)
+    torch.cuda.synchronize()
+    ref = _f64(q[:, :K]) @ _f64(w[:, :K]).T
+    assert ref.max() == 16384 * K
+    assert (np.abs(_f64(out) - ref) <= E32 * np.abs(ref)).all()
+
+
+def test_offsets_past_32_bits():
+    api = _api()
+    g = np.random.default_rng(9)
+    # rows 2^31 elements apart
+    C, ld = 200, 2 ** 31 + 8
+    buf = torch.empty(2 * ld + C, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((3, C), (ld, 1))
+    x.copy_(_rows(g, 3, C, torch.bfloat16))
+    xc = x.contiguous()
+    _say("strided rows past 2^31")
+    y, mean, rstd = api.layer_norm(x, stats=True)
+    assert torch.equal(y, api.layer_norm(xc))
+    a, b = api.quantize_rows(x), api.quantize_rows(xc)
+    assert torch.equal(a.q, b.q)
+    r1 = api.layer_norm_backward(x, x, mean, rstd)
+    r2 = api.layer_norm_backward(xc, xc, mean, rstd)
+    assert all(torch.equal(s, t) for s, t in zip(r1, r2))
+    torch.cuda.synchronize()
+    del buf, x
+    # an output of more than 2^31 elements
+    R, K, Cout = 540000, 32, 4000
+    _say("output past 2^31")
+    x, W, b, _ = _layer(g, api, R, K, Cout, torch.bfloat16, False, False, True)
+    out = api.linear_q8(x, W, b)
+    torch.cuda.synchronize()
+    rows = torch.tensor([0, 1, 268435, 536870, 536871, 539998, R - 1])
+    _check_layer(x, W, b, None, False, out, rows=rows)
+    y = api.layer_norm(out)
+    torch.cuda.synchronize()
+    assert torch.equal(y[rows], api.layer_norm(out[rows].contiguous()))
+
+
+def test_leading_axes_and_empty_dimensions():
+    api = _api()
+    g = np.random.default_rng(1)
+    x = _rows(g, 24, 64, torch.bfloat16).reshape(2, 3, 4, 64)
+    y, mean, rstd = api.layer_norm(x, stats=True)
+    assert y.shape == x.shape and mean.shape == (2, 3, 4)
+    assert torch.equal(y.reshape(24, 64), api.layer_norm(x.reshape(24, 64)))
+    wide = _rows(g, 24, 128, torch.bfloat16).reshape(2, 12, 128)[:, :, 32:96]
+    assert torch.equal(api.layer_norm(wide), api.layer_norm(wide.contiguous()))
+    q = api.quantize_rows(wide)
+    assert q.q.shape == (2, 12, 64) and q.scale.shape == (2, 12)
+    W = api.quantize_rows(_rows(g, 10, 64, torch.bfloat16))
+    assert api.linear_q8(q, W).shape == (2, 12, 10)
+    torch.cuda.synchronize()
+
+
+def test_refusals():
+    api = _api()
+    x = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        api.layer_norm(x, v[:63])
+    with pytest.raises(ValueError):
+        api.layer_norm(x, v.float())
+    with pytest.raises(ValueError):
+        api.layer_norm(x.cpu())
+    with pytest.raises(ValueError):
+        api.layer_norm(x.t())
+    with pytest.raises(ValueError):
+        api.layer_norm(torch.zeros((4, 6, 64), dtype=torch.bfloat16, device="cuda")[:, ::2][:, :, :32][::3, 1:])
+    with pytest.raises(TypeError):
+        api.layer_norm(x.half())
+    with pytest.raises(api.GraphLeapError):
+        api.layer_norm(x, eps=-1.0)
+    with pytest.raises(api.GraphLeapError):
+        api.layer_norm(x, eps=float("nan"))
+    with pytest.raises(api.GraphLeapError):
+        api.layer_norm(x[:0])
+    with pytest.raises(api.GraphLeapError):
+        api.layer_norm(x, out=x)
+    m = torch.zeros(4, device="cuda")
+    with pytest.raises(ValueError):
+        api.layer_norm_backward(x[:3], x, m, m)
+    with pytest.raises(ValueError):
+        api.layer_norm_backward(x, x, m[:3], m)
+    with pytest.raises(api.GraphLeapError):
+        api.layer_norm_backward(x, x, m, m, need=(False, False, False))
+    with pytest.raises(api.GraphLeapError) as e:
+        api.layer_norm_backward(x, x, m, m, ws=api.Workspace(16, x.device))
+    assert e.value.status == 9
+    q = api.quantize_rows(x)
+    with pytest.raises(ValueError):
+        api.linear_q8(q, api.quantize_rows(x[:, :32]))
+    with pytest.raises(ValueError):
+        api.linear_q8(q, q, bias=v)
+    with pytest.raises(ValueError):
+        api.linear_q8(q, q, residual=x)
+    with pytest.raises(ValueError):
+        api.quantize_rows(x, out=api.quantize_rows(x[:, :32]))
+    with pytest.raises(TypeError):
+        api.linear_q8(q, q, dtype=torch.float16)
+
+
+def test_other_stream_and_graph_replay():
+    """The calls run where they are told to; recorded, they replay to the same bits."""
+    api = _api()
+    g = np.random.default_rng(4)
+    R, C, H = 777, 192, 768
+    x = _rows(g, R, C, torch.bfloat16)
+    dy = _rows(g, R, C, torch.bfloat16)
+    gamma, beta = _vec(g, C, torch.bfloat16, 1.0), _vec(g, C, torch.bfloat16)
+    W = api.quantize_rows(_rows(g, H, C, torch.bfloat16))
+    y, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
+
+    def step(stream=None):
+        n = api.layer_norm_q8(x, gamma, beta, stream=stream)
+        h = api.linear_q8(n, W, act_out=api.GL_ACT_GELU, stream=stream)
+        q = api.quantize_rows(h, stream=stream)
+        grads = api.layer_norm_backward(dy, x, mean, rstd, gamma, stream=stream)
+        return (n.q, n.scale, h, q.q, q.scale) + grads
+
+    want = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rec = step()
+    for i in range(4):
+        for t in rec:
+            t.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(rec, want)), i
+        assert all(torch.equal(a, b) for a, b in zip(step(), want)), i
+
+
+def test_gradient_against_differences():
+    """Differences of the forward pass in fp32, along random directions."""
+    api = _api()
+    g = np.random.default_rng(8)
+    R, C = 5, 96
+    x, dy = _rows(g, R, C, torch.float32), _rows(g, R, C, torch.float32)
+    gamma, beta = _vec(g, C, torch.float32, 1.0), _vec(g, C, torch.float32)
+    _, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
+    dx, dg, db = api.layer_norm_backward(dy, x, mean, rstd, gamma)
+
+    def loss(x, gamma, beta):
+        return float((api.layer_norm(x, gamma, beta).double() * dy.double()).sum())
+
+    for which, grad in enumerate((dx, dg, db)):
+        args = [x.contiguous(), gamma, beta]
+        v = torch.from_numpy(g.standard_normal(tuple(grad.shape))).float().cuda()
+        step = 2.0 ** -9
+        up, dn = list(args), list(args)
+        up[which], dn[which] = args[which] + step * v, args[which] - step * v
+        want = float((grad.double() * v.double()).sum())
+        # the step's own rounding, fp32 of the outputs, and the third derivative
+        near = float(dy.abs().double().sum())
+        assert abs((loss(*up) - loss(*dn)) / (2 * step) - want) <= near * (16 * E32 / step + 4 * step ** 2), which

@@ -1,0 +1,111 @@
+"""Argument checks of layer norm and the 8-bit layers at the C ABI, on the host
+(fake, never-dereferenced addresses stand in for device pointers)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2604_21290_amd import api
+
+pytestmark = [pytest.mark.skipif(not os.path.exists(api.LIB_PATH), reason="libgraphleap.so not built"),
+              pytest.mark.skipif(torch.cuda.device_count() > 0, reason="host-only checks (fake pointers)")]
+
+A = 1 << 24
+P = lambda i, off=0: ctypes.c_void_p(A * (i + 1) + off)  # noqa: E731
+
+
+def _st(s):
+    return api.STATUS[s]
+
+
+def _norm(x=P(0), R=64, C=100, ld=100, gamma=P(1), beta=P(2), eps=1e-5, dt=1, out=P(3), mean=None, rstd=None):
+    return _st(api.lib().gl_layer_norm(x, R, C, ld, gamma, beta, eps, dt, out, mean, rstd, None))
+
+
+def test_layer_norm_refusals():
+    assert _norm(x=None) == _norm(out=None) == "GL_ERR_NULL_PTR"
+    assert _norm(dt=2) == "GL_ERR_UNSUPPORTED"
+    for bad in (dict(R=0), dict(C=0), dict(R=-1), dict(ld=99), dict(ld=-100), dict(ld=1 << 40), dict(eps=-1e-9),
+                dict(eps=float("nan")), dict(eps=float("inf")), dict(R=1 << 30, C=1 << 20, ld=1 << 20)):
+        assert _norm(**bad) == "GL_ERR_BAD_SHAPE", bad
+    assert _norm(x=P(0, 1)) == _norm(out=P(3, 1)) == _norm(gamma=P(1, 1)) == "GL_ERR_ALIGNMENT"
+    assert _norm(x=P(0, 2), dt=0) == _norm(mean=P(5, 2)) == "GL_ERR_ALIGNMENT"
+    assert _norm(out=P(0, 64)) == "GL_ERR_ALIAS"
+    assert _norm(mean=P(4), rstd=P(4, 64)) == "GL_ERR_ALIAS"
+    assert _norm(mean=P(0, 128)) == _norm(out=P(1, 64)) == "GL_ERR_ALIAS"
+    # a strided x reaches to the end of its last row
+    assert _norm(ld=1000, out=P(0, 63 * 2000 + 198)) == "GL_ERR_ALIAS"
+    assert "layer_norm" in api.lib().gl_last_error().decode()
+
+
+def _grad(dy=P(0), lddy=100, x=P(1), ldx=100, R=64, C=100, mean=P(2), rstd=P(3), gamma=P(4), dt=1, dx=P(5),
+          dg=P(6), db=P(7), ws=P(8), n=1 << 23):
+    return _st(api.lib().gl_layer_norm_backward(dy, lddy, x, ldx, R, C, mean, rstd, gamma, dt, dx, dg, db, ws, n,
+                                                None))
+
+
+def test_layer_norm_backward_refusals():
+    for bad in (dict(dy=None), dict(x=None), dict(mean=None), dict(rstd=None), dict(dx=None, dg=None, db=None)):
+        assert _grad(**bad) == "GL_ERR_NULL_PTR", bad
+    assert _grad(dt=3) == "GL_ERR_UNSUPPORTED"
+    for bad in (dict(R=0), dict(C=0), dict(ldx=99), dict(lddy=99)):
+        assert _grad(**bad) == "GL_ERR_BAD_SHAPE", bad
+    for bad in (dict(dy=P(0, 1)), dict(mean=P(2, 2)), dict(dg=P(6, 2)), dict(dx=P(5, 1))):
+        assert _grad(**bad) == "GL_ERR_ALIGNMENT", bad
+    for bad in (dict(dx=P(0, 16)), dict(dx=P(1, 16)), dict(dg=P(5, 64)), dict(db=P(6, 64)), dict(dg=P(2, 64)),
+                dict(ws=P(1, 64)), dict(ws=P(6, 64))):
+        assert _grad(**bad) == "GL_ERR_ALIAS", bad
+    need = api.lib().gl_layer_norm_backward_workspace_bytes(64, 100, 1)
+    assert need >= 800
+    assert _grad(ws=None) == _grad(n=need - 1) == _grad(ws=P(8, 8)) == "GL_ERR_WORKSPACE"
+    assert api.lib().gl_layer_norm_backward_workspace_bytes(0, 100, 1) == 0
+    assert api.lib().gl_layer_norm_backward_workspace_bytes(64, 100, 5) == 0
+
+
+def _q8(x=P(0), R=64, K=100, ld=100, dt=1, q=P(1), s=P(2)):
+    return _st(api.lib().gl_quantize_rows(x, R, K, ld, dt, q, s, None))
+
+
+def _nq8(x=P(0), R=64, K=100, ld=100, gamma=None, beta=None, eps=1e-5, dt=1, q=P(1), s=P(2)):
+    return _st(api.lib().gl_layer_norm_q8(x, R, K, ld, gamma, beta, eps, dt, q, s, None))
+
+
+@pytest.mark.parametrize("call", [_q8, _nq8])
+def test_rows_to_8_bits_refusals(call):
+    assert call(x=None) == call(q=None) == call(s=None) == "GL_ERR_NULL_PTR"
+    assert call(dt=-1) == "GL_ERR_UNSUPPORTED"
+    for bad in (dict(R=0), dict(K=0), dict(K=131072, ld=131072), dict(ld=5)):
+        assert call(**bad) == "GL_ERR_BAD_SHAPE", bad
+    assert call(q=P(1, 8)) == call(s=P(2, 2)) == call(x=P(0, 1)) == "GL_ERR_ALIGNMENT"
+    assert call(q=P(0, 16)) == call(s=P(1, 64 * 112 - 4)) == "GL_ERR_ALIAS"
+
+
+def test_layer_norm_q8_eps():
+    assert _nq8(eps=-1.0) == "GL_ERR_BAD_SHAPE"
+
+
+def test_q8_row_bytes():
+    f = api.lib().gl_q8_row_bytes
+    assert [f(k) for k in (1, 16, 17, 80, 131071)] == [16, 16, 32, 80, 131072]
+    assert [f(k) for k in (0, -5, 131072)] == [0, 0, 0]
+    with pytest.raises(api.GraphLeapError):
+        api.q8_row_bytes(0)
+
+
+def _lin(q=P(0), s=P(1), R=64, K=100, W=P(2), ws=P(3), bias=P(4), Cout=50, act=0, res=None, dt=1, out=P(5)):
+    return _st(api.lib().gl_linear_q8(q, s, R, K, W, ws, bias, Cout, act, res, dt, out, None))
+
+
+def test_linear_q8_refusals():
+    for bad in (dict(q=None), dict(s=None), dict(W=None), dict(ws=None), dict(out=None)):
+        assert _lin(**bad) == "GL_ERR_NULL_PTR", bad
+    assert _lin(dt=4) == _lin(act=2) == "GL_ERR_UNSUPPORTED"
+    for bad in (dict(R=0), dict(Cout=0), dict(K=0), dict(K=131072), dict(R=1 << 30, Cout=1 << 20)):
+        assert _lin(**bad) == "GL_ERR_BAD_SHAPE", bad
+    for bad in (dict(q=P(0, 8)), dict(W=P(2, 4)), dict(s=P(1, 2)), dict(ws=P(3, 1)), dict(out=P(5, 1)),
+                dict(bias=P(4, 1)), dict(res=P(6, 1)), dict(dt=0, out=P(5, 2))):
+        assert _lin(**bad) == "GL_ERR_ALIGNMENT", bad
+    for bad in (dict(out=P(0, 16)), dict(out=P(1, 16)), dict(out=P(2, 16)), dict(out=P(3, 16)), dict(out=P(4, 16)),
+                dict(res=P(5, 16))):
+        assert _lin(**bad) == "GL_ERR_ALIAS", bad

@@ -1,13 +1,12 @@
 // Fully connected layers on 8-bit rows:
 //   out[r, o] = act_out( (sum_k A[r, k] W[o, k]) sa[r] sw[o] + bias[o] ) + residual[r, o]
 // The sums are exact (int32, at most 131071 terms); then fp32 and one rounding.
-//   - Staging as in the bf16 GEMM: 16 bytes a lane straight into LDS, a row's
-//     16-byte slots permuted by its number, two buffers and one barrier a stage.
-//   - MFMA 16x16x64: a lane's 16 bytes of a row are one operand, so the slots that
-//     serve eight bf16 values serve sixteen of these.  Operands are swapped (W rows
-//     first): a lane ends with four consecutive output columns of one row.
-//   - Epilogue: the tile passes through LDS wave by wave, so that stores and
-//     residual loads cover whole rows.
+//   - Staging: 16 bytes a lane straight into LDS, a row's 16-byte slots permuted by
+//     its number so that the rows an operand read touches lie in all banks.
+//   - MFMA 16x16x64: a lane's 16 bytes of a row are one operand.  Operands are
+//     swapped (W rows first): a lane ends with consecutive output columns of one row.
+#include <type_traits>
+
 #include "gl_device.h"
 #include "gl_kernels.h"
 
@@ -60,161 +59,289 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
   else static_cast<float*>(p)[i] = f;
 }
 
-// BM x BN output tile, STEP bytes of K per row and stage, WR x WC waves.
-template <int BM_, int BN_, int STEP_, int WR_, int WC_>
-struct Q8Cfg {
-  static constexpr int BM = BM_, BN = BN_, STEP = STEP_, WR = WR_, WC = WC_;
+// ---------------------------------------------------------------------------
+// Large products: a pipeline that does not drain, neither between stages nor
+// between tiles.
+//   - A workgroup takes one tile after another, and its stages (128 bytes of K of
+//     each row) follow each other across tiles: the first two of the next tile are
+//     under way before the last of this one is multiplied.
+//   - Operands are double-buffered in registers: while one half stage (64 bytes of
+//     K) is multiplied, the next one's are read, a few between every few MFMAs.
+//   - The barrier of a stage stands before its last half is multiplied, when that
+//     half's operands are in registers: what follows it, the next stage's first
+//     reads and the loads into the buffer that is now free, runs under MFMAs.
+//   - MFMA tile j of a wave takes W's rows in an order that leaves a lane with eight
+//     consecutive columns of a row in tiles 2p and 2p + 1: results go from the
+//     accumulators to memory 16 bytes (bf16) a lane, 64 a row, with no trip
+//     through LDS.
+// Tiles are walked so that the 32 that an XCD works on at a time are 8 x 4.
+// ---------------------------------------------------------------------------
+template <int BM_, int BN_, int WR_, int WC_, int NBUF_>
+struct PipeCfg {
+  static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, NBUF = NBUF_, STEP = 128;
   static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
-  static constexpr int kStage = (BM + BN) * STEP;        // bytes of one stage buffer
-  static constexpr int kLoads = kStage / 16 / kThreads;  // loads per lane and stage
+  static constexpr int kStage = (BM + BN) * STEP;
+  static constexpr int kRPL = 1024 / STEP;  // rows of a wave's load
+  static constexpr int kLoadsA = BM / kRPL / kWaves, kLoadsW = BN / kRPL / kWaves;  // per wave and stage
   static constexpr int TM = BM / WR / 16, TN = BN / WC / 16;
-  static constexpr size_t kSmem = (size_t)2 * kStage;
-  static_assert((size_t)BM * BN * 4 <= kSmem, "epilogue tile exceeds the stage buffers");
-  static_assert(kStage % (1024 * kWaves) == 0 && (STEP == 128 || STEP == 256), "whole loads per wave");
+  static constexpr int kVec = BM + 2 * BN;  // a tile's scales and bias
+  static constexpr size_t kSmem = (size_t)NBUF * kStage + 2 * kVec * 4;
+  static constexpr int kPerCU = (int)(160 * 1024 / kSmem) * kWaves <= 16 ? (int)(160 * 1024 / kSmem) : 16 / kWaves;
+  static_assert(BM % (kRPL * kWaves) == 0 && BN % (kRPL * kWaves) == 0, "whole loads per wave");
+  static_assert(TN % 2 == 0, "pairs of column tiles");
+  static_assert(BM <= kThreads && BN <= kThreads, "a thread loads one of each vector");
 };
 
-template <class G, int DT, int ACT_OUT, bool RES>
-__global__ __launch_bounds__(G::kThreads) void gemm_q8_kernel(GemmQ8Args a) {
+// 16 bytes a lane from base + off to LDS (lds_dma16 with a uniform base)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_dma16_base(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// v, which the compiler takes for a value of its own each time: what is computed from
+// it is not kept in registers across the loop over K.
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// All but this wave's N newest loads have landed and its LDS reads are done; then the
+// workgroup's barrier.
+template <int N>
+__device__ __forceinline__ void dma_wait_barrier_but() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <class G, int DT, int ACT_OUT>
+__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(G::kWaves * G::kPerCU / 4, G::kWaves * G::kPerCU / 4)))
+void gemm_q8_pipe_kernel(GemmQ8Args a) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int BM = G::BM, BN = G::BN, STEP = G::STEP, TM = G::TM, TN = G::TN, NL = G::kLoads;
-  constexpr int SPR = STEP / 16, RPL = 64 / SPR;  // slots per row, rows per wave load
+  constexpr int BM = G::BM, BN = G::BN, STEP = G::STEP, TM = G::TM, TN = G::TN, NA = G::kLoadsA, NB = G::kLoadsW;
+  constexpr int NL = NA + NB, NBUF = G::NBUF;
+  constexpr int WROWS = 16 * TM, WCOLS = 16 * TN;
   const int R = a.R, Cout = a.Cout, rowb = a.Kp;
   const int nstages = (rowb + STEP - 1) / STEP;
-  const int ntn = (Cout + BN - 1) / BN;
-  const int blk = xcd_remap(blockIdx.x, gridDim.x);
-  const int mt = blk / ntn, nt = blk - mt * ntn;
-  const int m0 = mt * BM, n0 = nt * BN;
+  const int ntm = (R + BM - 1) / BM, ntn = (Cout + BN - 1) / BN, ntiles = ntm * ntn;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, t = lane & 15;
   const int wm = w / G::WC, wn = w % G::WC;
 
-  // staging: rows past R or Cout repeat the last one; slots past Kp read zeros
-  const uint32_t lds0 = lds_offset(smem);
-  const char* src[NL];
-  int slot[NL];
+  // place of tile number L of the dispatch order: groups of 8 rows of tiles, walked
+  // column by column, a stretch of them for each XCD
+  auto place = [&](int L, int& m0, int& n0) {
+    const int blk = xcd_remap(L, ntiles);
+    const int grp = blk / (8 * ntn), in = blk - grp * 8 * ntn, high = min(8, ntm - grp * 8);
+    const int nt = in / high;
+    m0 = (grp * 8 + in - nt * high) * BM;
+    n0 = nt * BN;
+  };
+
+  // staging: load i of wave w fills rows 8 (w + waves i) .. of the stage; lane l's
+  // 16 bytes land at place l % 8 of row l / 8 and hold slot place ^ key, where a row
+  // of A has key row % 8 and one of W, whose rows are read in fours of every other
+  // eight, row % 4 + 4 (row / 8 % 2).  Rows past R or Cout repeat the last one.
+  const uint32_t lds0 = lds_offset(smem) + w * 1024;
+  constexpr int RPL = G::kRPL;
+  const int lr = lane >> 3;
+  const int slot_a = ((lane & 7) ^ lr) * 16;
+  const int slot_w = ((lane & 7) ^ ((lr & 3) | ((w & 1) << 2))) * 16;
+  const int lim_a = rowb - 16 - slot_a, lim_w = rowb - 16 - slot_w;  // the row's last slot
+  const char *base_a, *base_w;     // of the tile that is being loaded
+  uint32_t src_a[NA], src_w[NB];   // at most 256 rows of 2^17 bytes
+  int L_load = blockIdx.x, s_load = 0;
+  auto aim = [&]() {
+    int m0, n0;
+    place(L_load, m0, n0);
+    base_a = reinterpret_cast<const char*>(a.A) + (size_t)m0 * rowb;
+    base_w = reinterpret_cast<const char*>(a.W) + (size_t)n0 * rowb;
+    const int r = fresh(RPL * w + lr);
 #pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int r = RPL * (w + G::kWaves * i) + lane / SPR;
-    slot[i] = ((lane % SPR) ^ (r & (SPR - 1))) * 16;
-    src[i] = (r < BM ? reinterpret_cast<const char*>(a.A) + (size_t)min(m0 + r, R - 1) * rowb
-                     : reinterpret_cast<const char*>(a.W) + (size_t)min(n0 + r - BM, Cout - 1) * rowb) +
-             slot[i];
-  }
-  auto stage = [&](int s) {
-    const int off = s * STEP;
-    const uint32_t d = lds0 + (s & 1) * G::kStage + w * 1024;
+    for (int i = 0; i < NA; ++i) src_a[i] = (uint32_t)min(r + RPL * G::kWaves * i, R - 1 - m0) * rowb + slot_a;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const char* p = src[i] + off;
-      if (off + STEP > rowb)  // uniform: the last, partial stage
-        p = off + slot[i] < rowb ? p : reinterpret_cast<const char*>(kZero16);
-      lds_dma16(p, d + G::kWaves * i * 1024);
+    for (int i = 0; i < NB; ++i) src_w[i] = (uint32_t)min(r + RPL * G::kWaves * i, Cout - 1 - n0) * rowb + slot_w;
+  };
+  // past the end of a row, W reads zeros, and A its last slot again
+  auto load = [&](int i, int buf) {
+    const int off = s_load * STEP;
+    const uint32_t d = lds0 + buf * G::kStage + i * G::kWaves * 1024;
+    if (i < NA) {
+      lds_dma16_base(base_a, src_a[i < NA ? i : 0] + min(off, lim_a), d);
+    } else {
+      const char* p = base_w + (src_w[i < NA ? 0 : i - NA] + off);
+      lds_dma16(off <= lim_w ? p : reinterpret_cast<const char*>(kZero16), d);
     }
   };
-  stage(0);
-
-  constexpr int WROWS = 16 * TM, WCOLS = 16 * TN;
-  constexpr int LPR = WCOLS / 8, RPP = 64 / LPR, NP = WROWS / RPP;  // lanes per row, rows per pass
-  constexpr int CSW = WCOLS / 4 < 16 ? WCOLS / 4 - 1 : 15;
-  const int cq = lane % LPR, rq = lane / LPR;
-  const int n = n0 + wn * WCOLS + cq * 8;
-  const int row0 = m0 + wm * WROWS + rq;
-  const bool vec = n + 8 <= Cout;
-  float bn[8], sw[8];
-#pragma unroll
-  for (int v = 0; v < 8; ++v) {
-    const int c = min(n + v, Cout - 1);
-    bn[v] = a.bias ? load1<DT>(a.bias, c) : 0.f;
-    sw[v] = a.sw[c];
-  }
-
-  i32x4 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-  for (int s = 0; s < nstages; ++s) {
-    // stage s has landed, and every wave is done reading stage s - 1's buffer
-    dma_wait_barrier();
-    if (s + 1 < nstages) stage(s + 1);
-    const char* sa = smem + (s & 1) * G::kStage + (wm * WROWS + t) * STEP;
-    const char* sb = smem + (s & 1) * G::kStage + (BM + wn * WCOLS + t) * STEP;
-#pragma unroll
-    for (int kk = 0; kk < STEP / 64; ++kk) {
-      uint4 af[TM], bf[TN];
-      const int co = ((kk * 4 + g) ^ (t & (SPR - 1))) * 16;
-#pragma unroll
-      for (int i = 0; i < TM; ++i) af[i] = *reinterpret_cast<const uint4*>(sa + i * 16 * STEP + co);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) bf[j] = *reinterpret_cast<const uint4*>(sb + j * 16 * STEP + co);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mfma_i8(bf[j], af[i], acc[i][j]);
-    }
-  }
-
-  // lane (g, t) of MFMA tile (i, j) holds columns 4g .. 4g+3 of row t
-  __syncthreads();
-  char* st = smem + w * (WROWS * WCOLS * 4);
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-      *reinterpret_cast<i32x4*>(st + (i * 16 + t) * (WCOLS * 4) + (((j * 4 + g) ^ (t & CSW)) * 16)) =
-          acc[i][j];
-  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    const int r = p * RPP + rq, row = row0 + p * RPP;
-    const char* sr = st + r * (WCOLS * 4);
-    const i32x4 x0 = *reinterpret_cast<const i32x4*>(sr + ((2 * cq) ^ (r & CSW)) * 16);
-    const i32x4 x1 = *reinterpret_cast<const i32x4*>(sr + ((2 * cq + 1) ^ (r & CSW)) * 16);
-    if (row >= R || n >= Cout) continue;
-    const float sar = a.sa[row];
-    float y[8];
-#pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      y[v] = fmaf((float)(v < 4 ? x0[v & 3] : x1[v & 3]), sar * sw[v], bn[v]);
-      if (ACT_OUT) y[v] = gelu_f32(y[v]);
-    }
-    const size_t o = (size_t)row * Cout + n;
-    if (vec) {
-      if (RES) {
-        float f[8];
-        load8<DT>(a.residual, o, f);
-#pragma unroll
-        for (int v = 0; v < 8; ++v) y[v] += f[v];
-      }
-      store8<DT>(a.out, o, y);
+  // after the last stage of the last tile the same stage is loaded again, and not read
+  auto next_load = [&]() {
+    if (++s_load < nstages) return;
+    if (L_load + (int)gridDim.x < ntiles) {
+      L_load += gridDim.x;
+      s_load = 0;
+      aim();
     } else {
+      s_load = nstages - 1;
+    }
+  };
+
+  // operands of half stage kk
+  uint4 fa[2][TM], fb[2][TN];
+  // (the second half of a stage's row is 64 bytes off: the slot's permutation is an
+  // exclusive or)
+  const int rd_a = (wm * WROWS + t) * STEP + (g ^ (t & 7)) * 16;
+  const int rd_b = (BM + wn * WCOLS + (t >> 2) * 8 + (t & 3)) * STEP + (g ^ (t & 7)) * 16;
+  auto read = [&](int set, int pa, int pb, int i) {  // TM of A, then TN of W
+    if (i < TM)
+      fa[set][i < TM ? i : 0] = *reinterpret_cast<const uint4*>(
+          smem + pa + i * 16 * STEP);
+    else
+      fb[set][i < TM ? 0 : i - TM] = *reinterpret_cast<const uint4*>(
+          smem + pb + (((i - TM) >> 1) * 32 + ((i - TM) & 1) * 4) * STEP);
+  };
+  i32x4 acc[TM][TN];
+  // multiply half kk (its operands are in set kk) while the next half's are read from
+  // `buf` and, in the second half, a stage is loaded into the buffer `lbuf`
+  constexpr int kSpread = TM > 2 ? TM / 2 : TM;  // row tiles that the loads are spread over
+  auto half = [&](auto KK, int buf, int lbuf) {
+    constexpr int kk = decltype(KK)::value;
+    constexpr int kPer = (TM + TN + TM - 2) / (TM - 1), kLPer = (NL + kSpread - 1) / kSpread;
+    const int pa = buf * G::kStage + (fresh(rd_a) ^ ((kk ^ 1) * 64));
+    const int pb = buf * G::kStage + (fresh(rd_b) ^ ((kk ^ 1) * 64));
 #pragma unroll
-      for (int v = 0; v < 8; ++v)
-        if (n + v < Cout) {
-          if (RES) y[v] += load1<DT>(a.residual, o + v);
-          store1<DT>(a.out, o + v, y[v]);
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma_i8(fb[kk][j], fa[kk][i], acc[i][j]);
+      if (kk == 1) {
+#pragma unroll
+        for (int l = i * kLPer; l < (i + 1) * kLPer && l < NL; ++l) load(l, lbuf);
+      }
+      // W's first: each of them is needed with every row tile
+#pragma unroll
+      for (int l = i * kPer; l < (i + 1) * kPer && l < TM + TN; ++l) read(kk ^ 1, pa, pb, l < TN ? TM + l : l - TN);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  aim();
+#pragma unroll
+  for (int b = 0; b < NBUF; ++b) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load(i, b);
+    next_load();
+  }
+  dma_wait_barrier_but<(NBUF - 1) * NL>();
+#pragma unroll
+  for (int i = 0; i < TM + TN; ++i) read(0, rd_a, rd_b, i);
+
+  float* const vec0 = reinterpret_cast<float*>(smem + NBUF * G::kStage);
+  int buf = 0, turn = 0;
+  for (int L = blockIdx.x; L < ntiles; L += gridDim.x, turn ^= 1) {
+    int m0, n0;
+    place(L, m0, n0);
+    // the tile's vectors: loaded now, put into LDS before the first barrier
+    float* const vec = vec0 + turn * G::kVec;
+    float v_sa, v_sw, v_b;
+    auto fetch = [&]() {
+      const int i = fresh(tid);
+      v_sa = i < BM ? a.sa[min(m0 + i, R - 1)] : 0.f;
+      v_sw = i < BN ? a.sw[min(n0 + i, Cout - 1)] : 0.f;
+      v_b = i < BN && a.bias ? load1<DT>(a.bias, min(n0 + i, Cout - 1)) : 0.f;
+    };
+    // (tiles whose accumulators leave no room for them load them then)
+    constexpr bool kLate = TM * TN >= 32;
+    if (!kLate) fetch();
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    using std::integral_constant;
+    auto fill = [&]() {
+      if (kLate) fetch();
+      const int i = fresh(tid);
+      if (i < BM) vec[i] = v_sa;
+      if (i < BN) vec[BM + i] = v_sw, vec[BM + BN + i] = v_b;
+    };
+    for (int s = 0; s < nstages; ++s) {
+      half(integral_constant<int, 0>(), buf, 0);
+      if (s == 0) fill();
+      // this wave has read all of the stage, and the next one has landed: for all waves
+      dma_wait_barrier_but<(NBUF - 2) * NL>();
+      const int free = buf;
+      buf = buf + 1 == NBUF ? 0 : buf + 1;
+      half(integral_constant<int, 1>(), buf, free);
+      next_load();
+    }
+
+    // lane (g, t) of MFMA tiles (i, 2p) and (i, 2p + 1): eight columns of row t.  Row
+    // tiles outermost: the two halves of a 128-byte line are stored together.
+    const int lane_e = fresh(lane), te = lane_e & 15, ge = lane_e >> 4;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int r = wm * WROWS + i * 16 + te, row = m0 + r;
+      const float sar = vec[r];
+#pragma unroll
+      for (int p = 0; p < TN / 2; ++p) {
+        const int c = wn * WCOLS + p * 32 + ge * 8, n = n0 + c;
+        float y[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          y[v] = fmaf((float)acc[i][2 * p + (v >> 2)][v & 3], sar * vec[BM + c + v], vec[BM + BN + c + v]);
+          if (ACT_OUT) y[v] = gelu_f32(y[v]);
         }
+        if (row >= R || n >= Cout) continue;
+        const size_t o = (size_t)row * Cout + n;
+        if (n + 8 <= Cout) {
+          if (a.residual) {
+            float f[8];
+            load8<DT>(a.residual, o, f);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) y[v] += f[v];
+          }
+          store8<DT>(a.out, o, y);
+        } else {
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            if (n + v < Cout) {
+              if (a.residual) y[v] += load1<DT>(a.residual, o + v);
+              store1<DT>(a.out, o + v, y[v]);
+            }
+        }
+      }
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives its workgroup
 }
 
 template <class G, int DT>
-hipError_t launch_cfg_q8(const GemmQ8Args& a, hipStream_t stream) {
-  const void* fn = a.act_out ? (a.residual ? (const void*)&gemm_q8_kernel<G, DT, 1, true>
-                                           : (const void*)&gemm_q8_kernel<G, DT, 1, false>)
-                             : (a.residual ? (const void*)&gemm_q8_kernel<G, DT, 0, true>
-                                           : (const void*)&gemm_q8_kernel<G, DT, 0, false>);
-  const dim3 grid((unsigned)(((long)(a.R + G::BM - 1) / G::BM) * ((a.Cout + G::BN - 1) / G::BN)));
+hipError_t launch_pipe_q8(const GemmQ8Args& a, hipStream_t stream) {
+  const void* fn = a.act_out ? (const void*)&gemm_q8_pipe_kernel<G, DT, 1> : (const void*)&gemm_q8_pipe_kernel<G, DT, 0>;
+  const long tiles = ((long)(a.R + G::BM - 1) / G::BM) * ((a.Cout + G::BN - 1) / G::BN);
+  const dim3 grid((unsigned)std::min(tiles, 256L * G::kPerCU));
   return launch_with_smem(fn, grid, dim3(G::kThreads), G::kSmem, stream, nullptr, nullptr, a);
 }
 
+// The tile whose last round ends first.  A round of 128 x 128 tiles, two to a CU, is
+// taken for 2.5 units, of 256 x 256, one to a CU, for 4, and of 64 x 64, two to a CU,
+// for 1 (half of each where one to a CU suffices): what each took of a product of
+// 8192 x 8192 x 8192 (527, 420 and 874 us).  Measured, us:
+//                    256 x 256   128 x 128   64 x 64
+//   16384x4096x4096    237 *        284         447
+//   12544x640x2560      28.4 *       30.6        51
+//   12544x2560x640      32.7         25.4 *      38
+//   2048x2048x2048      25.0         14.5 *      17.3
+//   1000x8000x1000      77.5         45.6        19.8 *
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
-  auto tiles = [&](int bm, int bn) { return (long)((a.R + bm - 1) / bm) * ((a.Cout + bn - 1) / bn); };
-  if (tiles(128, 128) >= 384) return launch_cfg_q8<Q8Cfg<128, 128, 128, 4, 2>, DT>(a, stream);
-  if (tiles(64, 64) >= 128) return launch_cfg_q8<Q8Cfg<64, 64, 128, 2, 2>, DT>(a, stream);
-  return launch_cfg_q8<Q8Cfg<32, 64, 256, 1, 4>, DT>(a, stream);
+  auto rounds = [&](int bm, int bn, int per_cu) {
+    const long t = ((long)(a.R + bm - 1) / bm) * ((a.Cout + bn - 1) / bn), slots = 256 * per_cu;
+    return t <= 256 ? 1.0 / per_cu : (double)((t + slots - 1) / slots);
+  };
+  const double c256 = 4 * rounds(256, 256, 1), c128 = 2.5 * rounds(128, 128, 2), c64 = rounds(64, 64, 2);
+  if (c256 <= c128 && c256 <= c64) return launch_pipe_q8<PipeCfg<256, 256, 2, 4, 2>, DT>(a, stream);
+  if (c128 <= c64) return launch_pipe_q8<PipeCfg<128, 128, 2, 4, 2>, DT>(a, stream);
+  return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 4>, DT>(a, stream);
 }
 
 hipError_t launch_gemm_q8(const GemmQ8Args& a, int dt_bf16, hipStream_t stream) {

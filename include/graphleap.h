@@ -467,9 +467,9 @@ gl_status gl_layer_norm(const void* x, int R, int C, long long ldx, const void* 
  *   pass; gamma [C] (dt) or NULL for ones.
  *   dx [R, C] (dt), contiguous; dgamma, dbeta [C] fp32.  Any of the three may
  *   be NULL (not all): it is then not computed.
- *   workspace: gl_layer_norm_backward_workspace_bytes(R, C, dt) bytes, 16-byte
- *   aligned, disjoint from every other argument; not needed (NULL) when dgamma
- *   and dbeta are NULL.
+ *   workspace: gl_layer_norm_backward_workspace_bytes(R, C, dt) bytes (0 for few
+ *   rows: NULL will do), 16-byte aligned, disjoint from every other argument; not
+ *   needed (NULL) when dgamma and dbeta are NULL.
  * Outputs must not overlap inputs or each other.  Limits and errors as
  * gl_layer_norm, and GL_ERR_WORKSPACE.
  * -------------------------------------------------------------------------*/

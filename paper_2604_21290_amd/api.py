@@ -401,8 +401,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     if need[1] or need[2]:
         if ws is None:
             wn = lib().gl_layer_norm_backward_workspace_bytes(R, C, _dt(x))
-            buf = _new((wn,), torch.uint8, x, stream)
-            wp = buf.data_ptr()
+            if wn:
+                buf = _new((wn,), torch.uint8, x, stream)
+                wp = buf.data_ptr()
         else:
             wp, wn = ws.ptr, ws.nbytes
             if stream is not None:

@@ -4,6 +4,14 @@
 // One kernel: a row is read once and stays in registers, in fp32, while its
 // statistics are taken (the mean first, then the squares of what is left, which
 // loses nothing to cancellation) and its top is found; then it is written once.
+// Memory bounds it: us (and TB/s of what it has to read and write; a copy of 1 GiB
+// reaches 5.3) in bf16, norm, 8 bits, norm to 8 bits:
+//   32768 x 2560   69.8 (4.8)   49.7 (5.1)   77.2 (3.3)
+//   100352 x 320   35.1 (3.7)   19.7 (4.9)   32.9 (2.9)
+//   100352 x 80    10.1 (3.2)    8.1 (3.0)   11.8 (2.1)
+//   6272 x 192      4.1 (1.2)    3.2 (1.1)    4.4 (0.8)
+// Small inputs take a launch and one trip to memory, about 3 us; the norm to 8 bits
+// has twice the arithmetic of the norm, which then shows.
 #include "gl_kernels.h"
 #include "row_device.h"
 
@@ -11,83 +19,113 @@ namespace gl {
 
 enum { kNorm = 0, kNormQ8 = 1, kQ8 = 2 };
 
-// LPR lanes hold a row, VPL chunks each.
+// LPR lanes hold a row, VPL chunks each.  A workgroup takes many rows: gamma and beta
+// stay in registers, and a row's loads are under way while the one before is worked on.
 template <int DT, int MODE, int LPR, int VPL>
-__global__ __launch_bounds__(LPR > 256 ? LPR : 256) void row_kernel(RowArgs a) {
+__global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   using T = Chunk<DT>;
-  constexpr int E = T::E;
-  __shared__ uint32_t slots[3][LPR > 64 ? LPR / 64 : 1];
-  const int lane = threadIdx.x & (LPR - 1);
-  const long long g = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / LPR;
-  const bool mine = g < a.R;
-  const size_t row = mine ? g : a.R - 1;
+  constexpr int E = T::E, GROUPS = 256 / LPR;
+  __shared__ uint32_t slots[2][3][4];
+  const int lane = threadIdx.x & (LPR - 1), grp = threadIdx.x / LPR;
   const int C = a.C, n = (C + E - 1) / E;
-  const char* x = static_cast<const char*>(a.x) + row * a.ldx * T::kSize;
+  const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
-  float f[VPL][E];
+  uint4 raw[VPL];
+  auto load = [&](long long r) {
+    const char* x = static_cast<const char*>(a.x) + min(r, (long long)a.R - 1) * a.ldx * T::kSize;
 #pragma unroll
-  for (int v = 0; v < VPL; ++v) {
-    const int c = lane + v * LPR;
-    if (c < n) T::load(x, min(c * E, C - E), f[v]);
-  }
+    for (int v = 0; v < VPL; ++v) {
+      const int c = lane + v * LPR;
+      if (c < n) raw[v] = T::raw(x, min(c * E, C - E));
+    }
+  };
+  const long long step = (long long)gridDim.x * GROUPS;
+  long long r0 = (long long)blockIdx.x * GROUPS;
+  load(r0 + grp);
+  uint4 gamma[VPL], beta[VPL];
   if (MODE != kQ8) {
-    float s = 0.f;
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR, skip = max(c * E + E - C, 0);
-      if (c < n)
-#pragma unroll
-        for (int j = 0; j < E; ++j) s += j >= skip ? f[v][j] : 0.f;
-    }
-    const float mean = sum_row<LPR>(s, slots[0]) * a.inv_c;
-    s = 0.f;
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR, skip = max(c * E + E - C, 0);
-      if (c < n)
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          f[v][j] -= mean;
-          s = fmaf(j >= skip ? f[v][j] : 0.f, f[v][j], s);
-        }
-    }
-    const float rstd = __builtin_amdgcn_rsqf(fmaf(sum_row<LPR>(s, slots[1]), a.inv_c, a.eps));
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       const int c = lane + v * LPR, i = min(c * E, C - E);
       if (c < n) {
-        float w[E], b[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j) w[j] = 1.f, b[j] = 0.f;
-        if (a.gamma) T::load(a.gamma, i, w);
-        if (a.beta) T::load(a.beta, i, b);
-#pragma unroll
-        for (int j = 0; j < E; ++j) f[v][j] = fmaf(f[v][j] * rstd, w[j], b[j]);
-        if (MODE == kNorm && mine) T::store(a.out, row * C + i, f[v]);
+        if (a.gamma) gamma[v] = T::raw(a.gamma, i);
+        if (a.beta) beta[v] = T::raw(a.beta, i);
       }
-    }
-    if (MODE == kNorm && mine && lane == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
     }
   }
-  if (MODE != kNorm) {
-    uint32_t top = 0;
+  int turn = 0;
+  // every group of a workgroup makes the same number of turns
+  for (; r0 < a.R; r0 += step, turn ^= 1) {
+    const bool mine = r0 + grp < a.R;
+    const size_t row = r0 + grp;
+    float f[VPL][E];
 #pragma unroll
     for (int v = 0; v < VPL; ++v)
-      if (lane + v * LPR < n)
+      if (lane + v * LPR < n) T::unpack(raw[v], f[v]);
+    if (r0 + step < a.R) load(r0 + step + grp);
+    if (MODE != kQ8) {
+      // sum over the row of what `term` makes of each value
+      auto sum = [&](auto term, uint32_t* slot) {
+        float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
-    const RowQ8 q(max_row<LPR>(top, slots[2]));
-    if (mine) {
-      int8_t* d = a.q + row * a.Kp;
+        for (int v = 0; v < VPL; ++v) {
+          const int c = lane + v * LPR;
+          if (c >= n) continue;
+          if (ragged) {
+            const int skip = max(c * E + E - C, 0);
+#pragma unroll
+            for (int j = 0; j < E; ++j) s = j >= skip ? term(s, f[v][j]) : s;
+          } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) s = term(s, f[v][j]);
+          }
+        }
+        return sum_row<LPR>(s, slot);
+      };
+      const float mean = sum([](float s, float x) { return s + x; }, slots[turn][0]) * a.inv_c;
+#pragma unroll
+      for (int v = 0; v < VPL; ++v)
+#pragma unroll
+        for (int j = 0; j < E; ++j) f[v][j] -= mean;
+      const float sq = sum([](float s, float x) { return fmaf(x, x, s); }, slots[turn][1]);
+      const float rstd = __builtin_amdgcn_rsqf(fmaf(sq, a.inv_c, a.eps));
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        const int c = lane + v * LPR;
-        if (c < n) store_q8<E>(d + min(c * E, C - E), q, f[v]);
+        const int c = lane + v * LPR, i = min(c * E, C - E);
+        if (c >= n) continue;
+        float w[E], b[E];
+        keep_packed(gamma[v]);
+        keep_packed(beta[v]);
+        if (a.gamma) T::unpack(gamma[v], w);
+        if (a.beta) T::unpack(beta[v], b);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          f[v][j] = fmaf(f[v][j] * rstd, a.gamma ? w[j] : 1.f, a.beta ? b[j] : 0.f);
+        if (MODE == kNorm && mine) T::store(a.out, row * C + i, f[v]);
       }
-      if (lane < a.Kp - C) d[C + lane] = 0;  // fewer than 16
-      if (lane == 0) a.scale[row] = q.scale;
+      if (MODE == kNorm && mine && lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+      }
+    }
+    if (MODE != kNorm) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int v = 0; v < VPL; ++v)
+        if (lane + v * LPR < n)
+#pragma unroll
+          for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
+      const RowQ8 q(max_row<LPR>(top, slots[turn][2]));
+      if (mine) {
+        int8_t* d = a.q + row * a.Kp;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+          const int c = lane + v * LPR;
+          if (c < n) store_q8<E>(d + min(c * E, C - E), q, f[v]);
+        }
+        if (lane < a.Kp - C) d[C + lane] = 0;  // fewer than 16
+        if (lane == 0) a.scale[row] = q.scale;
+      }
     }
   }
 }
@@ -98,8 +136,9 @@ template <int DT, int MODE>
 __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
   using T = Chunk<DT>;
   __shared__ uint32_t slots[3][4];
-  const size_t row = blockIdx.x;
   const int C = a.C;
+  for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
+  const size_t row = r;
   const char* x = static_cast<const char*>(a.x) + row * a.ldx * T::kSize;
   float mean = 0.f, rstd = 1.f;
   if (MODE != kQ8) {
@@ -130,29 +169,38 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
     for (int c = threadIdx.x; c < C; c += 256) top = max(top, __float_as_uint(value(c)) & 0x7fffffffu);
     const RowQ8 q(max_row<256>(top, slots[2]));
     int8_t* d = a.q + row * a.Kp;
-    for (int c = threadIdx.x; c < a.Kp; c += 256) d[c] = c < C ? (int8_t)(q.bits(value(c)) & 0xff) : 0;
+    for (int c = threadIdx.x; c < a.Kp; c += 256) d[c] = c < C ? q.one(value(c)) : 0;
     if (threadIdx.x == 0) a.scale[row] = q.scale;
+  }
+  __syncthreads();  // the words of slots are free again
   }
 }
 
+// The lanes and chunks for rows of n chunks: at most three a lane, whose registers leave
+// three waves a SIMD and more.  Many short rows lie four to a wave, 16 lanes each: their
+// sums take four steps within 16 lanes, and a wave has more bytes in flight.
 template <int DT, int MODE>
 hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
   constexpr int E = Chunk<DT>::E;
   const int n = (a.C + E - 1) / E;
   void* argv[] = {const_cast<RowArgs*>(&a)};
-  auto go = [&](const void* fn, int lpr) {
-    const int threads = lpr > 256 ? lpr : 256, per = threads / lpr;
-    return hipLaunchKernel(fn, dim3((unsigned)((a.R + per - 1) / per)), dim3(threads), argv, 0, stream);
+  // `rows` a workgroup and turn; at most `per_cu` workgroups a CU, with equal numbers of turns
+  auto go = [&](const void* fn, int rows, int per_cu = 16) {
+    const long long units = ((long long)a.R + rows - 1) / rows, most = 256LL * per_cu;
+    const long long turns = (units + most - 1) / most;
+    return hipLaunchKernel(fn, dim3((unsigned)((units + turns - 1) / turns)), dim3(256), argv, 0, stream);
   };
-  if (a.C < E || n > 2048) return go((const void*)&row_any_kernel<DT, MODE>, 256);
-  if (n <= 16) return go((const void*)&row_kernel<DT, MODE, 16, 1>, 16);
-  if (n <= 32) return go((const void*)&row_kernel<DT, MODE, 16, 2>, 16);
-  if (n <= 64) return go((const void*)&row_kernel<DT, MODE, 64, 1>, 64);
-  if (n <= 128) return go((const void*)&row_kernel<DT, MODE, 64, 2>, 64);
-  if (n <= 256) return go((const void*)&row_kernel<DT, MODE, 64, 4>, 64);
-  if (n <= 512) return go((const void*)&row_kernel<DT, MODE, 256, 2>, 256);
-  if (n <= 1024) return go((const void*)&row_kernel<DT, MODE, 256, 4>, 256);
-  return go((const void*)&row_kernel<DT, MODE, 256, 8>, 256);
+#define GL_ROW(LPR, VPL) go((const void*)&row_kernel<DT, MODE, LPR, VPL>, 256 / LPR)
+  if (a.C < E || n > 2048) return go((const void*)&row_any_kernel<DT, MODE>, 1);
+  if (n <= 16) return GL_ROW(16, 1);
+  if (n <= 48 && a.R >= 4096) return n <= 32 ? GL_ROW(16, 2) : GL_ROW(16, 3);
+  if (n <= 192) return n <= 64 ? GL_ROW(64, 1) : n <= 128 ? GL_ROW(64, 2) : GL_ROW(64, 3);
+  if (n <= 384) return n <= 256 ? GL_ROW(128, 2) : GL_ROW(128, 3);
+  if (n <= 1024) return n <= 512 ? GL_ROW(256, 2) : n <= 768 ? GL_ROW(256, 3) : GL_ROW(256, 4);
+  // two waves a SIMD: more workgroups would load gamma and beta for a row each (4096 x 8192
+  // fp32: 55 us, 91 with 16 a CU)
+  return go((const void*)&row_kernel<DT, MODE, 256, 8>, 1, 2);
+#undef GL_ROW
 }
 
 hipError_t launch_layer_norm(const RowArgs& a, int dt_bf16, hipStream_t stream) {

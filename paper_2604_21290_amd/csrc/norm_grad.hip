@@ -5,72 +5,109 @@
 // averages, write dx, and each lane adds its channels' terms of dgamma and dbeta to
 // sums of its own over all rows that it meets.  A workgroup then adds its lanes'
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
+// Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
+// 108 (4.7), 100352 x 320 42-50 (3.9-4.6), 100352 x 80 16.5 (2.9, of which the second
+// kernel takes 3).  Few rows take one launch (196 x 192 3.5 us, 7.4 in two kernels).
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"
 
 namespace gl {
 
-// LPR lanes hold a row, VPL chunks each; NT threads a workgroup.
+// LPR lanes hold a row, VPL chunks each; NT threads a workgroup.  A row's loads are
+// under way while the one before it is worked on.
 template <int DT, int LPR, int VPL, int NT>
 __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, GROUPS = NT / LPR, NW = NT / 64;
   constexpr int COLS = LPR * VPL * E;  // columns a group covers
-  __shared__ uint32_t slots[2][2][LPR > 64 ? LPR / 64 : 1];
+  __shared__ uint32_t slots[2][2][NT / 64];
   __shared__ float sums[LPR > 64 ? 1 : NW * COLS];
   const int lane = threadIdx.x & (LPR - 1), grp = threadIdx.x / LPR;
   const int C = a.C, n = (C + E - 1) / E;
+  const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
-  float w[VPL][E], dg[VPL][E], db[VPL][E];
-#pragma unroll
-  for (int v = 0; v < VPL; ++v)
-#pragma unroll
-    for (int j = 0; j < E; ++j) w[v][j] = 1.f, dg[v][j] = db[v][j] = 0.f;
-  if (a.gamma)
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR;
-      if (c < n) T::load(a.gamma, min(c * E, C - E), w[v]);
-    }
-  int turn = 0;
-  // every group of a workgroup makes the same number of turns
-  for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < a.R; r0 += (long long)gridDim.x * GROUPS) {
-    const bool mine = r0 + grp < a.R;
-    const size_t row = mine ? r0 + grp : a.R - 1;
+  uint4 raw_x[VPL], raw_d[VPL];
+  float mean, rstd;
+  auto load = [&](long long r) {
+    const size_t row = min(r, (long long)a.R - 1);
     const char* x = static_cast<const char*>(a.x) + row * a.ldx * T::kSize;
     const char* dy = static_cast<const char*>(a.dy) + row * a.lddy * T::kSize;
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float f[VPL][E], d[VPL][E];
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       const int c = lane + v * LPR;
       if (c < n) {
-        T::load(x, min(c * E, C - E), f[v]);
-        T::load(dy, min(c * E, C - E), d[v]);
+        raw_x[v] = T::raw(x, min(c * E, C - E));
+        raw_d[v] = T::raw(dy, min(c * E, C - E));
       }
     }
+    mean = a.mean[row];
+    rstd = a.rstd[row];
+  };
+  const long long step = (long long)gridDim.x * GROUPS;
+  long long r0 = (long long)blockIdx.x * GROUPS;
+  load(r0 + grp);
+
+  float dg[VPL][E], db[VPL][E];
+  uint4 raw_w[VPL];
+#pragma unroll
+  for (int v = 0; v < VPL; ++v) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) dg[v][j] = db[v][j] = 0.f;
+    const int c = lane + v * LPR;
+    if (a.gamma && c < n) raw_w[v] = T::raw(a.gamma, min(c * E, C - E));
+  }
+  int turn = 0;
+  // every group of a workgroup makes the same number of turns
+  for (; r0 < a.R; r0 += step, turn ^= 1) {
+    const bool mine = r0 + grp < a.R;
+    const size_t row = r0 + grp;
+    float f[VPL][E], d[VPL][E];
+    const float mu = mean, rs = rstd;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v)
+      if (lane + v * LPR < n) {
+        T::unpack(raw_x[v], f[v]);
+        T::unpack(raw_d[v], d[v]);
+      }
+    if (r0 + step < a.R) load(r0 + step + grp);
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR, skip = max(c * E + E - C, 0);
-      if (c < n)
+      const int c = lane + v * LPR;
+      if (c >= n) continue;
+      float w[E];
+      keep_packed(raw_w[v]);
+      if (a.gamma) T::unpack(raw_w[v], w);
+      if (!mine)
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[v][j] = 0.f;  // rows past the last count for nothing
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        f[v][j] = (f[v][j] - mu) * rs;
+        dg[v][j] = fmaf(d[v][j], f[v][j], dg[v][j]);
+        db[v][j] += d[v][j];
+        if (a.gamma) d[v][j] *= w[j];
+      }
+      if (ragged) {
+        const int skip = max(c * E + E - C, 0);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-          f[v][j] = (f[v][j] - mean) * rstd;
-          const float one = mine ? d[v][j] : 0.f;  // rows past the last count for nothing
-          dg[v][j] = fmaf(one, f[v][j], dg[v][j]);
-          db[v][j] += one;
-          d[v][j] *= w[v][j];
           const float h = j >= skip ? d[v][j] : 0.f;
           s0 += h;
           s1 = fmaf(h, f[v][j], s1);
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          s0 += d[v][j];
+          s1 = fmaf(d[v][j], f[v][j], s1);
+        }
+      }
     }
     // two turns' words never meet: a wave is at most one barrier ahead
-    s0 = sum_row<LPR>(s0, slots[turn & 1][0]) * a.inv_c;
-    s1 = sum_row<LPR>(s1, slots[turn & 1][1]) * a.inv_c;
-    ++turn;
+    s0 = sum_row<LPR>(s0, slots[turn][0]) * a.inv_c;
+    s1 = sum_row<LPR>(s1, slots[turn][1]) * a.inv_c;
     if (a.dx && mine)
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
@@ -78,7 +115,7 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
         if (c < n) {
           float y[E];
 #pragma unroll
-          for (int j = 0; j < E; ++j) y[j] = (d[v][j] - fmaf(f[v][j], s1, s0)) * rstd;
+          for (int j = 0; j < E; ++j) y[j] = (d[v][j] - fmaf(f[v][j], s1, s0)) * rs;
           T::store(a.dx, row * C + min(c * E, C - E), y);
         }
       }
@@ -118,6 +155,7 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
     for (int c = threadIdx.x; c < C; c += NT) {
       const int last = (n - 1) * E, at = c < last ? c : c + (n * E - C);
       float s = sums[at];
+#pragma unroll
       for (int k = 1; k < NW; ++k) s += sums[k * COLS + at];
       pg[half * C + c] = s;
     }
@@ -125,23 +163,118 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-// out[c] = sum over the G rows of part [G, cols]: 64 columns a workgroup, its 16
-// waves take every 16th row.
+// out[c] = sum over the G rows of part [G, cols]: 32 columns a workgroup, 32 rows at
+// a time, in the same order always.
 __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, int G, int cols,
                                                              float* dgamma, float* dbeta) {
-  __shared__ float sums[16][64];
-  const int t = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + t;
+  __shared__ float sums[32][33];
+  const int t = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + t;
   float s = 0.f;
   if (c < 2 * cols)
-    for (int g = w; g < G; g += 16) s += part[(size_t)g * 2 * cols + c];
+#pragma unroll 8
+    for (int g = w; g < G; g += 32) s += part[(size_t)g * 2 * cols + c];
   sums[w][t] = s;
   __syncthreads();
   if (w == 0 && c < 2 * cols) {
-    for (int k = 1; k < 16; ++k) s += sums[k][t];
+#pragma unroll
+    for (int k = 1; k < 32; ++k) s += sums[k][t];
     if (c < cols) {
       if (dgamma) dgamma[c] = s;
     } else if (dbeta) dbeta[c - cols] = s;
+  }
+}
+
+// Few rows, in one launch and without a workspace: the first `row_wgs` workgroups take
+// rows, 256 / LPR each, the others 16 chunks of columns each, over all rows: the
+// columns' sums need no average of a row, and reading a small input twice is cheap.
+template <int DT, int LPR, int VPL>
+__global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int row_wgs) {
+  using T = Chunk<DT>;
+  constexpr int E = T::E, GROUPS = 256 / LPR;
+  __shared__ uint32_t slots[2][4];
+  __shared__ float sums[2][16][16 * E + 1];
+  const int C = a.C, n = (C + E - 1) / E;
+  if ((int)blockIdx.x < row_wgs) {
+    const int lane = threadIdx.x & (LPR - 1);
+    const long long r = (long long)blockIdx.x * GROUPS + threadIdx.x / LPR;
+    const bool mine = r < a.R;
+    const size_t row = mine ? r : a.R - 1;
+    const char* x = static_cast<const char*>(a.x) + row * a.ldx * T::kSize;
+    const char* dy = static_cast<const char*>(a.dy) + row * a.lddy * T::kSize;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float f[VPL][E], d[VPL][E], s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int c = lane + v * LPR, i = min(c * E, C - E);
+      if (c >= n) continue;
+      T::unpack(T::raw(x, i), f[v]);
+      T::unpack(T::raw(dy, i), d[v]);
+      if (a.gamma) {
+        float w[E];
+        T::unpack(T::raw(a.gamma, i), w);
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[v][j] *= w[j];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int c = lane + v * LPR, skip = max(c * E + E - C, 0);
+      if (c >= n) continue;
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        f[v][j] = (f[v][j] - mean) * rstd;
+        const float h = j >= skip ? d[v][j] : 0.f;
+        s0 += h;
+        s1 = fmaf(h, f[v][j], s1);
+      }
+    }
+    s0 = sum_row<LPR>(s0, slots[0]) * a.inv_c;
+    s1 = sum_row<LPR>(s1, slots[1]) * a.inv_c;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int c = lane + v * LPR;
+      if (c >= n || !mine) continue;
+      float y[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) y[j] = (d[v][j] - fmaf(f[v][j], s1, s0)) * rstd;
+      T::store(a.dx, row * C + min(c * E, C - E), y);
+    }
+    return;
+  }
+  const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
+  const int c = ((int)blockIdx.x - row_wgs) * 16 + lane, i = min(c * E, C - E);
+  float dg[E] = {}, db[E] = {};
+  if (c < n) {
+#pragma unroll 4
+    for (int r = grp; r < a.R; r += 16) {
+      float f[E], d[E];
+      T::unpack(T::raw(static_cast<const char*>(a.x) + (size_t)r * a.ldx * T::kSize, i), f);
+      T::unpack(T::raw(static_cast<const char*>(a.dy) + (size_t)r * a.lddy * T::kSize, i), d);
+      const float mean = a.mean[r], rstd = a.rstd[r];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        dg[j] = fmaf(d[j], (f[j] - mean) * rstd, dg[j]);
+        db[j] += d[j];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    sums[0][grp][lane * E + j] = dg[j];
+    sums[1][grp][lane * E + j] = db[j];
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < 2 * 16 * E; k += 256) {
+    const int half = k / (16 * E), at = k % (16 * E);
+    const int ch = ((int)blockIdx.x - row_wgs) * 16 + at / E, col = min(ch * E, C - E) + at % E;
+    // (the last chunk's first columns are the one before's)
+    if (ch >= n || col < ch * E) continue;
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) s += sums[half][q][at];
+    float* out = half ? a.dbeta : a.dgamma;
+    if (out) out[col] = s;
   }
 }
 
@@ -193,8 +326,11 @@ namespace {
 
 struct Plan {
   const void* fn;  // null: value by value
-  int threads, groups, grid;
+  int threads, groups, grid;  // grid 0: the one launch for few rows
 };
+
+// 16 column workgroups' worth of rows: a lane of theirs adds at most 64 rows
+constexpr int kFewRows = 1024;
 
 template <int DT>
 Plan plan(int R, int C) {
@@ -205,14 +341,23 @@ Plan plan(int R, int C) {
     return Plan{fn, threads, groups, (int)std::min<long long>(((long long)R + groups - 1) / groups, most)};
   };
   if (C < E || n > 2048) return Plan{nullptr, 256, 1, std::min(R, 256)};
-  if (n <= 16) return make((const void*)&norm_grad_kernel<DT, 16, 1, 1024>, 1024, 16, 512);
+  if (R <= kFewRows && n <= 1024) {
+    if (n <= 16) return Plan{(const void*)&norm_grad_few_kernel<DT, 16, 1>, 256, 16, 0};
+    if (n <= 64) return Plan{(const void*)&norm_grad_few_kernel<DT, 64, 1>, 256, 4, 0};
+    if (n <= 256) return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 1>, 256, 1, 0};
+    return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 4>, 256, 1, 0};
+  }
+  if (n <= 16) return make((const void*)&norm_grad_kernel<DT, 16, 1, 512>, 512, 16, 512);
   if (n <= 32) return make((const void*)&norm_grad_kernel<DT, 16, 2, 512>, 512, 16, 512);
-  if (n <= 64) return make((const void*)&norm_grad_kernel<DT, 64, 1, 512>, 512, 64, 512);
+  if (n <= 48) return make((const void*)&norm_grad_kernel<DT, 16, 3, 512>, 512, 16, 256);
+  if (n <= 64) return make((const void*)&norm_grad_kernel<DT, 16, 4, 512>, 512, 16, 256);
   if (n <= 128) return make((const void*)&norm_grad_kernel<DT, 64, 2, 512>, 512, 64, 512);
+  if (n <= 192) return make((const void*)&norm_grad_kernel<DT, 64, 3, 256>, 256, 64, 512);
   if (n <= 256) return make((const void*)&norm_grad_kernel<DT, 64, 4, 256>, 256, 64, 512);
-  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 512);
+  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 1024);
+  if (n <= 768) return make((const void*)&norm_grad_kernel<DT, 256, 3, 256>, 256, 256, 512);
   if (n <= 1024) return make((const void*)&norm_grad_kernel<DT, 256, 4, 256>, 256, 256, 512);
-  return make((const void*)&norm_grad_kernel<DT, 1024, 2, 1024>, 1024, 1024, 256);
+  return make((const void*)&norm_grad_kernel<DT, 512, 4, 512>, 512, 512, 256);
 }
 
 template <int DT>
@@ -221,8 +366,14 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
   float* const part = a.part;
   const bool sums = a.dgamma || a.dbeta;
   if (!sums) a.part = nullptr;
-  void* argv[] = {&a};
+  void* argv[] = {&a, nullptr};
   hipError_t e = hipSuccess;
+  if (!p.grid) {
+    int row_wgs = a.dx ? (a.R + p.groups - 1) / p.groups : 0;
+    const int n = (a.C + Chunk<DT>::E - 1) / Chunk<DT>::E, col_wgs = sums ? (n + 15) / 16 : 0;
+    argv[1] = &row_wgs;
+    return hipLaunchKernel(p.fn, dim3(row_wgs + col_wgs), dim3(p.threads), argv, 0, stream);
+  }
   if (p.fn) {
     e = hipLaunchKernel(p.fn, dim3(p.grid), dim3(p.threads), argv, 0, stream);
   } else {
@@ -234,7 +385,7 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
                           dim3(256), argv, 0, stream);
   }
   if (e != hipSuccess || !sums) return e;
-  norm_grad_sum_kernel<<<(2 * a.C + 63) / 64, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
+  norm_grad_sum_kernel<<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 

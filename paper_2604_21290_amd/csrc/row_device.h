@@ -24,9 +24,10 @@ template <>
 struct Chunk<1> {
   static constexpr int E = 8;
   static constexpr size_t kSize = 2;
-  __device__ __forceinline__ static void load(const void* p, size_t i, float* f) {
-    unpack_bf16x8(load16_any(static_cast<const uint16_t*>(p) + i), f);
+  __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
+    return load16_any(static_cast<const uint16_t*>(p) + i);
   }
+  __device__ __forceinline__ static void unpack(const uint4& v, float* f) { unpack_bf16x8(v, f); }
   __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
     store16_any(static_cast<uint16_t*>(p) + i, pack_bf16x8(f));
   }
@@ -42,10 +43,12 @@ template <>
 struct Chunk<0> {
   static constexpr int E = 4;
   static constexpr size_t kSize = 4;
-  __device__ __forceinline__ static void load(const void* p, size_t i, float* f) {
-    const u32x4_any4 v = *reinterpret_cast<const u32x4_any4*>(static_cast<const float*>(p) + i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(v[j]);
+  __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
+    return __builtin_bit_cast(uint4, *reinterpret_cast<const u32x4_any4*>(static_cast<const float*>(p) + i));
+  }
+  __device__ __forceinline__ static void unpack(const uint4& v, float* f) {
+    f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
   }
   __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
     u32x4_any4 v;
@@ -61,10 +64,16 @@ struct Chunk<0> {
   }
 };
 
+// A packed vector that a loop keeps: hides from the compiler that it does not change, or
+// it would keep the unpacked values, twice the registers, instead.
+__device__ __forceinline__ void keep_packed(uint4& v) {
+  asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w));
+}
+
 // ---------------------------------------------------------------------------
 // sums and maxima over the LPR lanes (16, 64, or a workgroup's LPR / 64 waves) of
 // one row; every lane of the group gets the result, in the same order always.
-// `slot`: LPR / 64 words of LDS for this reduction alone (workgroup rows).
+// `slot`: a word of LDS for each wave, for this reduction alone (LPR > 64).
 // ---------------------------------------------------------------------------
 struct AddF {
   __device__ __forceinline__ static uint32_t of(uint32_t a, uint32_t b) {
@@ -92,7 +101,8 @@ __device__ __forceinline__ uint32_t reduce_row(uint32_t v, uint32_t* slot) {
   v = Op::of(a, b);
   if (LPR == 64) return v;
   constexpr int NW = LPR / 64;
-  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  slot += threadIdx.x / LPR * NW;
+  if ((threadIdx.x & 63) == 0) slot[(threadIdx.x >> 6) % NW] = v;
   __syncthreads();
   v = slot[0];
 #pragma unroll
@@ -122,6 +132,7 @@ constexpr uint32_t kTopMin = 0x04800000u;  // 2^-118: a row below it counts as z
 
 struct RowQ8 {
   float c, a, inv, scale;
+  uint32_t keep;  // 0: the row is not finite, and all its values are 0
   __device__ __forceinline__ explicit RowQ8(uint32_t top) {
     const bool zero = top < kTopMin, bad = top >= 0x7f800000u;  // an infinity or a NaN in the row
     const uint32_t t = zero || bad ? 0x3f800000u : top;
@@ -133,19 +144,19 @@ struct RowQ8 {
     const float f = __uint_as_float(t), s = f * (1.f / 127.f);
     scale = zero ? 0.f : bad ? __uint_as_float(0x7fc00000u)
                              : fmaf(fmaf(-127.f, s, f), 1.f / 127.f, s);
-    nan = bad;
+    keep = bad ? 0 : ~0u;
   }
-  bool nan;
   // the quotient's whole number in the low byte
   __device__ __forceinline__ uint32_t bits(float x) const {
-    const float t = (nan ? 0.f : x) * c;
+    const float t = x * c;
     const float q = t * inv;
     return __float_as_uint(fmaf(fmaf(-q, a, t), inv, q) + 12582912.f);
   }
+  __device__ __forceinline__ int8_t one(float x) const { return (int8_t)(bits(x) & keep); }
   __device__ __forceinline__ uint32_t pack4(const float* f) const {
     const uint32_t lo = __builtin_amdgcn_perm(bits(f[1]), bits(f[0]), 0x0c0c0400u);
     const uint32_t hi = __builtin_amdgcn_perm(bits(f[3]), bits(f[2]), 0x04000c0cu);
-    return lo | hi;
+    return (lo | hi) & keep;
   }
 };
 

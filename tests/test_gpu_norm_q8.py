@@ -396,7 +396,8 @@ def test_refusals():
     with pytest.raises(api.GraphLeapError):
         api.layer_norm_backward(x, x, m, m, need=(False, False, False))
     with pytest.raises(api.GraphLeapError) as e:
-        api.layer_norm_backward(x, x, m, m, ws=api.Workspace(16, x.device))
+        y = torch.zeros((5000, 64), dtype=torch.bfloat16, device="cuda")
+        api.layer_norm_backward(y, y, *2 * [torch.zeros(5000, device="cuda")], ws=api.Workspace(16, x.device))
     assert e.value.status == 9
     q = api.quantize_rows(x)
     with pytest.raises(ValueError):

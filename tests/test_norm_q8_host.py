@@ -54,11 +54,12 @@ def test_layer_norm_backward_refusals():
     for bad in (dict(dy=P(0, 1)), dict(mean=P(2, 2)), dict(dg=P(6, 2)), dict(dx=P(5, 1))):
         assert _grad(**bad) == "GL_ERR_ALIGNMENT", bad
     for bad in (dict(dx=P(0, 16)), dict(dx=P(1, 16)), dict(dg=P(5, 64)), dict(db=P(6, 64)), dict(dg=P(2, 64)),
-                dict(ws=P(1, 64)), dict(ws=P(6, 64))):
+                dict(R=5000, ws=P(1, 64)), dict(R=5000, ws=P(6, 64))):
         assert _grad(**bad) == "GL_ERR_ALIAS", bad
-    need = api.lib().gl_layer_norm_backward_workspace_bytes(64, 100, 1)
+    many = dict(R=5000)
+    need = api.lib().gl_layer_norm_backward_workspace_bytes(5000, 100, 1)
     assert need >= 800
-    assert _grad(ws=None) == _grad(n=need - 1) == _grad(ws=P(8, 8)) == "GL_ERR_WORKSPACE"
+    assert _grad(ws=None, **many) == _grad(n=need - 1, **many) == _grad(ws=P(8, 8), **many) == "GL_ERR_WORKSPACE"
     assert api.lib().gl_layer_norm_backward_workspace_bytes(0, 100, 1) == 0
     assert api.lib().gl_layer_norm_backward_workspace_bytes(64, 100, 5) == 0
 

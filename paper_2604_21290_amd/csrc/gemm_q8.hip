@@ -322,6 +322,59 @@ hipError_t launch_pipe_q8(const GemmQ8Args& a, hipStream_t stream) {
   return launch_with_smem(fn, grid, dim3(G::kThreads), G::kSmem, stream, nullptr, nullptr, a);
 }
 
+// ---------------------------------------------------------------------------
+// Few rows: the weights' bytes bound the layer, so every CU has to stream some.  A
+// workgroup takes 16 columns and 16 rows; its eight waves split K, 64 bytes of each row
+// in turn, and load their operands straight into registers, up to U steps before any is
+// used.  The eight partial sums meet in LDS.  (8192 x 8192 weights, one row: 5.2 TB/s.)
+// ---------------------------------------------------------------------------
+template <int DT, int ACT_OUT>
+__global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
+  constexpr int NW = 8, U = 8;
+  __shared__ __align__(16) int part[NW][256];
+  const int R = a.R, Cout = a.Cout, rowb = a.Kp;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, t = lane & 15;
+  const char* pw = reinterpret_cast<const char*>(a.W) + (size_t)min(n0 + t, Cout - 1) * rowb;
+  const char* pa = reinterpret_cast<const char*>(a.A) + (size_t)min(m0 + t, R - 1) * rowb;
+  i32x4 acc = {0, 0, 0, 0};
+  for (int k0 = w * 64; k0 < rowb; k0 += NW * 64 * U) {
+    uint4 fw[U], fa[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int ku = k0 + u * NW * 64, k = ku + g * 16;
+      fw[u] = fa[u] = make_uint4(0, 0, 0, 0);
+      if (ku < rowb) {  // uniform
+        const int at = k < rowb ? k : 0;
+        fw[u] = *reinterpret_cast<const uint4*>(pw + at);
+        fa[u] = *reinterpret_cast<const uint4*>(pa + at);
+        if (k >= rowb) fw[u] = make_uint4(0, 0, 0, 0);  // past the rows' end
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = mfma_i8(fw[u], fa[u], acc);
+  }
+  *reinterpret_cast<i32x4*>(&part[w][t * 16 + g * 4]) = acc;
+  __syncthreads();
+  const int row = m0 + (tid >> 4), n = n0 + (tid & 15);
+  if (tid >= 256 || row >= R || n >= Cout) return;
+  int s = 0;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) s += part[k][tid];
+  float y = fmaf((float)s, a.sa[row] * a.sw[n], a.bias ? load1<DT>(a.bias, n) : 0.f);
+  if (ACT_OUT) y = gelu_f32(y);
+  const size_t at = (size_t)row * Cout + n;
+  if (a.residual) y += load1<DT>(a.residual, at);
+  store1<DT>(a.out, at, y);
+}
+
+template <int DT>
+hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
+  const void* fn = a.act_out ? (const void*)&gemm_q8_rows_kernel<DT, 1> : (const void*)&gemm_q8_rows_kernel<DT, 0>;
+  return launch_with_smem(fn, dim3((a.Cout + 15) / 16, (a.R + 15) / 16), dim3(512), 0, stream, nullptr, nullptr, a);
+}
+
 // The tile whose last round ends first.  A round of 128 x 128 tiles, two to a CU, is
 // taken for 2.5 units, of 256 x 256, one to a CU, for 4, and of 64 x 64, two to a CU,
 // for 1 (half of each where one to a CU suffices): what each took of a product of
@@ -332,8 +385,14 @@ hipError_t launch_pipe_q8(const GemmQ8Args& a, hipStream_t stream) {
 //   12544x2560x640      32.7         25.4 *      38
 //   2048x2048x2048      25.0         14.5 *      17.3
 //   1000x8000x1000      77.5         45.6        19.8 *
+// The kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
+// 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
+// 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
+// 3.4 (3.9); at 196x2560x640 8.0 (7.4).
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
+  const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);
+  if (a.R <= 16 || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20)) return launch_rows_q8<DT>(a, stream);
   auto rounds = [&](int bm, int bn, int per_cu) {
     const long t = ((long)(a.R + bm - 1) / bm) * ((a.Cout + bn - 1) / bn), slots = 256 * per_cu;
     return t <= 256 ? 1.0 / per_cu : (double)((t + slots - 1) / slots);

@@ -234,6 +234,12 @@ LAYER_CASES = [
     (4100, 320, 80, False, True, True), (6272, 192, 768, True, False, True), (12544, 72, 641, False, True, True),
     (20000, 96, 24, False, True, True), (2049, 4096, 515, False, False, True), (5, 131071, 9, False, False, True),
     (8192, 640, 2048, True, True, True), (3000, 16, 4000, False, True, True),
+    # tiles of 256 x 256 with ragged edges, of 128 x 128, and of 64 x 64 in two rounds
+    (16380, 1000, 1010, True, True, True), (20000, 200, 300, False, True, True),
+    (33000, 48, 40, False, True, True), (33000, 130, 40, True, False, True),
+    # on both sides of the rule for few rows
+    (16, 300, 5000, False, True, True), (17, 300, 5000, False, True, True), (256, 4096, 256, False, True, True),
+    (257, 4096, 257, True, True, True), (196, 2560, 640, False, True, True), (1, 131071, 33, False, False, True),
 ]
 
 

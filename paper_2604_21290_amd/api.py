@@ -106,6 +106,23 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_native = None
+
+
+def _calls():
+    """The native argument marshalling of the short calls (csrc/calls.cpp)."""
+    global _native
+    if _native is None:
+        lib()
+        try:
+            from . import _calls as native
+        except ImportError as e:
+            raise RuntimeError("_calls.so is not built; run `python -m paper_2604_21290_amd.build`") from e
+        native.open(LIB_PATH)
+        _native = native
+    return _native
+
+
 def _check(name: str, status: int):
     if status != 0:
         raise GraphLeapError(name, status, lib().gl_last_error().decode())
@@ -269,7 +286,9 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None,
 
 
 # ---------------------------------------------------------------------------
-# layer norm and 8-bit layers
+# layer norm and 8-bit layers: these calls take a few microseconds on the device, so
+# their ordinary form (current stream, outputs allocated here) goes through native
+# marshalling first, which returns None for anything else
 # ---------------------------------------------------------------------------
 class Q8Rows:
     """8-bit rows (gl_quantize_rows): q [..., Kp] int8, whose last Kp - K bytes
@@ -357,6 +376,10 @@ def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None,
     """(x - mean) * rstd * gamma + beta over the last axis (gl_layer_norm).  x may
     be a slice of wider rows.  stats: return (out, mean, rstd), the row statistics
     in float32 that layer_norm_backward takes."""
+    if stream is None and out is None:
+        r = (_native or _calls()).layer_norm(x, gamma, beta, eps, stats)
+        if r is not None:
+            return r
     R, C, ld = _rows(x)
     _like("gamma", gamma, (C,), x.dtype, x)
     _like("beta", beta, (C,), x.dtype, x)
@@ -387,6 +410,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     and the row statistics it returned (gl_layer_norm_backward); dgamma and dbeta
     are float32 sums over all rows.  need: which of the three to compute (None
     for the others).  ws: the call's workspace (allocated here when not given)."""
+    if stream is None and ws is None and all(need):
+        r = (_native or _calls()).layer_norm_backward(dy, x, mean, rstd, gamma)
+        if r is not None:
+            return r
     R, C, ldx = _rows(x)
     Rd, Cd, lddy = _rows(dy)
     if dy.shape != x.shape or dy.dtype != x.dtype:
@@ -431,6 +458,10 @@ def _q8_out(x: torch.Tensor, R: int, K: int, out: Q8Rows | None, stream) -> Q8Ro
 def quantize_rows(x: torch.Tensor, out: Q8Rows | None = None, stream=None) -> Q8Rows:
     """x's rows (its last axis) as 8-bit integers with a scale each
     (gl_quantize_rows): activations per token, or a weight per output channel."""
+    if stream is None and out is None:
+        r = (_native or _calls()).quantize_rows(x)
+        if r is not None:
+            return Q8Rows(r[0], r[1], x.shape[-1])
     R, K, ld = _rows(x)
     out = _q8_out(x, R, K, out, stream)
     _hold(stream, x)
@@ -443,6 +474,10 @@ def layer_norm_q8(x: torch.Tensor, gamma: torch.Tensor | None = None,
                   beta: torch.Tensor | None = None, eps: float = 1e-5, out: Q8Rows | None = None,
                   stream=None) -> Q8Rows:
     """layer_norm and quantize_rows in one pass (gl_layer_norm_q8)."""
+    if stream is None and out is None:
+        r = (_native or _calls()).layer_norm_q8(x, gamma, beta, eps)
+        if r is not None:
+            return Q8Rows(r[0], r[1], x.shape[-1])
     R, K, ld = _rows(x)
     _like("gamma", gamma, (K,), x.dtype, x)
     _like("beta", beta, (K,), x.dtype, x)
@@ -458,6 +493,11 @@ def linear_q8(x: Q8Rows, W: Q8Rows, bias: torch.Tensor | None = None, act_out: i
               out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """out[..., Cout] = act_out(x W^T + bias) + residual of 8-bit rows x and weights
     W [Cout, K] (gl_linear_q8); bias, residual and out are in `dtype`."""
+    if stream is None and out is None and (dtype is torch.bfloat16 or dtype is torch.float32):
+        r = (_native or _calls()).linear_q8(x.q, x.scale, x.K, W.q, W.scale, W.K, bias, act_out, residual,
+                                            dtype is torch.bfloat16)
+        if r is not None:
+            return r
     R, Kp, _ = _rows(x.q)
     if W.q.dim() != 2 or x.K != W.K:
         raise ValueError(f"linear_q8: rows {tuple(x.shape)} do not match weights {tuple(W.shape)}")

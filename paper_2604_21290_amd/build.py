@@ -1,4 +1,4 @@
-"""Build libgraphleap.so in-tree with hipcc for gfx950.
+"""Build libgraphleap.so in-tree with hipcc for gfx950, and the binding's _calls.so.
 
     python -m paper_2604_21290_amd.build
 """
@@ -13,6 +13,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libgraphleap.so")
+CALLS = os.path.join(PKG, "_calls.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -39,6 +40,31 @@ def _run(cmd):
     return res.returncode, err
 
 
+def build_calls(verbose: bool = True) -> str:
+    """Compile the native argument marshalling (csrc/calls.cpp: host code, against the
+    installed torch and Python) to _calls.so."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    tmp = CALLS + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(base, "include"),
+           "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-I", "/opt/rocm/include", "-I", sysconfig.get_paths()["include"],
+           os.path.join(PKG, "csrc", "calls.cpp"), "-o", tmp,
+           "-L", os.path.join(base, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+    if verbose:
+        print("[build]", " ".join(cmd), flush=True)
+    rc, err = _run(cmd)
+    if rc != 0:
+        raise RuntimeError(f"{cmd[0]} failed ({rc}) on calls.cpp:\n{err}")
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build_library(verbose: bool = True, jobs: int | None = None) -> str:
     """Compile each source to an object in parallel, then link the library."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -54,8 +80,10 @@ def build_library(verbose: bool = True, jobs: int | None = None) -> str:
     if verbose:
         for c, _ in cmds:
             print("[build]", " ".join(c), flush=True)
-    with cf.ThreadPoolExecutor(jobs) as ex:
+    with cf.ThreadPoolExecutor(jobs + 1) as ex:
+        calls = ex.submit(build_calls, verbose)
         results = list(ex.map(lambda c: _run(c[0]), cmds))
+        calls.result()
     for (cmd, _), (rc, err) in zip(cmds, results):
         if rc != 0:
             raise RuntimeError(f"hipcc failed ({rc}) on {cmd[-3]}:\n{err}")

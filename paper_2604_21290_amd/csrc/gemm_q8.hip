@@ -19,22 +19,52 @@ __device__ __forceinline__ i32x4 mfma_i8(const uint4& a, const uint4& b, i32x4 a
                                                __builtin_bit_cast(i32x4, b), acc, 0, 0, 0);
 }
 
+// GELU x Phi(x), the error function by Abramowitz and Stegun 7.1.26 as in gelu_f32, with
+// its constants folded: Phi(-|x|) = poly(t) e^(-x^2 / 2), t = 1 / (1 + p |x| / sqrt 2),
+// and x Phi(x) = max(x, 0) - |x| Phi(-|x|).  13 instructions for 16.
+__device__ __forceinline__ float gelu_q8(float x) {
+  const float a = fabsf(x);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, a, 1.f));
+  float q = fmaf(t, 0.5307027145f, -0.7265760135f);
+  q = fmaf(t, q, 0.7107068705f);
+  q = fmaf(t, q, -0.142248368f);
+  q = fmaf(t, q, 0.127414796f);
+  const float y = x * 0.84932180028801907f;  // sqrt(log2(e) / 2)
+  const float e = __builtin_amdgcn_exp2f(-y * y);
+  return fmaf(-a, t * q * e, fmaxf(x, 0.f));
+}
+
 typedef uint32_t u32x4_w __attribute__((ext_vector_type(4), aligned(4), may_alias));
 
-// 8 consecutive values of a bias, a residual or an output at any element's place
+// 8 consecutive values of a residual at any element's place, as they lie in memory
 template <int DT>
-__device__ __forceinline__ void load8(const void* p, size_t i, float* f) {
-  if (DT) {
-    unpack_bf16x8(load16_any(static_cast<const uint16_t*>(p) + i), f);
-  } else {
+struct Raw8 {
+  uint4 v[DT ? 1 : 2];
+  __device__ __forceinline__ void load(const void* p, size_t i) {
+    if (DT) {
+      v[0] = load16_any(static_cast<const uint16_t*>(p) + i);
+    } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const u32x4_w v = reinterpret_cast<const u32x4_w*>(static_cast<const float*>(p) + i)[h];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[4 * h + j] = __uint_as_float(v[j]);
+      for (int h = 0; h < 2; ++h)
+        v[DT ? 0 : h] = __builtin_bit_cast(uint4, reinterpret_cast<const u32x4_w*>(static_cast<const float*>(p) + i)[h]);
     }
   }
-}
+  __device__ __forceinline__ void add_to(float* y) const {
+    if (DT) {
+      float f[8];
+      unpack_bf16x8(v[0], f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] += f[j];
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4& u = v[DT ? 0 : h];
+        y[4 * h] += __uint_as_float(u.x), y[4 * h + 1] += __uint_as_float(u.y);
+        y[4 * h + 2] += __uint_as_float(u.z), y[4 * h + 3] += __uint_as_float(u.w);
+      }
+    }
+  }
+};
 template <int DT>
 __device__ __forceinline__ float load1(const void* p, size_t i) {
   return DT ? bf16_bits_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
@@ -75,6 +105,12 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
 //     accumulators to memory 16 bytes (bf16) a lane, 64 a row, with no trip
 //     through LDS.
 // Tiles are walked so that the 32 that an XCD works on at a time are 8 x 4.
+// What bounds it: at 8192 x 8192 x 8192 (420-430 us, 2.6 POP/s; the library's int8
+// product 440) the matrix cores are busy 66 % of the cycles, at a clock that falls to
+// 1.7-1.8 GHz on random data; with all loads from L2's hottest lines 397 us, so the trip
+// to memory costs 8 %.  Tried and slower there: MFMA 32x32x32 (471 us), stages of 64
+// bytes in four buffers (446), 256 x 128 tiles in three buffers (478), four waves of
+// 128 x 128 (886: operands move between the register files).
 // ---------------------------------------------------------------------------
 template <int BM_, int BN_, int WR_, int WC_, int NBUF_>
 struct PipeCfg {
@@ -252,6 +288,24 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
     // (tiles whose accumulators leave no room for them load them then)
     constexpr bool kLate = TM * TN >= 32;
     if (!kLate) fetch();
+    // The residual's values: for small tiles loaded now, for others before or among the
+    // stores, kAhead row tiles ahead.  (Rows past R and columns past Cout are not loaded.)
+    constexpr bool kEarly = DT == 1 && TM * TN <= 8;
+    constexpr int kAhead = kEarly ? TM : DT == 1 ? 4 : 2;
+    Raw8<DT> res[kAhead][TN / 2];
+    auto load_res = [&](int i, int lane_e) {
+      const int row = m0 + wm * WROWS + i * 16 + (lane_e & 15);
+#pragma unroll
+      for (int p = 0; p < TN / 2; ++p) {
+        const int n = n0 + wn * WCOLS + p * 32 + (lane_e >> 4) * 8;
+        if (row < R && n + 8 <= Cout) res[i % kAhead][p].load(a.residual, (size_t)row * Cout + n);
+      }
+    };
+    if (kEarly && a.residual) {
+      const int lane_e = fresh(lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) load_res(i, lane_e);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -277,8 +331,15 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
     // lane (g, t) of MFMA tiles (i, 2p) and (i, 2p + 1): eight columns of row t.  Row
     // tiles outermost: the two halves of a 128-byte line are stored together.
     const int lane_e = fresh(lane), te = lane_e & 15, ge = lane_e >> 4;
+    if (!kEarly && a.residual) {
+#pragma unroll
+      for (int i = 0; i < kAhead - 1; ++i) load_res(i, lane_e);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
+      // (row tile by row tile, or their addresses and loads would fill the registers)
+      if (!kEarly) __builtin_amdgcn_sched_barrier(0);
+      if (!kEarly && a.residual && i + kAhead - 1 < TM) load_res(i + kAhead - 1, lane_e);
       const int r = wm * WROWS + i * 16 + te, row = m0 + r;
       const float sar = vec[r];
 #pragma unroll
@@ -288,17 +349,12 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
           y[v] = fmaf((float)acc[i][2 * p + (v >> 2)][v & 3], sar * vec[BM + c + v], vec[BM + BN + c + v]);
-          if (ACT_OUT) y[v] = gelu_f32(y[v]);
+          if (ACT_OUT) y[v] = gelu_q8(y[v]);
         }
         if (row >= R || n >= Cout) continue;
         const size_t o = (size_t)row * Cout + n;
         if (n + 8 <= Cout) {
-          if (a.residual) {
-            float f[8];
-            load8<DT>(a.residual, o, f);
-#pragma unroll
-            for (int v = 0; v < 8; ++v) y[v] += f[v];
-          }
+          if (a.residual) res[i % kAhead][p].add_to(y);
           store8<DT>(a.out, o, y);
         } else {
 #pragma unroll
@@ -309,6 +365,12 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
             }
         }
       }
+    }
+    // (the next tile's first operands again: kept across the epilogue they would not leave
+    // it enough registers)
+    if (kLate) {
+#pragma unroll
+      for (int i = 0; i < TM + TN; ++i) read(0, buf * G::kStage + rd_a, buf * G::kStage + rd_b, i);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives its workgroup
@@ -363,7 +425,7 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
 #pragma unroll
   for (int k = 0; k < NW; ++k) s += part[k][tid];
   float y = fmaf((float)s, a.sa[row] * a.sw[n], a.bias ? load1<DT>(a.bias, n) : 0.f);
-  if (ACT_OUT) y = gelu_f32(y);
+  if (ACT_OUT) y = gelu_q8(y);
   const size_t at = (size_t)row * Cout + n;
   if (a.residual) y += load1<DT>(a.residual, at);
   store1<DT>(a.out, at, y);
@@ -375,17 +437,21 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
   return launch_with_smem(fn, dim3((a.Cout + 15) / 16, (a.R + 15) / 16), dim3(512), 0, stream, nullptr, nullptr, a);
 }
 
-// The tile whose last round ends first.  A round of 128 x 128 tiles, two to a CU, is
-// taken for 2.5 units, of 256 x 256, one to a CU, for 4, and of 64 x 64, two to a CU,
-// for 1 (half of each where one to a CU suffices): what each took of a product of
-// 8192 x 8192 x 8192 (527, 420 and 874 us).  Measured, us:
-//                    256 x 256   128 x 128   64 x 64
-//   16384x4096x4096    237 *        284         447
-//   12544x640x2560      28.4 *       30.6        51
-//   12544x2560x640      32.7         25.4 *      38
-//   2048x2048x2048      25.0         14.5 *      17.3
-//   1000x8000x1000      77.5         45.6        19.8 *
-// The kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
+// The tile for a layer, by what each takes for one round of all CUs, in us: so much for
+// every 128 bytes of K, for the rest of a tile, and for a GELU or a residual in its
+// epilogue.  A CU's tiles share it, so part of a round takes its part of the time, but
+// no less than the latency of one tile.  Fitted to (us, plain / GELU / residual):
+//                    256 x 256         128 x 128          64 x 64, 4 a CU    64 x 64, 2 a CU
+//   8192x8192x8192   420               528                853                874
+//   16384x4096x4096  237               284                434                447
+//   12544x640x2560   32.5/46.0/57.9 *  32.9/42.7/50.4 *   40.8/52.7/60.7     50.0/59.2/65.3
+//   12544x2560x640   37.1/42.4/41.1    26.4/28.3/28.4 *   36.4/37.3/39.5     36.5/39.5/38.8
+//   25088x192x768    21.0/31.4/36.9    14.9/19.8/19.1 *   17.0/21.6/20.2     20.5/25.8/24.1
+//   100352x80x320    29.2/51.0/65.2    20.2/31.9/37.1     20.5/29.8/37.2 *   26.7/35.6/44.8
+//   6272x192x768     11.6/17.0/17.0     8.0/ 9.7/ 9.7      7.4/ 8.4/ 8.8 *    8.3/ 9.7/ 9.9
+//   1000x8000x1000   77.5              45.6               31.1               19.8 *
+// (* the one taken: at 12544x640x2560 the larger tile without GELU or residual).  The
+// kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
 // 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
 // 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
 // 3.4 (3.9); at 196x2560x640 8.0 (7.4).
@@ -393,14 +459,21 @@ template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
   const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);
   if (a.R <= 16 || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20)) return launch_rows_q8<DT>(a, stream);
-  auto rounds = [&](int bm, int bn, int per_cu) {
-    const long t = ((long)(a.R + bm - 1) / bm) * ((a.Cout + bn - 1) / bn), slots = 256 * per_cu;
-    return t <= 256 ? 1.0 / per_cu : (double)((t + slots - 1) / slots);
+  const double n = (a.Kp + 127) / 128, gelu = a.act_out ? 1 : 0, res = a.residual ? 1 : 0;
+  auto cost = [&](int edge, int per_cu, double round, double tile) {
+    const long t = ((long)(a.R + edge - 1) / edge) * ((a.Cout + edge - 1) / edge);
+    return std::max((double)((t + 255) / 256) / per_cu * round, tile);
   };
-  const double c256 = 4 * rounds(256, 256, 1), c128 = 2.5 * rounds(128, 128, 2), c64 = rounds(64, 64, 2);
-  if (c256 <= c128 && c256 <= c64) return launch_pipe_q8<PipeCfg<256, 256, 2, 4, 2>, DT>(a, stream);
-  if (c128 <= c64) return launch_pipe_q8<PipeCfg<128, 128, 2, 4, 2>, DT>(a, stream);
-  return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 4>, DT>(a, stream);
+  const double c[4] = {cost(256, 1, 1.5 * n + 7.5 + 6 * gelu + 10 * res, 0),
+                       cost(128, 2, 1.0 * n + 2.5 + 2.1 * gelu + 3 * res, 0.7 * n + 2),
+                       cost(64, 4, 0.78 * n + 1.2 + 1.2 * gelu + 1.7 * res, 0.45 * n + 1.5),
+                       cost(64, 2, 0.37 * n + 1.15 + 0.6 * gelu + 0.95 * res, 0.27 * n + 1.5)};
+  switch (std::min_element(c, c + 4) - c) {
+    case 0: return launch_pipe_q8<PipeCfg<256, 256, 2, 4, 2>, DT>(a, stream);
+    case 1: return launch_pipe_q8<PipeCfg<128, 128, 2, 4, 2>, DT>(a, stream);
+    case 2: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 2>, DT>(a, stream);
+    default: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 4>, DT>(a, stream);
+  }
 }
 
 hipError_t launch_gemm_q8(const GemmQ8Args& a, int dt_bf16, hipStream_t stream) {

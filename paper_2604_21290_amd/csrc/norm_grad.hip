@@ -144,10 +144,7 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         float s = half ? db[v][j] : dg[v][j];
-        if (LPR == 16) {  // the wave's four groups
-          s += __shfl_xor(s, 16);
-          s += __shfl_xor(s, 32);
-        }
+        if (LPR == 16) s = sum_over_rows16(s);  // the wave's four groups
         if ((threadIdx.x & 63) < LPR) sums[wave * COLS + (lane + v * LPR) * E + j] = s;
       }
     __syncthreads();
@@ -163,22 +160,27 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-// out[c] = sum over the G rows of part [G, cols]: 32 columns a workgroup, 32 rows at
-// a time, in the same order always.
+// out[c] = sum over the G rows of part [G, cols]: COLS columns a workgroup, 1024 / COLS
+// rows at a time, in the same order always.
+template <int COLS>
 __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, int G, int cols,
                                                              float* dgamma, float* dbeta) {
-  __shared__ float sums[32][33];
-  const int t = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + t;
+  constexpr int ROWS = 1024 / COLS;
+  __shared__ float sums[ROWS][COLS + 1];
+  const int t = threadIdx.x % COLS, w = threadIdx.x / COLS;
+  const int c = blockIdx.x * COLS + t;
   float s = 0.f;
   if (c < 2 * cols)
 #pragma unroll 8
-    for (int g = w; g < G; g += 32) s += part[(size_t)g * 2 * cols + c];
+    for (int g = w; g < G; g += ROWS) s += part[(size_t)g * 2 * cols + c];
   sums[w][t] = s;
-  __syncthreads();
-  if (w == 0 && c < 2 * cols) {
 #pragma unroll
-    for (int k = 1; k < 32; ++k) s += sums[k][t];
+  for (int h = ROWS / 2; h >= 1; h /= 2) {
+    __syncthreads();
+    if (w < h) sums[w][t] += sums[w + h][t];
+  }
+  if (w == 0 && c < 2 * cols) {
+    s = sums[0][t];
     if (c < cols) {
       if (dgamma) dgamma[c] = s;
     } else if (dbeta) dbeta[c - cols] = s;
@@ -186,14 +188,14 @@ __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, 
 }
 
 // Few rows, in one launch and without a workspace: the first `row_wgs` workgroups take
-// rows, 256 / LPR each, the others 16 chunks of columns each, over all rows: the
-// columns' sums need no average of a row, and reading a small input twice is cheap.
+// rows, 256 / LPR each, the others 16 chunks of columns each, over all rows: the columns'
+// sums need no average of a row, and reading a small input twice is cheap.
 template <int DT, int LPR, int VPL>
 __global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int row_wgs) {
   using T = Chunk<DT>;
-  constexpr int E = T::E, GROUPS = 256 / LPR;
-  __shared__ uint32_t slots[2][4];
-  __shared__ float sums[2][16][16 * E + 1];
+  constexpr int E = T::E, NT = 256, GROUPS = NT / LPR, RG = NT / 16;
+  __shared__ uint32_t slots[2][NT / 64];
+  __shared__ float sums[RG][16 * E + 1];
   const int C = a.C, n = (C + E - 1) / E;
   if ((int)blockIdx.x < row_wgs) {
     const int lane = threadIdx.x & (LPR - 1);
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int 
   float dg[E] = {}, db[E] = {};
   if (c < n) {
 #pragma unroll 4
-    for (int r = grp; r < a.R; r += 16) {
+    for (int r = grp; r < a.R; r += RG) {
       float f[E], d[E];
       T::unpack(T::raw(static_cast<const char*>(a.x) + (size_t)r * a.ldx * T::kSize, i), f);
       T::unpack(T::raw(static_cast<const char*>(a.dy) + (size_t)r * a.lddy * T::kSize, i), d);
@@ -259,22 +261,22 @@ __global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int 
       }
     }
   }
+  for (int half = 0; half < 2; ++half) {
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    sums[0][grp][lane * E + j] = dg[j];
-    sums[1][grp][lane * E + j] = db[j];
-  }
-  __syncthreads();
-  for (int k = threadIdx.x; k < 2 * 16 * E; k += 256) {
-    const int half = k / (16 * E), at = k % (16 * E);
-    const int ch = ((int)blockIdx.x - row_wgs) * 16 + at / E, col = min(ch * E, C - E) + at % E;
-    // (the last chunk's first columns are the one before's)
-    if (ch >= n || col < ch * E) continue;
-    float s = 0.f;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) s += sums[half][q][at];
+    for (int j = 0; j < E; ++j) sums[grp][lane * E + j] = half ? db[j] : dg[j];
+    __syncthreads();
     float* out = half ? a.dbeta : a.dgamma;
-    if (out) out[col] = s;
+    if (const int at = threadIdx.x; at < 16 * E && out) {
+      const int ch = ((int)blockIdx.x - row_wgs) * 16 + at / E, col = min(ch * E, C - E) + at % E;
+      // (the last chunk's first columns are the one before's)
+      if (ch < n && col >= ch * E) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int q = 0; q < RG; ++q) s += sums[q][at];
+        out[col] = s;
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -329,8 +331,13 @@ struct Plan {
   int threads, groups, grid;  // grid 0: the one launch for few rows
 };
 
-// 16 column workgroups' worth of rows: a lane of theirs adds at most 64 rows
-constexpr int kFewRows = 1024;
+// Up to so many rows take one launch.  Its column workgroups add R / 16 rows a lane, so
+// its time grows with R; the two kernels' sums grow with C.  us, one launch (two):
+//   bf16 R       C = 80      192          640          2560
+//   196          4.0 (6.5)   4.1 (8.3)    4.2 (7.0)    4.3 (11.4)
+//   392          5.4 (6.6)   5.5 (8.4)    5.7 (7.1)    7.0 (12.2)
+//   784          8.5 (6.7)   8.5 (8.4)    8.9 (7.4)   12.6 (15.9)
+constexpr int kFewRows = 512, kFewWide = 1024;
 
 template <int DT>
 Plan plan(int R, int C) {
@@ -338,10 +345,12 @@ Plan plan(int R, int C) {
   const int n = (C + E - 1) / E;
   auto make = [&](const void* fn, int threads, int lpr, int most) {
     const int groups = threads / lpr;
-    return Plan{fn, threads, groups, (int)std::min<long long>(((long long)R + groups - 1) / groups, most)};
+    // (a workgroup that takes few rows costs as much by its sums: 256 of them, or eight rows each)
+    const int g = most > 256 ? std::min(std::max(R / 8, 256), most) : most;
+    return Plan{fn, threads, groups, (int)std::min<long long>(((long long)R + groups - 1) / groups, g)};
   };
   if (C < E || n > 2048) return Plan{nullptr, 256, 1, std::min(R, 256)};
-  if (R <= kFewRows && n <= 1024) {
+  if (R <= (n > 128 ? kFewWide : kFewRows) && n <= 1024) {
     if (n <= 16) return Plan{(const void*)&norm_grad_few_kernel<DT, 16, 1>, 256, 16, 0};
     if (n <= 64) return Plan{(const void*)&norm_grad_few_kernel<DT, 64, 1>, 256, 4, 0};
     if (n <= 256) return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 1>, 256, 1, 0};
@@ -385,7 +394,11 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
                           dim3(256), argv, 0, stream);
   }
   if (e != hipSuccess || !sums) return e;
-  norm_grad_sum_kernel<<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
+  // (few columns are spread over more workgroups)
+  if (2 * a.C <= 2048)
+    norm_grad_sum_kernel<8><<<(2 * a.C + 7) / 8, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
+  else
+    norm_grad_sum_kernel<32><<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 

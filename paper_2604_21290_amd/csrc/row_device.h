@@ -92,6 +92,17 @@ __device__ __forceinline__ uint32_t reduce16(uint32_t v) {
   return Op::of(v, dpp_mov<0x140>(v));  // row mirror: the other eight
 }
 
+// Sum over the four rows of 16 lanes of a wave, lane by lane (gfx950 swaps rows of two
+// registers: with both the same, each ends with one of each pair's rows twice).
+__device__ __forceinline__ float sum_over_rows16(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const uint32_t w = __float_as_uint(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 template <class Op, int LPR>
 __device__ __forceinline__ uint32_t reduce_row(uint32_t v, uint32_t* slot) {
   v = reduce16<Op>(v);

@@ -6,10 +6,10 @@
 // loses nothing to cancellation) and its top is found; then it is written once.
 // Memory bounds it: us (and TB/s of what it has to read and write; a copy of 1 GiB
 // reaches 5.3) in bf16, norm, 8 bits, norm to 8 bits:
-//   32768 x 2560   69.8 (4.8)   49.7 (5.1)   77.2 (3.3)
-//   100352 x 320   35.1 (3.7)   19.7 (4.9)   32.9 (2.9)
-//   100352 x 80    10.1 (3.2)    8.1 (3.0)   11.8 (2.1)
-//   6272 x 192      4.1 (1.2)    3.2 (1.1)    4.4 (0.8)
+//   32768 x 2560   63.5 (5.3)   48.4 (5.2)   62.9 (4.0)
+//   100352 x 320   29.6 (4.3)   18.4 (5.2)   26.4 (3.6)
+//   100352 x 80     9.4 (3.4)    7.9 (3.1)   11.0 (2.2)
+//   6272 x 192      3.9 (1.2)    3.2 (1.1)    4.2 (0.9)
 // Small inputs take a launch and one trip to memory, about 3 us; the norm to 8 bits
 // has twice the arithmetic of the norm, which then shows.
 #include "gl_kernels.h"
@@ -30,14 +30,17 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   const int C = a.C, n = (C + E - 1) / E;
   const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
+  // lanes past the row's last chunk hold it once more: their values count in no sum, and
+  // are not stored
+  int at[VPL];  // the chunk's place in its row
+#pragma unroll
+  for (int v = 0; v < VPL; ++v) at[v] = min(min(lane + v * LPR, n - 1) * E, C - E);
+  auto on = [&](int v) { return lane + v * LPR < n; };
   uint4 raw[VPL];
   auto load = [&](long long r) {
     const char* x = static_cast<const char*>(a.x) + min(r, (long long)a.R - 1) * a.ldx * T::kSize;
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR;
-      if (c < n) raw[v] = T::raw(x, min(c * E, C - E));
-    }
+    for (int v = 0; v < VPL; ++v) raw[v] = T::raw(x, at[v]);
   };
   const long long step = (long long)gridDim.x * GROUPS;
   long long r0 = (long long)blockIdx.x * GROUPS;
@@ -46,11 +49,10 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   if (MODE != kQ8) {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR, i = min(c * E, C - E);
-      if (c < n) {
-        if (a.gamma) gamma[v] = T::raw(a.gamma, i);
-        if (a.beta) beta[v] = T::raw(a.beta, i);
-      }
+      gamma[v] = T::ones();
+      beta[v] = make_uint4(0, 0, 0, 0);
+      if (a.gamma) gamma[v] = T::raw(a.gamma, at[v]);
+      if (a.beta) beta[v] = T::raw(a.beta, at[v]);
     }
   }
   int turn = 0;
@@ -60,8 +62,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
     const size_t row = r0 + grp;
     float f[VPL][E];
 #pragma unroll
-    for (int v = 0; v < VPL; ++v)
-      if (lane + v * LPR < n) T::unpack(raw[v], f[v]);
+    for (int v = 0; v < VPL; ++v) T::unpack(raw[v], f[v]);
     if (r0 + step < a.R) load(r0 + step + grp);
     if (MODE != kQ8) {
       // sum over the row of what `term` makes of each value
@@ -69,16 +70,16 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
         float s = 0.f;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-          const int c = lane + v * LPR;
-          if (c >= n) continue;
+          float p = 0.f;
           if (ragged) {
-            const int skip = max(c * E + E - C, 0);
+            const int skip = (lane + v * LPR) * E - at[v];
 #pragma unroll
-            for (int j = 0; j < E; ++j) s = j >= skip ? term(s, f[v][j]) : s;
+            for (int j = 0; j < E; ++j) p = j >= skip ? term(p, f[v][j]) : p;
           } else {
 #pragma unroll
-            for (int j = 0; j < E; ++j) s = term(s, f[v][j]);
+            for (int j = 0; j < E; ++j) p = term(p, f[v][j]);
           }
+          s += on(v) ? p : 0.f;
         }
         return sum_row<LPR>(s, slot);
       };
@@ -91,17 +92,14 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
       const float rstd = __builtin_amdgcn_rsqf(fmaf(sq, a.inv_c, a.eps));
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        const int c = lane + v * LPR, i = min(c * E, C - E);
-        if (c >= n) continue;
         float w[E], b[E];
         keep_packed(gamma[v]);
         keep_packed(beta[v]);
-        if (a.gamma) T::unpack(gamma[v], w);
-        if (a.beta) T::unpack(beta[v], b);
+        T::unpack(gamma[v], w);
+        T::unpack(beta[v], b);
 #pragma unroll
-        for (int j = 0; j < E; ++j)
-          f[v][j] = fmaf(f[v][j] * rstd, a.gamma ? w[j] : 1.f, a.beta ? b[j] : 0.f);
-        if (MODE == kNorm && mine) T::store(a.out, row * C + i, f[v]);
+        for (int j = 0; j < E; ++j) f[v][j] = fmaf(f[v][j] * rstd, w[j], b[j]);
+        if (MODE == kNorm && mine && on(v)) T::store(a.out, row * C + at[v], f[v]);
       }
       if (MODE == kNorm && mine && lane == 0) {
         if (a.mean) a.mean[row] = mean;
@@ -112,17 +110,14 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
       uint32_t top = 0;
 #pragma unroll
       for (int v = 0; v < VPL; ++v)
-        if (lane + v * LPR < n)
 #pragma unroll
-          for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
+        for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
       const RowQ8 q(max_row<LPR>(top, slots[turn][2]));
       if (mine) {
         int8_t* d = a.q + row * a.Kp;
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) {
-          const int c = lane + v * LPR;
-          if (c < n) store_q8<E>(d + min(c * E, C - E), q, f[v]);
-        }
+        for (int v = 0; v < VPL; ++v)
+          if (on(v)) store_q8<E>(d + at[v], q, f[v]);
         if (lane < a.Kp - C) d[C + lane] = 0;  // fewer than 16
         if (lane == 0) a.scale[row] = q.scale;
       }

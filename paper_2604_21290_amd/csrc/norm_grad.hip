@@ -6,8 +6,8 @@
 // sums of its own over all rows that it meets.  A workgroup then adds its lanes'
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
 // Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
-// 108 (4.7), 100352 x 320 42-50 (3.9-4.6), 100352 x 80 16.5 (2.9, of which the second
-// kernel takes 3).  Few rows take one launch (196 x 192 3.5 us, 7.4 in two kernels).
+// 111 (4.5), 100352 x 320 40 (4.8), 100352 x 80 15.4 (3.1, of which the second kernel and
+// the gap before it take 4), 8193 x 1001 16.8 (2.9).  Few rows take one launch.
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"
@@ -17,7 +17,8 @@ namespace gl {
 // LPR lanes hold a row, VPL chunks each; NT threads a workgroup.  A row's loads are
 // under way while the one before it is worked on.
 template <int DT, int LPR, int VPL, int NT>
-__global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(VPL <= 2 ? 4 : 2)))
+void norm_grad_kernel(NormGradArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, GROUPS = NT / LPR, NW = NT / 64;
   constexpr int COLS = LPR * VPL * E;  // columns a group covers
@@ -27,6 +28,12 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
   const int C = a.C, n = (C + E - 1) / E;
   const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
+  // lanes past the row's last chunk hold it once more: their values count in no sum, and
+  // are not stored
+  int at[VPL];  // the chunk's place in its row
+#pragma unroll
+  for (int v = 0; v < VPL; ++v) at[v] = min(min(lane + v * LPR, n - 1) * E, C - E);
+  auto on = [&](int v) { return lane + v * LPR < n; };
   uint4 raw_x[VPL], raw_d[VPL];
   float mean, rstd;
   auto load = [&](long long r) {
@@ -35,11 +42,8 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
     const char* dy = static_cast<const char*>(a.dy) + row * a.lddy * T::kSize;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR;
-      if (c < n) {
-        raw_x[v] = T::raw(x, min(c * E, C - E));
-        raw_d[v] = T::raw(dy, min(c * E, C - E));
-      }
+      raw_x[v] = T::raw(x, at[v]);
+      raw_d[v] = T::raw(dy, at[v]);
     }
     mean = a.mean[row];
     rstd = a.rstd[row];
@@ -54,8 +58,8 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
   for (int v = 0; v < VPL; ++v) {
 #pragma unroll
     for (int j = 0; j < E; ++j) dg[v][j] = db[v][j] = 0.f;
-    const int c = lane + v * LPR;
-    if (a.gamma && c < n) raw_w[v] = T::raw(a.gamma, min(c * E, C - E));
+    raw_w[v] = T::ones();
+    if (a.gamma) raw_w[v] = T::raw(a.gamma, at[v]);
   }
   int turn = 0;
   // every group of a workgroup makes the same number of turns
@@ -65,60 +69,59 @@ __global__ __launch_bounds__(NT) void norm_grad_kernel(NormGradArgs a) {
     float f[VPL][E], d[VPL][E];
     const float mu = mean, rs = rstd;
 #pragma unroll
-    for (int v = 0; v < VPL; ++v)
-      if (lane + v * LPR < n) {
-        T::unpack(raw_x[v], f[v]);
-        T::unpack(raw_d[v], d[v]);
-      }
+    for (int v = 0; v < VPL; ++v) {
+      T::unpack(raw_x[v], f[v]);
+      T::unpack(raw_d[v], d[v]);
+    }
     if (r0 + step < a.R) load(r0 + step + grp);
+    if (!mine)  // rows past the last count for nothing
+#pragma unroll
+      for (int v = 0; v < VPL; ++v)
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[v][j] = 0.f;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      const int c = lane + v * LPR;
-      if (c >= n) continue;
-      float w[E];
+      float w[E], p0 = 0.f, p1 = 0.f;
       keep_packed(raw_w[v]);
-      if (a.gamma) T::unpack(raw_w[v], w);
-      if (!mine)
-#pragma unroll
-        for (int j = 0; j < E; ++j) d[v][j] = 0.f;  // rows past the last count for nothing
+      T::unpack(raw_w[v], w);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         f[v][j] = (f[v][j] - mu) * rs;
         dg[v][j] = fmaf(d[v][j], f[v][j], dg[v][j]);
         db[v][j] += d[v][j];
-        if (a.gamma) d[v][j] *= w[j];
+        d[v][j] *= w[j];
       }
       if (ragged) {
-        const int skip = max(c * E + E - C, 0);
+        const int skip = (lane + v * LPR) * E - at[v];
 #pragma unroll
         for (int j = 0; j < E; ++j) {
           const float h = j >= skip ? d[v][j] : 0.f;
-          s0 += h;
-          s1 = fmaf(h, f[v][j], s1);
+          p0 += h;
+          p1 = fmaf(h, f[v][j], p1);
         }
       } else {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-          s0 += d[v][j];
-          s1 = fmaf(d[v][j], f[v][j], s1);
+          p0 += d[v][j];
+          p1 = fmaf(d[v][j], f[v][j], p1);
         }
       }
+      s0 += on(v) ? p0 : 0.f;
+      s1 += on(v) ? p1 : 0.f;
     }
     // two turns' words never meet: a wave is at most one barrier ahead
     s0 = sum_row<LPR>(s0, slots[turn][0]) * a.inv_c;
     s1 = sum_row<LPR>(s1, slots[turn][1]) * a.inv_c;
     if (a.dx && mine)
 #pragma unroll
-      for (int v = 0; v < VPL; ++v) {
-        const int c = lane + v * LPR;
-        if (c < n) {
+      for (int v = 0; v < VPL; ++v)
+        if (on(v)) {
           float y[E];
 #pragma unroll
           for (int j = 0; j < E; ++j) y[j] = (d[v][j] - fmaf(f[v][j], s1, s0)) * rs;
-          T::store(a.dx, row * C + min(c * E, C - E), y);
+          T::store(a.dx, row * C + at[v], y);
         }
-      }
   }
   if (!a.part) return;
 
@@ -363,9 +366,10 @@ Plan plan(int R, int C) {
   if (n <= 128) return make((const void*)&norm_grad_kernel<DT, 64, 2, 512>, 512, 64, 512);
   if (n <= 192) return make((const void*)&norm_grad_kernel<DT, 64, 3, 256>, 256, 64, 512);
   if (n <= 256) return make((const void*)&norm_grad_kernel<DT, 64, 4, 256>, 256, 64, 512);
-  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 1024);
+  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 768);
   if (n <= 768) return make((const void*)&norm_grad_kernel<DT, 256, 3, 256>, 256, 256, 512);
-  if (n <= 1024) return make((const void*)&norm_grad_kernel<DT, 256, 4, 256>, 256, 256, 512);
+  // (10000 x 8192 bf16: 101 us, 114 with four chunks a lane of 256)
+  if (n <= 1024) return make((const void*)&norm_grad_kernel<DT, 1024, 1, 1024>, 1024, 1024, 256);
   return make((const void*)&norm_grad_kernel<DT, 512, 4, 512>, 512, 512, 256);
 }
 

@@ -27,6 +27,9 @@ struct Chunk<1> {
   __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
     return load16_any(static_cast<const uint16_t*>(p) + i);
   }
+  __device__ __forceinline__ static uint4 ones() {
+    return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  }
   __device__ __forceinline__ static void unpack(const uint4& v, float* f) { unpack_bf16x8(v, f); }
   __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
     store16_any(static_cast<uint16_t*>(p) + i, pack_bf16x8(f));
@@ -45,6 +48,9 @@ struct Chunk<0> {
   static constexpr size_t kSize = 4;
   __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
     return __builtin_bit_cast(uint4, *reinterpret_cast<const u32x4_any4*>(static_cast<const float*>(p) + i));
+  }
+  __device__ __forceinline__ static uint4 ones() {
+    return make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u);
   }
   __device__ __forceinline__ static void unpack(const uint4& v, float* f) {
     f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y);

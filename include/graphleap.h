@@ -449,8 +449,9 @@ gl_status gl_vig_stack(gl_lookahead_t h, const void* x0, int B, int H, int W, in
  *   gamma, beta [C] (dt) or NULL for ones and zeros; eps >= 0.
  *   out [R, C] (dt), contiguous.  mean, rstd [R] fp32 or NULL: what
  *   gl_layer_norm_backward needs.  Outputs must not overlap x, gamma or beta.
- * A row with a NaN or an infinity is NaN.
- * Limits: R, C >= 1; R * C < 2^40.
+ * A row with a NaN or an infinity is NaN.  Squares are fp32: deviations past 1e19
+ * overflow.
+ * Limits: 1 <= R <= 2^30, 1 <= C <= 2^29, R * C <= 2^40.
  * Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype), GL_ERR_BAD_SHAPE (sizes,
  * ldx < C, eps negative or not finite), GL_ERR_ALIGNMENT, GL_ERR_ALIAS, GL_ERR_HIP.
  * -------------------------------------------------------------------------*/
@@ -512,7 +513,7 @@ gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const voi
  *   the weights likewise.  bias [Cout] (dt) or NULL; residual [R, Cout] (dt) or
  *   NULL, and may be `out` itself; out [R, Cout] (dt), must not overlap the
  *   other arguments.  Any whole number of -128 .. 127 is taken as a value.
- * Limits: R, Cout >= 1; 1 <= K <= GL_MAX_Q8_K.
+ * Limits: 1 <= R, Cout <= 2^30; 1 <= K <= GL_MAX_Q8_K; R * Cout <= 2^40.
  * -------------------------------------------------------------------------*/
 gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const int8_t* Wq,
                        const float* w_scale, const void* bias, int Cout, gl_act act_out,

@@ -1213,7 +1213,8 @@ size_t span(int R, int C, long long ld, size_t es) { return ((size_t)(R - 1) * l
 
 gl_status check_rows(const char* who, const void* x, int R, int C, long long ld, gl_dtype dt) {
   if (!dtype_ok(dt)) return fail(GL_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, (int)dt);
-  if (R < 1 || C < 1 || !size_ok(R, 1, C))
+  // (the kernels count columns, and twice as many sums, in 32 bits)
+  if (R < 1 || C < 1 || R > 1 << 30 || C > 1 << 29 || !size_ok(R, 1, C))
     return fail(GL_ERR_BAD_SHAPE, "%s: bad shape R=%d C=%d", who, R, C);
   if (R > 1 && (ld < C || ld > (1LL << 40) / R))
     return fail(GL_ERR_BAD_SHAPE, "%s: rows of %d channels %lld elements apart", who, C, ld);
@@ -1295,7 +1296,7 @@ gl_status gl_layer_norm(const void* x, int R, int C, long long ldx, const void* 
 }
 
 size_t gl_layer_norm_backward_workspace_bytes(int R, int C, gl_dtype dt) {
-  if (!dtype_ok(dt) || R < 1 || C < 1 || !size_ok(R, 1, C)) return 0;
+  if (!dtype_ok(dt) || R < 1 || C < 1 || R > 1 << 30 || C > 1 << 29 || !size_ok(R, 1, C)) return 0;
   return gl::norm_grad_ws_bytes(R, C, dt == GL_BF16);
 }
 
@@ -1384,7 +1385,7 @@ gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const 
     return fail(GL_ERR_UNSUPPORTED, "%s: unknown activation", who);
   gl_status s = check_q8_rows(who, q, scale, K);
   if (s != GL_OK || (s = check_q8_rows(who, Wq, w_scale, K)) != GL_OK) return s;
-  if (R < 1 || Cout < 1 || !size_ok(R, 1, K) || !size_ok(R, 1, Cout) || !size_ok(Cout, 1, K))
+  if (R < 1 || Cout < 1 || R > 1 << 30 || Cout > 1 << 30 || !size_ok(R, 1, K) || !size_ok(R, 1, Cout) || !size_ok(Cout, 1, K))
     return fail(GL_ERR_BAD_SHAPE, "%s: bad shape R=%d K=%d Cout=%d", who, R, K, Cout);
   const size_t es = esize(dt), ob = (size_t)R * Cout * es, kp = gl::q8_row_bytes(K);
   if (!aligned(out, es) || (bias && !aligned(bias, es)) || (residual && !aligned(residual, es)))

@@ -13,6 +13,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "graphleap.h"
@@ -91,13 +92,13 @@ at::Tensor empty(at::IntArrayRef shape, const at::Tensor& like, at::ScalarType t
   return at::empty(shape, like.options().dtype(type).requires_grad(false));
 }
 
-// Runs f; a C++ exception becomes a Python one.
+// Runs f; a C++ exception becomes torch's Python one.
 template <class F>
 PyObject* guarded(F f) {
   try {
     return f();
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
     return nullptr;
   }
 }

@@ -21,7 +21,8 @@ __device__ __forceinline__ i32x4 mfma_i8(const uint4& a, const uint4& b, i32x4 a
 
 // GELU x Phi(x), the error function by Abramowitz and Stegun 7.1.26 as in gelu_f32, with
 // its constants folded: Phi(-|x|) = poly(t) e^(-x^2 / 2), t = 1 / (1 + p |x| / sqrt 2),
-// and x Phi(x) = max(x, 0) - |x| Phi(-|x|).  13 instructions for 16.
+// and x Phi(x) = max(x, 0) - |x| Phi(-|x|).  14 instructions for 16; its limits at the
+// infinities.
 __device__ __forceinline__ float gelu_q8(float x) {
   const float a = fabsf(x);
   const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, a, 1.f));
@@ -31,7 +32,7 @@ __device__ __forceinline__ float gelu_q8(float x) {
   q = fmaf(t, q, 0.127414796f);
   const float y = x * 0.84932180028801907f;  // sqrt(log2(e) / 2)
   const float e = __builtin_amdgcn_exp2f(-y * y);
-  return fmaf(-a, t * q * e, fmaxf(x, 0.f));
+  return fmaf(-fminf(a, 3.4e38f), t * q * e, fmaxf(x, 0.f));
 }
 
 typedef uint32_t u32x4_w __attribute__((ext_vector_type(4), aligned(4), may_alias));
@@ -108,7 +109,8 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
 // What bounds it: at 8192 x 8192 x 8192 (420-430 us, 2.6 POP/s; the library's int8
 // product 440) the matrix cores are busy 66 % of the cycles, at a clock that falls to
 // 1.7-1.8 GHz on random data; with all loads from L2's hottest lines 397 us, so the trip
-// to memory costs 8 %.  Tried and slower there: MFMA 32x32x32 (471 us), stages of 64
+// to memory costs 8 %.  Its loads alone take 360 us, its products alone 346: each stage's
+// loads take about as long as its products, and LDS holds one stage ahead.  Tried and slower there: MFMA 32x32x32 (471 us), stages of 64
 // bytes in four buffers (446), 256 x 128 tiles in three buffers (478), four waves of
 // 128 x 128 (886: operands move between the register files).
 // ---------------------------------------------------------------------------
@@ -185,8 +187,8 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   const int slot_a = ((lane & 7) ^ lr) * 16;
   const int slot_w = ((lane & 7) ^ ((lr & 3) | ((w & 1) << 2))) * 16;
   const int lim_a = rowb - 16 - slot_a, lim_w = rowb - 16 - slot_w;  // the row's last slot
-  const char *base_a, *base_w;     // of the tile that is being loaded
-  uint32_t src_a[NA], src_w[NB];   // at most 256 rows of 2^17 bytes
+  const char *base_a, *base_w;    // of the tile that is being loaded
+  uint32_t src_a[NA], src_w[NB];  // at most 256 rows of 2^17 bytes
   int L_load = blockIdx.x, s_load = 0;
   auto aim = [&]() {
     int m0, n0;
@@ -230,8 +232,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   const int rd_b = (BM + wn * WCOLS + (t >> 2) * 8 + (t & 3)) * STEP + (g ^ (t & 7)) * 16;
   auto read = [&](int set, int pa, int pb, int i) {  // TM of A, then TN of W
     if (i < TM)
-      fa[set][i < TM ? i : 0] = *reinterpret_cast<const uint4*>(
-          smem + pa + i * 16 * STEP);
+      fa[set][i < TM ? i : 0] = *reinterpret_cast<const uint4*>(smem + pa + i * 16 * STEP);
     else
       fb[set][i < TM ? 0 : i - TM] = *reinterpret_cast<const uint4*>(
           smem + pb + (((i - TM) >> 1) * 32 + ((i - TM) & 1) * 4) * STEP);

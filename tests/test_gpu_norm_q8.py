@@ -322,6 +322,23 @@ def test_linear_q8_extremes_are_exact():
     assert (np.abs(_f64(out) - ref) <= E32 * np.abs(ref)).all()
 
 
+@pytest.mark.parametrize("R,Cout", [(3, 24), (1000, 1000)])
+def test_linear_q8_overflow_and_gelu_limits(R, Cout):
+    """Outputs past fp32: infinities, which the GELU takes to infinity and 0."""
+    api = _api()
+    g = np.random.default_rng(R)
+    x, W, _, _ = _layer(g, api, R, 100, Cout, torch.float32, False, False, False)
+    x.scale.fill_(3e38)
+    W.scale.fill_(1e6)
+    lin = api.linear_q8(x, W, dtype=torch.float32)
+    gelu = api.linear_q8(x, W, act_out=api.GL_ACT_GELU, dtype=torch.float32)
+    torch.cuda.synchronize()
+    ref = x.q[:, :100].double() @ W.q[:, :100].double().t()
+    inf = torch.tensor(float("inf"), device="cuda")
+    assert torch.equal(lin[ref != 0], torch.where(ref > 0, inf, -inf)[ref != 0])
+    assert torch.equal(gelu[ref != 0], torch.where(ref > 0, inf, 0 * ref.float())[ref != 0])
+
+
 def test_offsets_past_32_bits():
     api = _api()
     g = np.random.default_rng(9)

@@ -27,7 +27,8 @@ def test_layer_norm_refusals():
     assert _norm(x=None) == _norm(out=None) == "GL_ERR_NULL_PTR"
     assert _norm(dt=2) == "GL_ERR_UNSUPPORTED"
     for bad in (dict(R=0), dict(C=0), dict(R=-1), dict(ld=99), dict(ld=-100), dict(ld=1 << 40), dict(eps=-1e-9),
-                dict(eps=float("nan")), dict(eps=float("inf")), dict(R=1 << 30, C=1 << 20, ld=1 << 20)):
+                dict(eps=float("nan")), dict(eps=float("inf")), dict(R=1 << 30, C=1 << 20, ld=1 << 20),
+                dict(R=(1 << 30) + 1, C=1, ld=1), dict(R=1, C=(1 << 29) + 1, ld=(1 << 29) + 1)):
         assert _norm(**bad) == "GL_ERR_BAD_SHAPE", bad
     assert _norm(x=P(0, 1)) == _norm(out=P(3, 1)) == _norm(gamma=P(1, 1)) == "GL_ERR_ALIGNMENT"
     assert _norm(x=P(0, 2), dt=0) == _norm(mean=P(5, 2)) == "GL_ERR_ALIGNMENT"
@@ -62,6 +63,7 @@ def test_layer_norm_backward_refusals():
     assert _grad(ws=None, **many) == _grad(n=need - 1, **many) == _grad(ws=P(8, 8), **many) == "GL_ERR_WORKSPACE"
     assert api.lib().gl_layer_norm_backward_workspace_bytes(0, 100, 1) == 0
     assert api.lib().gl_layer_norm_backward_workspace_bytes(64, 100, 5) == 0
+    assert api.lib().gl_layer_norm_backward_workspace_bytes(1, (1 << 29) + 1, 1) == 0
 
 
 def _q8(x=P(0), R=64, K=100, ld=100, dt=1, q=P(1), s=P(2)):
@@ -102,7 +104,8 @@ def test_linear_q8_refusals():
     for bad in (dict(q=None), dict(s=None), dict(W=None), dict(ws=None), dict(out=None)):
         assert _lin(**bad) == "GL_ERR_NULL_PTR", bad
     assert _lin(dt=4) == _lin(act=2) == "GL_ERR_UNSUPPORTED"
-    for bad in (dict(R=0), dict(Cout=0), dict(K=0), dict(K=131072), dict(R=1 << 30, Cout=1 << 20)):
+    for bad in (dict(R=0), dict(Cout=0), dict(K=0), dict(K=131072), dict(R=1 << 30, Cout=1 << 20),
+                dict(R=(1 << 30) + 1, K=1, Cout=1), dict(R=1, K=1, Cout=(1 << 30) + 1)):
         assert _lin(**bad) == "GL_ERR_BAD_SHAPE", bad
     for bad in (dict(q=P(0, 8)), dict(W=P(2, 4)), dict(s=P(1, 2)), dict(ws=P(3, 1)), dict(out=P(5, 1)),
                 dict(bias=P(4, 1)), dict(res=P(6, 1)), dict(dt=0, out=P(5, 2))):

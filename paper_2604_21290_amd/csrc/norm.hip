@@ -6,10 +6,10 @@
 // loses nothing to cancellation) and its top is found; then it is written once.
 // Memory bounds it: us (and TB/s of what it has to read and write; a copy of 1 GiB
 // reaches 5.3) in bf16, norm, 8 bits, norm to 8 bits:
-//   32768 x 2560   63.5 (5.3)   48.4 (5.2)   62.9 (4.0)
-//   100352 x 320   29.6 (4.3)   18.4 (5.2)   26.4 (3.6)
-//   100352 x 80     9.4 (3.4)    7.9 (3.1)   11.0 (2.2)
-//   6272 x 192      3.9 (1.2)    3.2 (1.1)    4.2 (0.9)
+//   32768 x 2560   62.2 (5.4)   47.9 (5.3)   60.5 (4.2)
+//   100352 x 320   28.0 (4.6)   18.5 (5.2)   27.5 (3.5)
+//   100352 x 80     8.4 (3.8)    8.0 (3.0)   10.3 (2.3)
+//   6272 x 192      3.8 (1.3)    3.3 (1.1)    4.1 (0.9)
 // Small inputs take a launch and one trip to memory, about 3 us; the norm to 8 bits
 // has twice the arithmetic of the norm, which then shows.
 #include "gl_kernels.h"
@@ -26,7 +26,8 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, GROUPS = 256 / LPR;
   __shared__ uint32_t slots[2][3][4];
-  const int lane = threadIdx.x & (LPR - 1), grp = threadIdx.x / LPR;
+  const WaveRows<LPR> rows;
+  const int lane = threadIdx.x & (LPR - 1);
   const int C = a.C, n = (C + E - 1) / E;
   const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
@@ -37,14 +38,15 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   for (int v = 0; v < VPL; ++v) at[v] = min(min(lane + v * LPR, n - 1) * E, C - E);
   auto on = [&](int v) { return lane + v * LPR < n; };
   uint4 raw[VPL];
-  auto load = [&](long long r) {
-    const char* x = static_cast<const char*>(a.x) + min(r, (long long)a.R - 1) * a.ldx * T::kSize;
+  auto load = [&](long long r0) {
+    uint32_t off;
+    const char* x = rows.at(a.x, r0 + rows.wave, a.R, a.ldx * (long long)T::kSize, &off);
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) raw[v] = T::raw(x, at[v]);
+    for (int v = 0; v < VPL; ++v) raw[v] = T::raw_at(x, off + at[v] * (uint32_t)T::kSize);
   };
   const long long step = (long long)gridDim.x * GROUPS;
   long long r0 = (long long)blockIdx.x * GROUPS;
-  load(r0 + grp);
+  load(r0);
   uint4 gamma[VPL], beta[VPL];
   if (MODE != kQ8) {
 #pragma unroll
@@ -58,12 +60,12 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   int turn = 0;
   // every group of a workgroup makes the same number of turns
   for (; r0 < a.R; r0 += step, turn ^= 1) {
-    const bool mine = r0 + grp < a.R;
-    const size_t row = r0 + grp;
+    const long long first = r0 + rows.wave;  // the wave's
+    const bool mine = first + rows.lane < a.R;
     float f[VPL][E];
 #pragma unroll
     for (int v = 0; v < VPL; ++v) T::unpack(raw[v], f[v]);
-    if (r0 + step < a.R) load(r0 + step + grp);
+    if (r0 + step < a.R) load(r0 + step);
     if (MODE != kQ8) {
       // sum over the row of what `term` makes of each value
       auto sum = [&](auto term, uint32_t* slot) {
@@ -93,17 +95,18 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
         float w[E], b[E];
-        keep_packed(gamma[v]);
-        keep_packed(beta[v]);
+        if (VPL > 1) keep_packed(gamma[v]), keep_packed(beta[v]);
         T::unpack(gamma[v], w);
         T::unpack(beta[v], b);
 #pragma unroll
         for (int j = 0; j < E; ++j) f[v][j] = fmaf(f[v][j] * rstd, w[j], b[j]);
-        if (MODE == kNorm && mine && on(v)) T::store(a.out, row * C + at[v], f[v]);
+        if (MODE == kNorm && mine && on(v))
+          T::store_at(static_cast<char*>(a.out) + first * C * (long long)T::kSize,
+                      (rows.lane * (uint32_t)C + at[v]) * (uint32_t)T::kSize, f[v]);
       }
       if (MODE == kNorm && mine && lane == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
+        if (a.mean) (a.mean + first)[rows.lane] = mean;
+        if (a.rstd) (a.rstd + first)[rows.lane] = rstd;
       }
     }
     if (MODE != kNorm) {
@@ -114,12 +117,13 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
         for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
       const RowQ8 q(max_row<LPR>(top, slots[turn][2]));
       if (mine) {
-        int8_t* d = a.q + row * a.Kp;
+        int8_t* d = a.q + first * a.Kp;
+        const uint32_t off = rows.lane * (uint32_t)a.Kp;
 #pragma unroll
         for (int v = 0; v < VPL; ++v)
-          if (on(v)) store_q8<E>(d + at[v], q, f[v]);
-        if (lane < a.Kp - C) d[C + lane] = 0;  // fewer than 16
-        if (lane == 0) a.scale[row] = q.scale;
+          if (on(v)) store_q8<E>(d + (off + at[v]), q, f[v]);
+        if (lane < a.Kp - C) d[off + C + lane] = 0;  // fewer than 16
+        if (lane == 0) (a.scale + first)[rows.lane] = q.scale;
       }
     }
   }
@@ -187,8 +191,10 @@ hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
   };
 #define GL_ROW(LPR, VPL) go((const void*)&row_kernel<DT, MODE, LPR, VPL>, 256 / LPR)
   if (a.C < E || n > 2048) return go((const void*)&row_any_kernel<DT, MODE>, 1);
-  if (n <= 16) return GL_ROW(16, 1);
-  if (n <= 48 && a.R >= 4096) return n <= 32 ? GL_ROW(16, 2) : GL_ROW(16, 3);
+  // four rows of a wave lie within 32 bits of the first
+  const bool near = a.R == 1 || a.ldx < 1 << 27;
+  if (n <= 16 && near) return GL_ROW(16, 1);
+  if (n <= 48 && near && a.R >= 4096) return n <= 32 ? GL_ROW(16, 2) : GL_ROW(16, 3);
   if (n <= 192) return n <= 64 ? GL_ROW(64, 1) : n <= 128 ? GL_ROW(64, 2) : GL_ROW(64, 3);
   if (n <= 384) return n <= 256 ? GL_ROW(128, 2) : GL_ROW(128, 3);
   if (n <= 1024) return n <= 512 ? GL_ROW(256, 2) : n <= 768 ? GL_ROW(256, 3) : GL_ROW(256, 4);

@@ -6,8 +6,8 @@
 // sums of its own over all rows that it meets.  A workgroup then adds its lanes'
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
 // Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
-// 111 (4.5), 100352 x 320 40 (4.8), 100352 x 80 15.4 (3.1, of which the second kernel and
-// the gap before it take 4), 8193 x 1001 16.8 (2.9).  Few rows take one launch.
+// 103 (4.9), 100352 x 320 39 (4.9), 100352 x 80 15.0 (3.2, of which the second kernel and
+// the gap before it take 4), 8193 x 1001 17 (2.9).  Few rows take one launch.
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"
@@ -24,7 +24,8 @@ void norm_grad_kernel(NormGradArgs a) {
   constexpr int COLS = LPR * VPL * E;  // columns a group covers
   __shared__ uint32_t slots[2][2][NT / 64];
   __shared__ float sums[LPR > 64 ? 1 : NW * COLS];
-  const int lane = threadIdx.x & (LPR - 1), grp = threadIdx.x / LPR;
+  const WaveRows<LPR> rows;
+  const int lane = threadIdx.x & (LPR - 1);
   const int C = a.C, n = (C + E - 1) / E;
   const bool ragged = C % E != 0;  // the last chunk repeats values of the one before it
 
@@ -36,21 +37,23 @@ void norm_grad_kernel(NormGradArgs a) {
   auto on = [&](int v) { return lane + v * LPR < n; };
   uint4 raw_x[VPL], raw_d[VPL];
   float mean, rstd;
-  auto load = [&](long long r) {
-    const size_t row = min(r, (long long)a.R - 1);
-    const char* x = static_cast<const char*>(a.x) + row * a.ldx * T::kSize;
-    const char* dy = static_cast<const char*>(a.dy) + row * a.lddy * T::kSize;
+  auto load = [&](long long r0) {
+    uint32_t off_x, off_d, off;
+    const char* x = rows.at(a.x, r0 + rows.wave, a.R, a.ldx * (long long)T::kSize, &off_x);
+    const char* dy = rows.at(a.dy, r0 + rows.wave, a.R, a.lddy * (long long)T::kSize, &off_d);
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      raw_x[v] = T::raw(x, at[v]);
-      raw_d[v] = T::raw(dy, at[v]);
+      raw_x[v] = T::raw_at(x, off_x + at[v] * (uint32_t)T::kSize);
+      raw_d[v] = T::raw_at(dy, off_d + at[v] * (uint32_t)T::kSize);
     }
-    mean = a.mean[row];
-    rstd = a.rstd[row];
+    const char* m = rows.at(a.mean, r0 + rows.wave, a.R, 4, &off);
+    mean = *reinterpret_cast<const float*>(m + off);
+    const char* s = rows.at(a.rstd, r0 + rows.wave, a.R, 4, &off);
+    rstd = *reinterpret_cast<const float*>(s + off);
   };
   const long long step = (long long)gridDim.x * GROUPS;
   long long r0 = (long long)blockIdx.x * GROUPS;
-  load(r0 + grp);
+  load(r0);
 
   float dg[VPL][E], db[VPL][E];
   uint4 raw_w[VPL];
@@ -64,8 +67,8 @@ void norm_grad_kernel(NormGradArgs a) {
   int turn = 0;
   // every group of a workgroup makes the same number of turns
   for (; r0 < a.R; r0 += step, turn ^= 1) {
-    const bool mine = r0 + grp < a.R;
-    const size_t row = r0 + grp;
+    const long long first = r0 + rows.wave;  // the wave's
+    const bool mine = first + rows.lane < a.R;
     float f[VPL][E], d[VPL][E];
     const float mu = mean, rs = rstd;
 #pragma unroll
@@ -73,7 +76,7 @@ void norm_grad_kernel(NormGradArgs a) {
       T::unpack(raw_x[v], f[v]);
       T::unpack(raw_d[v], d[v]);
     }
-    if (r0 + step < a.R) load(r0 + step + grp);
+    if (r0 + step < a.R) load(r0 + step);
     if (!mine)  // rows past the last count for nothing
 #pragma unroll
       for (int v = 0; v < VPL; ++v)
@@ -83,7 +86,7 @@ void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       float w[E], p0 = 0.f, p1 = 0.f;
-      keep_packed(raw_w[v]);
+      if (VPL > 1) keep_packed(raw_w[v]);
       T::unpack(raw_w[v], w);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
@@ -111,16 +114,17 @@ void norm_grad_kernel(NormGradArgs a) {
       s1 += on(v) ? p1 : 0.f;
     }
     // two turns' words never meet: a wave is at most one barrier ahead
-    s0 = sum_row<LPR>(s0, slots[turn][0]) * a.inv_c;
-    s1 = sum_row<LPR>(s1, slots[turn][1]) * a.inv_c;
+    s0 = sum_row<LPR>(s0, slots[turn][0]) * a.inv_c * -rs;
+    s1 = sum_row<LPR>(s1, slots[turn][1]) * a.inv_c * -rs;
     if (a.dx && mine)
 #pragma unroll
       for (int v = 0; v < VPL; ++v)
         if (on(v)) {
           float y[E];
 #pragma unroll
-          for (int j = 0; j < E; ++j) y[j] = (d[v][j] - fmaf(f[v][j], s1, s0)) * rs;
-          T::store(a.dx, row * C + at[v], y);
+          for (int j = 0; j < E; ++j) y[j] = fmaf(d[v][j], rs, fmaf(f[v][j], s1, s0));
+          T::store_at(static_cast<char*>(a.dx) + first * C * (long long)T::kSize,
+                      (rows.lane * (uint32_t)C + at[v]) * (uint32_t)T::kSize, y);
         }
   }
   if (!a.part) return;
@@ -375,7 +379,13 @@ Plan plan(int R, int C) {
 
 template <int DT>
 hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
-  const Plan p = plan<DT>(a.R, a.C);
+  Plan p = plan<DT>(a.R, a.C);
+  // four rows of a wave have to lie within 32 bits of the first (any kernel takes any grid)
+  const bool near = a.R == 1 || (a.ldx < 1 << 27 && a.lddy < 1 << 27);
+  if (!near && p.grid && p.fn && (a.C + Chunk<DT>::E - 1) / Chunk<DT>::E <= 64) {
+    p.fn = (const void*)&norm_grad_kernel<DT, 64, 1, 512>;
+    p.threads = 512;
+  }
   float* const part = a.part;
   const bool sums = a.dgamma || a.dbeta;
   if (!sums) a.part = nullptr;

@@ -27,6 +27,10 @@ struct Chunk<1> {
   __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
     return load16_any(static_cast<const uint16_t*>(p) + i);
   }
+  __device__ __forceinline__ static uint4 raw_at(const char* p, uint32_t byte) { return load16_any(p + byte); }
+  __device__ __forceinline__ static void store_at(char* p, uint32_t byte, const float* f) {
+    store16_any(p + byte, pack_bf16x8(f));
+  }
   __device__ __forceinline__ static uint4 ones() {
     return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   }
@@ -47,7 +51,13 @@ struct Chunk<0> {
   static constexpr int E = 4;
   static constexpr size_t kSize = 4;
   __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
-    return __builtin_bit_cast(uint4, *reinterpret_cast<const u32x4_any4*>(static_cast<const float*>(p) + i));
+    return raw_at(static_cast<const char*>(p), (uint32_t)i * 4);
+  }
+  __device__ __forceinline__ static uint4 raw_at(const char* p, uint32_t byte) {
+    return __builtin_bit_cast(uint4, *reinterpret_cast<const u32x4_any4*>(p + byte));
+  }
+  __device__ __forceinline__ static void store_at(char* p, uint32_t byte, const float* f) {
+    store(p + byte, 0, f);
   }
   __device__ __forceinline__ static uint4 ones() {
     return make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u);
@@ -67,6 +77,28 @@ struct Chunk<0> {
   }
   __device__ __forceinline__ static void store1(void* p, size_t i, float f) {
     static_cast<float*>(p)[i] = f;
+  }
+};
+
+// Where the rows of a workgroup lie, LPR lanes to each: a wave's first row is uniform, so
+// that rows are addressed by a uniform base and 32 bits a lane (LPR < 64: the caller's
+// strides leave the wave's other rows within them).
+template <int LPR>
+struct WaveRows {
+  static constexpr int kRows = LPR < 64 ? 64 / LPR : 1;  // rows of a wave
+  int wave, lane;  // the wave's first row in the workgroup, the lane's row in the wave
+  __device__ __forceinline__ WaveRows()
+      : wave(__builtin_amdgcn_readfirstlane(LPR < 64 ? (threadIdx.x >> 6) * kRows : threadIdx.x / LPR)),
+        lane(LPR < 64 ? (threadIdx.x & 63) / LPR : 0) {}
+  // rows of `bytes` from row `first` of R on: the base, and where the lane's row lies from
+  // it; rows past the last repeat it
+  __device__ __forceinline__ const char* at(const void* p, long long first, long long R, long long bytes,
+                                            uint32_t* off) const {
+    const long long f = min(first, R - 1);
+    int l = lane;
+    if (LPR < 64 && f + kRows > R) l = min(l, (int)(R - 1 - f));
+    *off = LPR < 64 ? (uint32_t)l * (uint32_t)bytes : 0u;
+    return static_cast<const char*>(p) + f * bytes;
   }
 };
 

@@ -356,8 +356,27 @@ def test_offsets_past_32_bits():
     r1 = api.layer_norm_backward(x, x, mean, rstd)
     r2 = api.layer_norm_backward(xc, xc, mean, rstd)
     assert all(torch.equal(s, t) for s, t in zip(r1, r2))
+    # many rows that lie far apart, and narrow ones (a wave holds four of the latter)
+    for R, C, ld in ((600, 64, 1 << 25), (5, 40, 1 << 31), (5000, 24, 1 << 22)):
+        buf = torch.empty((R - 1) * ld + C, dtype=torch.bfloat16, device="cuda")
+        s = buf.as_strided((R, C), (ld, 1))
+        s.copy_(_rows(g, R, C, torch.bfloat16))
+        c = s.contiguous()
+        _say("rows", R, C, "of stride", ld)
+        y, mean, rstd = api.layer_norm(s, stats=True)
+        ref = Q.layer_norm_ref(_f64(c), None, None, float(np.float32(1e-5)))
+        _within("y", _f64(y), ref[0], _y_bound(_f64(c), *ref, None, None) + U[torch.bfloat16] * np.abs(ref[0]))
+        assert torch.equal(api.quantize_rows(s).q, api.quantize_rows(c).q)
+        dx, dg, _ = api.layer_norm_backward(s, s, mean, rstd)
+        cx, cg, _ = api.layer_norm_backward(c, c, mean, rstd)
+        # sums in another order: as near as each is to the exact ones
+        assert ((dx.float() - cx.float()).abs() <= 2.0 ** -7 * cx.float().abs() + 2.0 ** -14 * rstd[:, None]
+                * c.float().abs().amax()).all()
+        assert ((dg - cg).abs() <= 2.0 ** -12 * (c.float() * ((c.float() - mean[:, None]) * rstd[:, None])).abs().sum(0)).all()
+        torch.cuda.synchronize()
+        del buf, s
+    del x
     torch.cuda.synchronize()
-    del buf, x
     # an output of more than 2^31 elements
     R, K, Cout = 540000, 32, 4000
     _say("output past 2^31")

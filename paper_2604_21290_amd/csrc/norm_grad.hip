@@ -7,7 +7,7 @@
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
 // Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
 // 103 (4.9), 100352 x 320 39 (4.9), 100352 x 80 15.0 (3.2, of which the second kernel and
-// the gap before it take 4), 8193 x 1001 17 (2.9).  Few rows take one launch.
+// the gap before it take 4), 8193 x 1001 15.7 (3.1).  Few rows take one launch.
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"
@@ -167,19 +167,27 @@ void norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-// out[c] = sum over the G rows of part [G, cols]: COLS columns a workgroup, 1024 / COLS
-// rows at a time, in the same order always.
-template <int COLS>
+// out[c] = sum over the G rows of part [G, 2 cols]: 32 columns a workgroup (whole lines;
+// with 8 the second kernel of 8193 x 1001 took 1.7 us more), 32 rows at a time, in the
+// same order always.
 __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, int G, int cols,
                                                              float* dgamma, float* dbeta) {
-  constexpr int ROWS = 1024 / COLS;
+  constexpr int COLS = 32, ROWS = 1024 / COLS;
   __shared__ float sums[ROWS][COLS + 1];
   const int t = threadIdx.x % COLS, w = threadIdx.x / COLS;
   const int c = blockIdx.x * COLS + t;
   float s = 0.f;
-  if (c < 2 * cols)
-#pragma unroll 8
-    for (int g = w; g < G; g += ROWS) s += part[(size_t)g * 2 * cols + c];
+  // (eight loads under way at a time, also where there are fewer left)
+  for (int g0 = w; g0 < G; g0 += 8 * ROWS) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int g = g0 + u * ROWS;
+      v[u] = part[(size_t)min(g, G - 1) * 2 * cols + min(c, 2 * cols - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += g0 + u * ROWS < G ? v[u] : 0.f;
+  }
   sums[w][t] = s;
 #pragma unroll
   for (int h = ROWS / 2; h >= 1; h /= 2) {
@@ -408,11 +416,7 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
                           dim3(256), argv, 0, stream);
   }
   if (e != hipSuccess || !sums) return e;
-  // (few columns are spread over more workgroups)
-  if (2 * a.C <= 2048)
-    norm_grad_sum_kernel<8><<<(2 * a.C + 7) / 8, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
-  else
-    norm_grad_sum_kernel<32><<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
+  norm_grad_sum_kernel<<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 

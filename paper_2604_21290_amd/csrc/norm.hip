@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
 #pragma unroll
         for (int v = 0; v < VPL; ++v)
           if (on(v)) store_q8<E>(d + (off + at[v]), q, f[v]);
-        if (lane < a.Kp - C) d[off + C + lane] = 0;  // fewer than 16
+        for (int k = lane; k < a.Kp - C; k += LPR) d[off + C + k] = 0;  // fewer than 16
         if (lane == 0) (a.scale + first)[rows.lane] = q.scale;
       }
     }
@@ -177,7 +177,10 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
 
 // The lanes and chunks for rows of n chunks: at most three a lane, whose registers leave
 // three waves a SIMD and more.  Many short rows lie four to a wave, 16 lanes each: their
-// sums take four steps within 16 lanes, and a wave has more bytes in flight.
+// sums take four steps within 16 lanes, and a wave has more bytes in flight.  Eight to a
+// wave where that leaves one chunk a lane (100352 x 40 bf16, norm 6.0 us for 7.6), and
+// for 8 bits alone, which need no weights, up to three (100352 x 192 11.1 for 12.3; the
+// norm would take 17.4 for 15.3).
 template <int DT, int MODE>
 hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
   constexpr int E = Chunk<DT>::E;
@@ -191,8 +194,13 @@ hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
   };
 #define GL_ROW(LPR, VPL) go((const void*)&row_kernel<DT, MODE, LPR, VPL>, 256 / LPR)
   if (a.C < E || n > 2048) return go((const void*)&row_any_kernel<DT, MODE>, 1);
-  // four rows of a wave lie within 32 bits of the first
+  // the eight rows of a wave lie within 32 bits of the first
   const bool near = a.R == 1 || a.ldx < 1 << 27;
+  if (near && a.R >= 16384) {
+    if (n <= 8) return GL_ROW(8, 1);
+    if constexpr (MODE == kQ8)
+      if (n <= 24) return n <= 16 ? GL_ROW(8, 2) : GL_ROW(8, 3);
+  }
   if (n <= 16 && near) return GL_ROW(16, 1);
   if (n <= 48 && near && a.R >= 4096) return n <= 32 ? GL_ROW(16, 2) : GL_ROW(16, 3);
   if (n <= 192) return n <= 64 ? GL_ROW(64, 1) : n <= 128 ? GL_ROW(64, 2) : GL_ROW(64, 3);

@@ -151,7 +151,7 @@ void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         float s = half ? db[v][j] : dg[v][j];
-        if (LPR == 16) s = sum_over_rows16(s);  // the wave's four groups
+        if (LPR < 64) s = sum_over_groups<LPR>(s);  // the wave's
         if ((threadIdx.x & 63) < LPR) sums[wave * COLS + (lane + v * LPR) * E + j] = s;
       }
     __syncthreads();
@@ -371,6 +371,8 @@ Plan plan(int R, int C) {
     if (n <= 256) return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 1>, 256, 1, 0};
     return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 4>, 256, 1, 0};
   }
+  // (100352 x 40 bf16: 11.4 us, 14.0 with 16 lanes a row)
+  if (n <= 8 && R >= 16384) return make((const void*)&norm_grad_kernel<DT, 8, 1, 512>, 512, 8, 512);
   if (n <= 16) return make((const void*)&norm_grad_kernel<DT, 16, 1, 512>, 512, 16, 512);
   if (n <= 32) return make((const void*)&norm_grad_kernel<DT, 16, 2, 512>, 512, 16, 512);
   if (n <= 48) return make((const void*)&norm_grad_kernel<DT, 16, 3, 512>, 512, 16, 256);
@@ -388,7 +390,7 @@ Plan plan(int R, int C) {
 template <int DT>
 hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
   Plan p = plan<DT>(a.R, a.C);
-  // four rows of a wave have to lie within 32 bits of the first (any kernel takes any grid)
+  // the rows of a wave have to lie within 32 bits of the first (any kernel takes any grid)
   const bool near = a.R == 1 || (a.ldx < 1 << 27 && a.lddy < 1 << 27);
   if (!near && p.grid && p.fn && (a.C + Chunk<DT>::E - 1) / Chunk<DT>::E <= 64) {
     p.fn = (const void*)&norm_grad_kernel<DT, 64, 1, 512>;

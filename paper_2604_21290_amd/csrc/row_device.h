@@ -109,7 +109,7 @@ __device__ __forceinline__ void keep_packed(uint4& v) {
 }
 
 // ---------------------------------------------------------------------------
-// sums and maxima over the LPR lanes (16, 64, or a workgroup's LPR / 64 waves) of
+// sums and maxima over the LPR lanes (8, 16, 64, or a workgroup's LPR / 64 waves) of
 // one row; every lane of the group gets the result, in the same order always.
 // `slot`: a word of LDS for each wave, for this reduction alone (LPR > 64).
 // ---------------------------------------------------------------------------
@@ -123,16 +123,22 @@ struct MaxU {
 };
 
 template <class Op>
+__device__ __forceinline__ uint32_t reduce8(uint32_t v) {
+  v = Op::of(v, dpp_mov<0xB1>(v));      // quad_perm [1,0,3,2]
+  v = Op::of(v, dpp_mov<0x4E>(v));      // quad_perm [2,3,0,1]
+  return Op::of(v, dpp_mov<0x141>(v));  // half-row mirror: the other quad of eight
+}
+template <class Op>
 __device__ __forceinline__ uint32_t reduce16(uint32_t v) {
-  v = Op::of(v, dpp_mov<0xB1>(v));   // quad_perm [1,0,3,2]
-  v = Op::of(v, dpp_mov<0x4E>(v));   // quad_perm [2,3,0,1]
-  v = Op::of(v, dpp_mov<0x141>(v));  // half-row mirror: the other quad of eight
+  v = reduce8<Op>(v);
   return Op::of(v, dpp_mov<0x140>(v));  // row mirror: the other eight
 }
 
-// Sum over the four rows of 16 lanes of a wave, lane by lane (gfx950 swaps rows of two
+// Sum over the groups of 8 or 16 lanes of a wave, lane by lane (gfx950 swaps rows of two
 // registers: with both the same, each ends with one of each pair's rows twice).
-__device__ __forceinline__ float sum_over_rows16(float v) {
+template <int LPR>
+__device__ __forceinline__ float sum_over_groups(float v) {
+  if (LPR == 8) v += __uint_as_float(dpp_mov<0x128>(__float_as_uint(v)));  // row rotate by 8
   const uint32_t u = __float_as_uint(v);
   const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -143,6 +149,7 @@ __device__ __forceinline__ float sum_over_rows16(float v) {
 
 template <class Op, int LPR>
 __device__ __forceinline__ uint32_t reduce_row(uint32_t v, uint32_t* slot) {
+  if (LPR == 8) return reduce8<Op>(v);
   v = reduce16<Op>(v);
   if (LPR == 16) return v;
   const uint32_t a = Op::of(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16));

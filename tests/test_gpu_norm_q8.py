@@ -82,7 +82,9 @@ def _edges(dt):
 NORM_CASES = [(dt, C, (1, 3, 37)[i % 3], (0, 0, 5)[i % 3], i % 2, i % 4 != 3)
               for dt in ("bf16", "f32") for i, C in enumerate(_edges(dt))]
 NORM_CASES += [("bf16", 80, 4099, 0, 0, True), ("f32", 192, 1000, 0, 0, True), ("bf16", 640, 2051, 3, 1, True),
-               ("bf16", 33, 20001, 0, 1, True), ("f32", 16, 65537, 0, 0, False), ("bf16", 2560, 700, 0, 0, True)]
+               ("bf16", 33, 20001, 0, 1, True), ("bf16", 64, 16384, 0, 0, True), ("bf16", 65, 16390, 0, 0, True),
+               ("bf16", 123, 16385, 2, 1, False), ("bf16", 192, 20000, 0, 0, True), ("bf16", 13, 16400, 5, 1, True),
+               ("f32", 31, 17001, 1, 0, True), ("f32", 90, 16385, 0, 0, True), ("f32", 16, 65537, 0, 0, False), ("bf16", 2560, 700, 0, 0, True)]
 
 
 @pytest.mark.parametrize("dt,C,R,gap,shift,affine", NORM_CASES)

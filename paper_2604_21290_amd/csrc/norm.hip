@@ -63,8 +63,12 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
     const long long first = r0 + rows.wave;  // the wave's
     const bool mine = first + rows.lane < a.R;
     float f[VPL][E];
+    uint32_t top = 0;
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) T::unpack(raw[v], f[v]);
+    for (int v = 0; v < VPL; ++v) {
+      T::unpack(raw[v], f[v]);
+      if (MODE == kQ8) top = max(top, T::top(raw[v]));
+    }
     if (r0 + step < a.R) load(r0 + step);
     if (MODE != kQ8) {
       // sum over the row of what `term` makes of each value
@@ -110,12 +114,13 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
       }
     }
     if (MODE != kNorm) {
-      uint32_t top = 0;
+      if (MODE == kNormQ8) {
 #pragma unroll
-      for (int v = 0; v < VPL; ++v)
+        for (int v = 0; v < VPL; ++v)
 #pragma unroll
-        for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
-      const RowQ8 q(max_row<LPR>(top, slots[turn][2]));
+          for (int j = 0; j < E; ++j) top = max(top, __float_as_uint(f[v][j]) & 0x7fffffffu);
+      }
+      const RowQ8<DT == 0 && MODE == kQ8> q(max_row<LPR>(top, slots[turn][2]));
       if (mine) {
         int8_t* d = a.q + first * a.Kp;
         const uint32_t off = rows.lane * (uint32_t)a.Kp;
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
   } else {
     uint32_t top = 0;
     for (int c = threadIdx.x; c < C; c += 256) top = max(top, __float_as_uint(value(c)) & 0x7fffffffu);
-    const RowQ8 q(max_row<256>(top, slots[2]));
+    const RowQ8<DT == 0 && MODE == kQ8> q(max_row<256>(top, slots[2]));
     int8_t* d = a.q + row * a.Kp;
     for (int c = threadIdx.x; c < a.Kp; c += 256) d[c] = c < C ? q.one(value(c)) : 0;
     if (threadIdx.x == 0) a.scale[row] = q.scale;

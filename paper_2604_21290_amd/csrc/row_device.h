@@ -35,6 +35,14 @@ struct Chunk<1> {
     return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   }
   __device__ __forceinline__ static void unpack(const uint4& v, float* f) { unpack_bf16x8(v, f); }
+  // the largest magnitude's bits as fp32, two values at a time
+  __device__ __forceinline__ static uint32_t top(const uint4& v) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    auto mag = [](uint32_t w) { return __builtin_bit_cast(u16x2, w & 0x7fff7fffu); };
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(v.x), mag(v.y)),
+                                              __builtin_elementwise_max(mag(v.z), mag(v.w)));
+    return (uint32_t)max(m[0], m[1]) << 16;
+  }
   __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
     store16_any(static_cast<uint16_t*>(p) + i, pack_bf16x8(f));
   }
@@ -65,6 +73,9 @@ struct Chunk<0> {
   __device__ __forceinline__ static void unpack(const uint4& v, float* f) {
     f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y);
     f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
+  }
+  __device__ __forceinline__ static uint32_t top(const uint4& v) {
+    return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
   }
   __device__ __forceinline__ static void store(void* p, size_t i, const float* f) {
     u32x4_any4 v;
@@ -178,41 +189,50 @@ __device__ __forceinline__ uint32_t max_row(uint32_t v, uint32_t* slot) {
 
 // ---------------------------------------------------------------------------
 // 8-bit rows: q = rne(127 x / top), scale = top / 127, top the row's largest
-// magnitude.  The quotient is the correctly rounded one (for bf16 it then ties
-// exactly where 127 x / top does): x is taken times 127 2^-e, exact for bf16,
-// with e top's exponent, so nothing over- or underflows that matters; a product
-// with the reciprocal is corrected once by its remainder.  Adding 1.5 2^23
+// magnitude.  The quotient is the correctly rounded one, so that it ties exactly where
+// 127 x / top does: 127 / top is held in two parts, hi + lo, and fma(x, hi, x lo) rounds
+// their sum once (for bf16 the quotient is never nearer to a tie than 2^-17 of itself
+// without being one).  Stored fp32 (F32) takes the quotient of the rounded 127 x, as the
+// definition in fp32 does; 2^-e, e top's exponent, keeps it in range.  Adding 1.5 2^23
 // rounds to the nearest even whole number and leaves it in the low byte.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kTopMin = 0x04800000u;  // 2^-118: a row below it counts as zero
 
+template <bool F32>
 struct RowQ8 {
-  float c, a, inv, scale;
+  float c, hi, lo, scale;
   uint32_t keep;  // 0: the row is not finite, and all its values are 0
   __device__ __forceinline__ explicit RowQ8(uint32_t top) {
     const bool zero = top < kTopMin, bad = top >= 0x7f800000u;  // an infinity or a NaN in the row
     const uint32_t t = zero || bad ? 0x3f800000u : top;
-    a = __uint_as_float((t & 0x7fffffu) | 0x3f800000u);  // in [1, 2)
+    const float f = __uint_as_float(t);
+    const float a = __uint_as_float((t & 0x7fffffu) | 0x3f800000u);  // f 2^-e, in [1, 2)
     const float r = __builtin_amdgcn_rcpf(a);
-    inv = fmaf(fmaf(-a, r, 1.f), r, r);
+    const float inv = fmaf(fmaf(-a, r, 1.f), r, r);
     // 127 2^-e; 0 brings every value to 0
     c = zero || bad ? 0.f : __uint_as_float(((133u + 127u - (t >> 23)) << 23) | 0x7e0000u);
-    const float f = __uint_as_float(t), s = f * (1.f / 127.f);
+    if (F32) {  // the reciprocal of a in two parts
+      hi = inv;
+      lo = fmaf(-inv, a, 1.f) * inv;
+    } else {
+      hi = c * inv;
+      lo = zero || bad ? 0.f : fmaf(-hi, f, 127.f) * inv * (c * (1.f / 127.f));
+    }
+    const float s = f * (1.f / 127.f);
     scale = zero ? 0.f : bad ? __uint_as_float(0x7fc00000u)
                              : fmaf(fmaf(-127.f, s, f), 1.f / 127.f, s);
     keep = bad ? 0 : ~0u;
   }
   // the quotient's whole number in the low byte
   __device__ __forceinline__ uint32_t bits(float x) const {
-    const float t = x * c;
-    const float q = t * inv;
-    return __float_as_uint(fmaf(fmaf(-q, a, t), inv, q) + 12582912.f);
+    const float t = F32 ? x * c : x;
+    return __float_as_uint(fmaf(t, hi, t * lo) + 12582912.f);
   }
   __device__ __forceinline__ int8_t one(float x) const { return (int8_t)(bits(x) & keep); }
   __device__ __forceinline__ uint32_t pack4(const float* f) const {
-    const uint32_t lo = __builtin_amdgcn_perm(bits(f[1]), bits(f[0]), 0x0c0c0400u);
-    const uint32_t hi = __builtin_amdgcn_perm(bits(f[3]), bits(f[2]), 0x04000c0cu);
-    return (lo | hi) & keep;
+    const uint32_t lo4 = __builtin_amdgcn_perm(bits(f[1]), bits(f[0]), 0x0c0c0400u);
+    const uint32_t hi4 = __builtin_amdgcn_perm(bits(f[3]), bits(f[2]), 0x04000c0cu);
+    return (lo4 | hi4) & keep;
   }
 };
 
@@ -220,8 +240,8 @@ typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
 typedef uint32_t u32x2_any1 __attribute__((ext_vector_type(2), aligned(1), may_alias));
 
 // E values of a chunk to 8 bits at any place
-template <int E>
-__device__ __forceinline__ void store_q8(int8_t* p, const RowQ8& q, const float* f) {
+template <int E, class Q>
+__device__ __forceinline__ void store_q8(int8_t* p, const Q& q, const float* f) {
   if (E == 8) *reinterpret_cast<u32x2_any1*>(p) = u32x2_any1{q.pack4(f), q.pack4(f + 4)};
   else *reinterpret_cast<u32_any*>(p) = q.pack4(f);
 }

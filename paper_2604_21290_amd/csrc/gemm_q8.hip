@@ -386,6 +386,155 @@ hipError_t launch_pipe_q8(const GemmQ8Args& a, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------------------
+// Short rows: a workgroup keeps 64 or 96 columns of W, all of K, in LDS, and its four
+// waves take strips of 16 rows, each for itself, with no barrier between them.  A strip
+// goes straight to registers; each 64 bytes of K of the wave's next strip are requested
+// when this one's have been multiplied, and its residual after this one's results.  So
+// every wave has a strip on its way from memory (5 to 7 waves a SIMD), where the tiles
+// above load W with every tile and meet at a barrier every 128 bytes of K.
+//   100352x320x80 with residual 13.7 us (16.4 by tiles), 64 MB of memory traffic;
+//   6272x192x768 with GELU 7.3 (8.3), of which 3.4 are the GELU's instructions.
+// Loading both halves of a 128-byte line together changed nothing; strips of 32 rows
+// leave too few waves (6272x192x192 4.0 for 3.6).
+// ---------------------------------------------------------------------------
+template <int DT_, int KS_, int TN_>
+struct StripCfg {  // KS: 64-byte steps of K; TN: 16-column tiles
+  static constexpr int DT = DT_, KS = KS_, TN = TN_;
+  static constexpr int BM = 16, BN = 16 * TN, NS = (KS + 1) / 2;
+  static constexpr int kUnits = NS * BN / 8 / 4;  // 8 rows by 128 bytes of W, per wave
+  static constexpr size_t kSmem = (size_t)NS * BN * 128 + 2 * BN * 4;
+  // operands of a strip, its sums, a step of W, a residual, addresses and the epilogue
+  static constexpr int kRegs = 4 * (KS + 2 * TN) + 2 * TN * (DT ? 1 : 2) + 24;
+  static constexpr int kByLds = (int)(160 * 1024 / kSmem), kByRegs = 512 / kRegs;
+  static constexpr int kPerCU = kByLds < kByRegs ? kByLds : kByRegs;
+  static_assert(TN % 2 == 0 && BN <= 256 && kPerCU >= 1 && kPerCU <= 8, "whole units a wave, a thread a column");
+};
+
+template <class G, int ACT_OUT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G::kPerCU, G::kPerCU)))
+void gemm_q8_strip_kernel(GemmQ8Args a) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int DT = G::DT, KS = G::KS, TN = G::TN, BM = G::BM, BN = G::BN;
+  const int R = a.R, Cout = a.Cout, rowb = a.Kp;
+  const int ntm = (R + BM - 1) / BM, ntn = (Cout + BN - 1) / BN, per = (int)gridDim.x / ntn;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, t = lane & 15;
+  // workgroups with the same rows follow each other on an XCD
+  const int blk = xcd_remap(blockIdx.x, gridDim.x), rb = blk / ntn, n0 = (blk - rb * ntn) * BN;
+
+  // W: unit u is 8 of its rows at 128 bytes of K, its 16-byte slots permuted as in the
+  // pipeline; zeros past the rows' end
+#pragma unroll
+  for (int i = 0; i < G::kUnits; ++i) {
+    const int u = w + 4 * i, s = u / (BN / 8), grp = u - s * (BN / 8), lr = lane >> 3;
+    const int k = s * 128 + ((lane & 7) ^ ((lr & 3) | ((grp & 1) << 2))) * 16;
+    const char* p = reinterpret_cast<const char*>(a.W) + (size_t)min(n0 + 8 * grp + lr, Cout - 1) * rowb + k;
+    lds_dma16(k < rowb ? p : reinterpret_cast<const char*>(kZero16), lds_offset(smem) + u * 1024);
+  }
+  float* const vec = reinterpret_cast<float*>(smem + G::NS * BN * 128);
+  if (tid < BN) {
+    const int n = min(n0 + tid, Cout - 1);
+    vec[tid] = a.sw[n];
+    vec[BN + tid] = a.bias ? load1<DT>(a.bias, n) : 0.f;
+  }
+
+  uint4 fa[KS];
+  float sa;
+  Raw8<DT> res[TN / 2];
+  // rows past R repeat the last one; past a row's end its last slot, where W is zero
+  auto load_step = [&](int k, int m0) {
+    const char* base = reinterpret_cast<const char*>(a.A) + (size_t)m0 * rowb;
+    const int at = k < KS - 1 ? 64 * k + 16 * g : min(64 * k + 16 * g, rowb - 16);
+    fa[k] = *reinterpret_cast<const uint4*>(base + (uint32_t)(min(t, R - 1 - m0) * rowb + at));
+  };
+  auto load_rest = [&](int m0) {
+    const int row = min(m0 + t, R - 1);
+    sa = a.sa[row];
+    if (!a.residual) return;
+#pragma unroll
+    for (int p = 0; p < TN / 2; ++p) {
+      const int n = n0 + 32 * p + 8 * g;
+      if (n + 8 <= Cout) res[p].load(a.residual, (size_t)row * Cout + n);
+    }
+  };
+  const int step = per * 4;
+  int mt = rb * 4 + w;
+  if (mt < ntm) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) load_step(k, mt * BM);
+    load_rest(mt * BM);
+  }
+  dma_wait_barrier();
+
+  const int rd = ((t >> 2) * 8 + (t & 3)) * 128 + (g ^ (t & 7)) * 16;
+  auto strip = [&](auto MORE) {
+    constexpr bool more = decltype(MORE)::value;
+    const int m0 = mt * BM, m1 = m0 + step * BM;
+    i32x4 acc[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[j] = i32x4{0, 0, 0, 0};
+    const int at = fresh(rd);  // (or all of W would move to registers)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const char* const pw = smem + (k >> 1) * BN * 128 + (at ^ ((k & 1) * 64));
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[j] = mfma_i8(*reinterpret_cast<const uint4*>(pw + ((j >> 1) * 32 + (j & 1) * 4) * 128), fa[k], acc[j]);
+      if (more) load_step(k, m1);
+    }
+    // lane (g, t) of MFMA tiles 2p and 2p + 1: eight columns of row t
+    const int row = m0 + t;
+#pragma unroll
+    for (int p = 0; p < TN / 2; ++p) {
+      const int c = 32 * p + 8 * g, n = n0 + c;
+      float y[8];
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        y[v] = fmaf((float)acc[2 * p + (v >> 2)][v & 3], sa * vec[c + v], vec[BN + c + v]);
+        if (ACT_OUT) y[v] = gelu_q8(y[v]);
+      }
+      if (row >= R || n >= Cout) continue;
+      const size_t o = (size_t)row * Cout + n;
+      if (n + 8 <= Cout) {
+        if (a.residual) res[p].add_to(y);
+        store8<DT>(a.out, o, y);
+      } else {
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+          if (n + v < Cout) {
+            if (a.residual) y[v] += load1<DT>(a.residual, o + v);
+            store1<DT>(a.out, o + v, y[v]);
+          }
+      }
+    }
+    if (more) load_rest(m1);
+  };
+  for (; mt < ntm - step; mt += step) strip(std::true_type());
+  if (mt < ntm) strip(std::false_type());
+}
+
+// As many workgroups as the CUs hold together, or fewer with the same number of turns.
+template <class G>
+hipError_t launch_strip_q8(const GemmQ8Args& a, hipStream_t stream) {
+  const void* fn = a.act_out ? (const void*)&gemm_q8_strip_kernel<G, 1> : (const void*)&gemm_q8_strip_kernel<G, 0>;
+  const long ntn = (a.Cout + G::BN - 1) / G::BN, fours = ((long)(a.R + G::BM - 1) / G::BM + 3) / 4;
+  const long most = std::max(1L, 256L * G::kPerCU / ntn), turns = (fours + most - 1) / most;
+  const long per = (fours + turns - 1) / turns;
+  return launch_with_smem(fn, dim3((unsigned)(per * ntn)), dim3(256), G::kSmem, stream, nullptr, nullptr, a);
+}
+
+template <int DT, int TN>
+hipError_t launch_strips_q8(const GemmQ8Args& a, hipStream_t stream) {
+  switch ((a.Kp + 63) / 64) {
+    case 1: return launch_strip_q8<StripCfg<DT, 1, TN>>(a, stream);
+    case 2: return launch_strip_q8<StripCfg<DT, 2, TN>>(a, stream);
+    case 3: return launch_strip_q8<StripCfg<DT, 3, TN>>(a, stream);
+    case 4: return launch_strip_q8<StripCfg<DT, 4, TN>>(a, stream);
+    default: return launch_strip_q8<StripCfg<DT, 5, TN>>(a, stream);
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Few rows: the weights' bytes bound the layer, so every CU has to stream some.  A
 // workgroup takes 16 columns and 16 rows; its eight waves split K, 64 bytes of each row
 // in turn, and load their operands straight into registers, up to U steps before any is
@@ -447,19 +596,36 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
 //   16384x4096x4096  237               284                434                447
 //   12544x640x2560   32.5/46.0/57.9 *  32.9/42.7/50.4 *   40.8/52.7/60.7     50.0/59.2/65.3
 //   12544x2560x640   37.1/42.4/41.1    26.4/28.3/28.4 *   36.4/37.3/39.5     36.5/39.5/38.8
-//   25088x192x768    21.0/31.4/36.9    14.9/19.8/19.1 *   17.0/21.6/20.2     20.5/25.8/24.1
-//   100352x80x320    29.2/51.0/65.2    20.2/31.9/37.1     20.5/29.8/37.2 *   26.7/35.6/44.8
-//   6272x192x768     11.6/17.0/17.0     8.0/ 9.7/ 9.7      7.4/ 8.4/ 8.8 *    8.3/ 9.7/ 9.9
+//   25088x192x768    21.0/31.4/36.9    14.9/19.8/19.1     17.0/21.6/20.2     20.5/25.8/24.1
+//   100352x80x320    29.2/51.0/65.2    20.2/31.9/37.1     20.5/29.8/37.2     26.7/35.6/44.8
+//   6272x192x768     11.6/17.0/17.0     8.0/ 9.7/ 9.7      7.4/ 8.4/ 8.8      8.3/ 9.7/ 9.9
 //   1000x8000x1000   77.5              45.6               31.1               19.8 *
-// (* the one taken: at 12544x640x2560 the larger tile without GELU or residual).  The
+// (* the one taken: at 12544x640x2560 the larger tile without GELU or residual; strips
+// take three of the others).  The
 // kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
 // 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
 // 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
 // 3.4 (3.9); at 196x2560x640 8.0 (7.4).
+//
+// Strips where K is short, against the best of the tiles (us, plain / GELU / residual):
+//   100352x320x80    11.7/16.0/13.7    15.0/18.6/16.3
+//   100352x80x320    17.1/27.2/36.9    20.8/31.1/37.5
+//   6272x192x768      5.9/ 7.3/ 7.7     7.2/ 8.4/ 8.8
+//   25088x320x320     9.7/11.8/10.9    11.6/13.5/13.3
+//   6272x192x192      3.6/ 4.4/ 4.1     4.3/ 4.9/ 4.5
+//   1200x320x320      3.5/ 3.9/ 3.6     3.7/ 4.2/ 3.9
+// Not taken: K past 320 (6272x384x384 6.1/7.0/7.1 for 5.7/6.4/6.7: each strip reads all of
+// W from LDS), rows of 256 bytes (25088x256x512 14.1/17.4/17.7 for 13.2/17.4/15.2), and
+// wide or large outputs, which tiles of 128 columns write in longer runs (4096x128x4096
+// 13.0/17.6/17.3 for 12.2/17.0/16.5, 100352x80x320 fp32 45/46/66 for 36/41/64).  96
+// columns where one such strip is all (100352x320x80 by 64: 12.4/16.9/14.8).
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
   const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);
   if (a.R <= 16 || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20)) return launch_rows_q8<DT>(a, stream);
+  const double bytes = (double)a.R * a.Cout * (DT ? 2 : 4);
+  if (a.Kp <= 320 && a.Kp != 256 && a.Cout <= 2048 && bytes <= 1 << 26)
+    return a.Cout > 64 && a.Cout <= 96 ? launch_strips_q8<DT, 6>(a, stream) : launch_strips_q8<DT, 4>(a, stream);
   const double n = (a.Kp + 127) / 128, gelu = a.act_out ? 1 : 0, res = a.residual ? 1 : 0;
   auto cost = [&](int edge, int per_cu, double round, double tile) {
     const long t = ((long)(a.R + edge - 1) / edge) * ((a.Cout + edge - 1) / edge);

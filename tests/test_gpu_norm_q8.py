@@ -295,6 +295,39 @@ def test_linear_q8(dt, R, K, Cout, gelu, residual, bias):
         assert torch.equal(res, out)
 
 
+# short rows: every number of 64-byte steps of K and its edges, column tiles of 64 and 96
+# with and without a rest, one and more strips a wave, and the sizes next to those taken
+SHORT_CASES = [
+    (5000, 1, 80, False, False, True), (5121, 16, 77, True, True, True), (7000, 63, 65, False, True, False),
+    (3333, 64, 96, True, False, True), (2500, 65, 97, False, True, True), (1111, 129, 500, True, False, False),
+    (4099, 192, 192, True, True, True), (999, 200, 771, False, True, True), (2047, 241, 129, False, False, True),
+    (2047, 250, 129, True, True, True), (2047, 257, 129, False, True, True), (1501, 320, 320, True, True, True),
+    (1501, 321, 320, False, True, True), (513, 100, 2048, False, False, True), (513, 100, 2049, False, False, True),
+    (40009, 80, 320, True, True, True), (60001, 320, 80, False, True, True), (30011, 300, 8, False, True, True),
+    (41000, 80, 7, True, True, True), (131089, 48, 1, False, True, True), (26216, 40, 640, False, False, False),
+]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("R,K,Cout,gelu,residual,bias", SHORT_CASES)
+def test_linear_q8_short_rows(dt, R, K, Cout, gelu, residual, bias):
+    api = _api()
+    _say("linear_q8, short rows", dt, R, K, Cout, gelu, residual, bias)
+    g = np.random.default_rng(R + 3 * K + 5 * Cout)
+    x, W, b, res = _layer(g, api, R, K, Cout, DT[dt], gelu, residual, bias)
+    act = api.GL_ACT_GELU if gelu else api.GL_ACT_NONE
+    buf = torch.full((R * Cout + 128,), 7.0, dtype=DT[dt], device="cuda")
+    out = buf[64: 64 + R * Cout].view(R, Cout)
+    api.linear_q8(x, W, b, act, res, DT[dt], out=out)
+    torch.cuda.synchronize()
+    assert (buf[:64] == 7).all() and (buf[64 + R * Cout:] == 7).all(), "outside the output"
+    _check_layer(x, W, b, res, gelu, out)
+    if res is not None:  # the residual updated in place
+        api.linear_q8(x, W, b, act, res, DT[dt], out=res)
+        torch.cuda.synchronize()
+        assert torch.equal(res, out)
+
+
 @pytest.mark.parametrize("R,Cout,shift", [(5, 64, 1), (300, 257, 3), (5000, 640, 5), (20000, 81, 7)])
 def test_linear_q8_unaligned_output(R, Cout, shift):
     api = _api()

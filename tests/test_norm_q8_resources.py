@@ -35,7 +35,7 @@ def test_no_spills(tmp_path):
     with ThreadPoolExecutor(len(SOURCES)) as ex:
         found = dict(zip(SOURCES, ex.map(lambda s: _kernels(s, tmp_path), SOURCES)))
     counts = {"row_kernel": 0, "norm_grad_kernel": 0, "norm_grad_few_kernel": 0, "gemm_q8_pipe_kernel": 0,
-              "gemm_q8_rows_kernel": 0}
+              "gemm_q8_rows_kernel": 0, "gemm_q8_strip_kernel": 0}
     for kernels in found.values():
         for name, (scratch, waves, body) in kernels.items():
             for k in counts:
@@ -48,6 +48,8 @@ def test_no_spills(tmp_path):
                 assert loops and not any("scratch_" in b for b in loops), name
             else:
                 assert scratch == 0, (name, scratch)
+            if "StripCfg" in name:
+                assert waves >= 4, (name, waves)
             if "PipeCfgILi128ELi128E" in name or "PipeCfgILi64ELi64ELi2ELi2ELi2E" in name:
                 assert waves >= 4, (name, waves)
     assert all(counts.values()), counts

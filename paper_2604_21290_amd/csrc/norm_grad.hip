@@ -14,6 +14,11 @@
 
 namespace gl {
 
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
+__device__ __forceinline__ void store4_any(float* p, const float* f) {
+  *reinterpret_cast<f32x4_any*>(p) = f32x4_any{f[0], f[1], f[2], f[3]};
+}
+
 // LPR lanes hold a row, VPL chunks each; NT threads a workgroup.  A row's loads are
 // under way while the one before it is worked on.
 template <int DT, int LPR, int VPL, int NT>
@@ -134,13 +139,20 @@ void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       const int c = lane + v * LPR, i = min(c * E, C - E), skip = max(c * E + E - C, 0);
-      if (c < n)
+      if (c < n && skip == 0) {
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+          store4_any(pg + i + j, &dg[v][j]);
+          store4_any(pg + C + i + j, &db[v][j]);
+        }
+      } else if (c < n) {
 #pragma unroll
         for (int j = 0; j < E; ++j)
           if (j >= skip) {
             pg[i + j] = dg[v][j];
             pg[C + i + j] = db[v][j];
           }
+      }
     }
     return;
   }
@@ -203,14 +215,16 @@ __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, 
 }
 
 // Few rows, in one launch and without a workspace: the first `row_wgs` workgroups take
-// rows, 256 / LPR each, the others 16 chunks of columns each, over all rows: the columns'
-// sums need no average of a row, and reading a small input twice is cheap.
+// rows, 512 / LPR each, the others 8 chunks of columns each, over all rows: the columns'
+// sums need no average of a row, and reading a small input twice is cheap.  What a column
+// workgroup takes is trips to memory, of up to 8 x 64 rows each (with 256 threads on 16
+// chunks 392 x 2560 bf16 took 7.0 us for 5.5, 784 x 2560 12.6 for 9.3).
 template <int DT, int LPR, int VPL>
-__global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int row_wgs) {
+__global__ __launch_bounds__(512) void norm_grad_few_kernel(NormGradArgs a, int row_wgs) {
   using T = Chunk<DT>;
-  constexpr int E = T::E, NT = 256, GROUPS = NT / LPR, RG = NT / 16;
+  constexpr int E = T::E, NT = 512, GROUPS = NT / LPR, CL = 8, RG = NT / CL;
   __shared__ uint32_t slots[2][NT / 64];
-  __shared__ float sums[RG][16 * E + 1];
+  __shared__ float sums[2][NT / 64][CL * E];
   const int C = a.C, n = (C + E - 1) / E;
   if ((int)blockIdx.x < row_wgs) {
     const int lane = threadIdx.x & (LPR - 1);
@@ -259,39 +273,54 @@ __global__ __launch_bounds__(256) void norm_grad_few_kernel(NormGradArgs a, int 
     }
     return;
   }
-  const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
-  const int c = ((int)blockIdx.x - row_wgs) * 16 + lane, i = min(c * E, C - E);
+  const int lane = threadIdx.x % CL, grp = threadIdx.x / CL;
+  const int c = ((int)blockIdx.x - row_wgs) * CL + lane, i = min(c * E, C - E);
   float dg[E] = {}, db[E] = {};
   if (c < n) {
-#pragma unroll 4
-    for (int r = grp; r < a.R; r += RG) {
-      float f[E], d[E];
-      T::unpack(T::raw(static_cast<const char*>(a.x) + (size_t)r * a.ldx * T::kSize, i), f);
-      T::unpack(T::raw(static_cast<const char*>(a.dy) + (size_t)r * a.lddy * T::kSize, i), d);
-      const float mean = a.mean[r], rstd = a.rstd[r];
+    // (U rows under way at a time, also where there are fewer left)
+    constexpr int U = 8;
+    for (int first = 0; first < a.R; first += U * RG) {
+      uint4 f4[U] = {}, d4[U] = {};
+      float mean[U] = {}, rstd[U] = {};
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        dg[j] = fmaf(d[j], (f[j] - mean) * rstd, dg[j]);
-        db[j] += d[j];
+      for (int u = 0; u < U; ++u) {
+        if (first + u * RG >= a.R) break;
+        const int r = first + u * RG + grp, row = min(r, a.R - 1);
+        f4[u] = T::raw(static_cast<const char*>(a.x) + (size_t)row * a.ldx * T::kSize, i);
+        d4[u] = T::raw(static_cast<const char*>(a.dy) + (size_t)row * a.lddy * T::kSize, i);
+        mean[u] = a.mean[row], rstd[u] = a.rstd[row];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float f[E], d[E];
+        T::unpack(f4[u], f);
+        T::unpack(first + u * RG + grp < a.R ? d4[u] : make_uint4(0, 0, 0, 0), d);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          dg[j] = fmaf(d[j], (f[j] - mean[u]) * rstd[u], dg[j]);
+          db[j] += d[j];
+        }
       }
     }
   }
-  for (int half = 0; half < 2; ++half) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) sums[grp][lane * E + j] = half ? db[j] : dg[j];
-    __syncthreads();
-    float* out = half ? a.dbeta : a.dgamma;
-    if (const int at = threadIdx.x; at < 16 * E && out) {
-      const int ch = ((int)blockIdx.x - row_wgs) * 16 + at / E, col = min(ch * E, C - E) + at % E;
-      // (the last chunk's first columns are the one before's)
-      if (ch < n && col >= ch * E) {
-        float s = 0.f;
-#pragma unroll 8
-        for (int q = 0; q < RG; ++q) s += sums[q][at];
-        out[col] = s;
-      }
+  for (int j = 0; j < E; ++j) {
+    const float s0 = sum_over_groups<CL>(dg[j]), s1 = sum_over_groups<CL>(db[j]);  // the wave's
+    if ((threadIdx.x & 63) < CL) {
+      sums[0][threadIdx.x >> 6][lane * E + j] = s0;
+      sums[1][threadIdx.x >> 6][lane * E + j] = s1;
     }
-    __syncthreads();
+  }
+  __syncthreads();
+  const int half = threadIdx.x / (CL * E), at = threadIdx.x % (CL * E);
+  float* out = half ? a.dbeta : a.dgamma;
+  const int ch = ((int)blockIdx.x - row_wgs) * CL + at / E, col = min(ch * E, C - E) + at % E;
+  // (the last chunk's first columns are the one before's)
+  if (half < 2 && out && ch < n && col >= ch * E) {
+    float s = sums[half][0][at];
+#pragma unroll
+    for (int q = 1; q < NT / 64; ++q) s += sums[half][q][at];
+    out[col] = s;
   }
 }
 
@@ -346,13 +375,15 @@ struct Plan {
   int threads, groups, grid;  // grid 0: the one launch for few rows
 };
 
-// Up to so many rows take one launch.  Its column workgroups add R / 16 rows a lane, so
+// Up to so many rows take one launch.  Its column workgroups add R / 64 rows a lane, so
 // its time grows with R; the two kernels' sums grow with C.  us, one launch (two):
-//   bf16 R       C = 80      192          640          2560
-//   196          4.0 (6.5)   4.1 (8.3)    4.2 (7.0)    4.3 (11.4)
-//   392          5.4 (6.6)   5.5 (8.4)    5.7 (7.1)    7.0 (12.2)
-//   784          8.5 (6.7)   8.5 (8.4)    8.9 (7.4)   12.6 (15.9)
-constexpr int kFewRows = 512, kFewWide = 1024;
+//   bf16 R       C = 80      192          640          2560         1000
+//   196          4.2 (5.8)   4.3 (7.0)    4.4          4.6
+//   392          4.6         4.6 (7.1)    4.8 (7.1)    5.5 (10.0)
+//   640                                                             7.2 (7.4)
+//   784          6.2 (6.1)   6.2 (7.4)    6.6 (7.3)    9.3 (12.5)   8.1 (7.6)
+//   1200                     7.9 (7.4)                14.4 (14.3)
+constexpr int kFewRows = 800, kFewMid = 640, kFewWide = 1024;
 
 template <int DT>
 Plan plan(int R, int C) {
@@ -365,11 +396,11 @@ Plan plan(int R, int C) {
     return Plan{fn, threads, groups, (int)std::min<long long>(((long long)R + groups - 1) / groups, g)};
   };
   if (C < E || n > 2048) return Plan{nullptr, 256, 1, std::min(R, 256)};
-  if (R <= (n > 128 ? kFewWide : kFewRows) && n <= 1024) {
-    if (n <= 16) return Plan{(const void*)&norm_grad_few_kernel<DT, 16, 1>, 256, 16, 0};
-    if (n <= 64) return Plan{(const void*)&norm_grad_few_kernel<DT, 64, 1>, 256, 4, 0};
-    if (n <= 256) return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 1>, 256, 1, 0};
-    return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 4>, 256, 1, 0};
+  if (R <= (n > 128 ? kFewWide : n > 96 ? kFewMid : kFewRows) && n <= 1024) {
+    if (n <= 16) return Plan{(const void*)&norm_grad_few_kernel<DT, 16, 1>, 512, 32, 0};
+    if (n <= 64) return Plan{(const void*)&norm_grad_few_kernel<DT, 64, 1>, 512, 8, 0};
+    if (n <= 256) return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 1>, 512, 2, 0};
+    return Plan{(const void*)&norm_grad_few_kernel<DT, 256, 4>, 512, 2, 0};
   }
   // (100352 x 40 bf16: 11.4 us, 14.0 with 16 lanes a row)
   if (n <= 8 && R >= 16384) return make((const void*)&norm_grad_kernel<DT, 8, 1, 512>, 512, 8, 512);
@@ -380,7 +411,7 @@ Plan plan(int R, int C) {
   if (n <= 128) return make((const void*)&norm_grad_kernel<DT, 64, 2, 512>, 512, 64, 512);
   if (n <= 192) return make((const void*)&norm_grad_kernel<DT, 64, 3, 256>, 256, 64, 512);
   if (n <= 256) return make((const void*)&norm_grad_kernel<DT, 64, 4, 256>, 256, 64, 512);
-  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 768);
+  if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 512);
   if (n <= 768) return make((const void*)&norm_grad_kernel<DT, 256, 3, 256>, 256, 256, 512);
   // (10000 x 8192 bf16: 101 us, 114 with four chunks a lane of 256)
   if (n <= 1024) return make((const void*)&norm_grad_kernel<DT, 1024, 1, 1024>, 1024, 1024, 256);
@@ -403,7 +434,7 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (!p.grid) {
     int row_wgs = a.dx ? (a.R + p.groups - 1) / p.groups : 0;
-    const int n = (a.C + Chunk<DT>::E - 1) / Chunk<DT>::E, col_wgs = sums ? (n + 15) / 16 : 0;
+    const int n = (a.C + Chunk<DT>::E - 1) / Chunk<DT>::E, col_wgs = sums ? (n + 7) / 8 : 0;
     argv[1] = &row_wgs;
     return hipLaunchKernel(p.fn, dim3(row_wgs + col_wgs), dim3(p.threads), argv, 0, stream);
   }

@@ -85,6 +85,10 @@ NORM_CASES += [("bf16", 80, 4099, 0, 0, True), ("f32", 192, 1000, 0, 0, True), (
                ("bf16", 33, 20001, 0, 1, True), ("bf16", 64, 16384, 0, 0, True), ("bf16", 65, 16390, 0, 0, True),
                ("bf16", 123, 16385, 2, 1, False), ("bf16", 192, 20000, 0, 0, True), ("bf16", 13, 16400, 5, 1, True),
                ("f32", 31, 17001, 1, 0, True), ("f32", 90, 16385, 0, 0, True), ("f32", 16, 65537, 0, 0, False), ("bf16", 2560, 700, 0, 0, True)]
+# one launch of more than one trip over the rows, and wide rows' sums through the workspace
+NORM_CASES += [("bf16", 100, 799, 0, 1, True), ("f32", 37, 513, 3, 0, False), ("bf16", 1003, 640, 0, 0, True),
+               ("bf16", 3001, 1024, 1, 0, True), ("f32", 1999, 1030, 0, 0, True), ("bf16", 2561, 1100, 0, 1, True),
+               ("bf16", 5423, 1027, 0, 0, True), ("bf16", 7000, 1029, 8, 0, False), ("f32", 5001, 1040, 0, 1, True)]
 
 
 @pytest.mark.parametrize("dt,C,R,gap,shift,affine", NORM_CASES)

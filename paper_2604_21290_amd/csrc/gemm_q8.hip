@@ -545,7 +545,12 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
   constexpr int NW = 8, U = 8;
   __shared__ __align__(16) int part[NW][256];
   const int R = a.R, Cout = a.Cout, rowb = a.Kp;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+  // columns first; where there are more rows, an XCD takes a stretch of them with all
+  // columns (1885x2699x81 6.8 us for 8.5), and elsewhere most widths give it its own
+  // columns with all rows as they are (196x192x768 2.5, 3.1 by stretches)
+  const int ntm = (R + 15) / 16, ntn = (Cout + 15) / 16;
+  const int blk = ntm > ntn ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x, mb = blk / ntn;
+  const int n0 = (blk - mb * ntn) * 16, m0 = mb * 16;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, t = lane & 15;
   const char* pw = reinterpret_cast<const char*>(a.W) + (size_t)min(n0 + t, Cout - 1) * rowb;
@@ -584,7 +589,7 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
 template <int DT>
 hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
   const void* fn = a.act_out ? (const void*)&gemm_q8_rows_kernel<DT, 1> : (const void*)&gemm_q8_rows_kernel<DT, 0>;
-  return launch_with_smem(fn, dim3((a.Cout + 15) / 16, (a.R + 15) / 16), dim3(512), 0, stream, nullptr, nullptr, a);
+  return launch_with_smem(fn, dim3((unsigned)((a.Cout + 15) / 16 * ((a.R + 15) / 16))), dim3(512), 0, stream, nullptr, nullptr, a);
 }
 
 // The tile for a layer, by what each takes for one round of all CUs, in us: so much for
@@ -605,7 +610,10 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
 // kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
 // 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
 // 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
-// 3.4 (3.9); at 196x2560x640 8.0 (7.4).
+// 3.4 (3.9); at 196x2560x640 8.0 (7.4).  And where its own estimate, by the bytes that its
+// units read (rows a multiple of 512 bytes apart meet in the same channels), is below the
+// tiles': 1910x2993x57 5.7 (8.6), 1885x2699x81 6.7 (9.4), 300x6000x300 11.6 (16.2); not
+// at 784x4096x200 12.9 (10.3).
 //
 // Strips where K is short, against the best of the tiles (us, plain / GELU / residual):
 //   100352x320x80    11.7/16.0/13.7    15.0/18.6/16.3
@@ -622,7 +630,9 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
   const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);
-  if (a.R <= 16 || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20)) return launch_rows_q8<DT>(a, stream);
+  // (a launch has fewer than 2^32 threads)
+  if ((a.R <= 16 && units < 1 << 22) || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20))
+    return launch_rows_q8<DT>(a, stream);
   const double bytes = (double)a.R * a.Cout * (DT ? 2 : 4);
   if (a.Kp <= 320 && a.Kp != 256 && a.Cout <= 2048 && bytes <= 1 << 26)
     return a.Cout > 64 && a.Cout <= 96 ? launch_strips_q8<DT, 6>(a, stream) : launch_strips_q8<DT, 4>(a, stream);
@@ -635,7 +645,10 @@ hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
                        cost(128, 2, 1.0 * n + 2.5 + 2.1 * gelu + 3 * res, 0.7 * n + 2),
                        cost(64, 4, 0.78 * n + 1.2 + 1.2 * gelu + 1.7 * res, 0.45 * n + 1.5),
                        cost(64, 2, 0.37 * n + 1.15 + 0.6 * gelu + 0.95 * res, 0.27 * n + 1.5)};
-  switch (std::min_element(c, c + 4) - c) {
+  const double* best = std::min_element(c, c + 4);
+  const double mb = 1e-6 * units * a.Kp * (a.Kp % 512 ? 1 : 1.4);
+  if (units <= 4096 && 1.2 + 3.2 * mb < *best) return launch_rows_q8<DT>(a, stream);
+  switch (best - c) {
     case 0: return launch_pipe_q8<PipeCfg<256, 256, 2, 4, 2>, DT>(a, stream);
     case 1: return launch_pipe_q8<PipeCfg<128, 128, 2, 4, 2>, DT>(a, stream);
     case 2: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 2>, DT>(a, stream);

@@ -182,12 +182,12 @@ void norm_grad_kernel(NormGradArgs a) {
 // out[c] = sum over the G rows of part [G, 2 cols]: 32 columns a workgroup (whole lines;
 // with 8 the second kernel of 8193 x 1001 took 1.7 us more), 32 rows at a time, in the
 // same order always.
-__global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, int G, int cols,
+__global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, int G, int cols, int first,
                                                              float* dgamma, float* dbeta) {
   constexpr int COLS = 32, ROWS = 1024 / COLS;
   __shared__ float sums[ROWS][COLS + 1];
   const int t = threadIdx.x % COLS, w = threadIdx.x / COLS;
-  const int c = blockIdx.x * COLS + t;
+  const int c = first + blockIdx.x * COLS + t;
   float s = 0.f;
   // (eight loads under way at a time, also where there are fewer left)
   for (int g0 = w; g0 < G; g0 += 8 * ROWS) {
@@ -449,7 +449,10 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
                           dim3(256), argv, 0, stream);
   }
   if (e != hipSuccess || !sums) return e;
-  norm_grad_sum_kernel<<<(2 * a.C + 31) / 32, 1024, 0, stream>>>(part, p.grid, a.C, a.dgamma, a.dbeta);
+  constexpr int kMost = 1 << 20;  // workgroups a launch: fewer than 2^32 threads
+  for (int c = 0; c < 2 * a.C; c += 32 * kMost)
+    norm_grad_sum_kernel<<<std::min((2 * a.C - c + 31) / 32, kMost), 1024, 0, stream>>>(part, p.grid, a.C, c,
+                                                                                      a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 

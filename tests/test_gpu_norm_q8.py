@@ -312,6 +312,11 @@ SHORT_CASES = [
 ]
 
 
+# few outputs of long rows, more rows than columns and the other way round
+SHORT_CASES += [(1910, 2993, 57, True, True, True), (1885, 2699, 81, False, False, True), (300, 6000, 300, False, True, True),
+                (1200, 2560, 96, True, False, False), (33, 4100, 1000, False, True, True), (5000, 1000, 3, True, True, True)]
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("R,K,Cout,gelu,residual,bias", SHORT_CASES)
 def test_linear_q8_short_rows(dt, R, K, Cout, gelu, residual, bias):
@@ -343,6 +348,38 @@ def test_linear_q8_unaligned_output(R, Cout, shift):
     torch.cuda.synchronize()
     assert (buf[:shift] == 7).all() and (buf[shift + R * Cout:] == 7).all(), "outside the output"
     _check_layer(x, W, b, None, False, out)
+
+
+def test_gradient_of_very_many_columns():
+    """More columns than one launch of the sums' kernel has threads for."""
+    api = _api()
+    C = 2 ** 26 + 9
+    _say("gradient of", C, "columns")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn(2, C, generator=g, device="cuda", dtype=torch.float32) for _ in range(2))
+    y, mean, rstd = api.layer_norm(x, stats=True)
+    _, dgamma, dbeta = api.layer_norm_backward(dy, x, mean, rstd, need=(False, True, True))
+    torch.cuda.synchronize()
+    assert torch.equal(dbeta, dy[0] + dy[1])
+    terms = dy * ((x - mean[:, None]) * rstd[:, None])
+    # a term rounds three times, the sum once
+    assert ((dgamma - terms[0] - terms[1]).abs() <= 4 * E32 * terms.abs().sum(0) + 1e-37).all()
+
+
+def test_linear_q8_one_row_of_very_many_columns():
+    """More 16-column units than one launch has workgroups of 512 threads for."""
+    api = _api()
+    N = 2 ** 26 + 40
+    _say("one row to", N, "columns")
+    w = torch.randint(-127, 128, (N, 16), dtype=torch.int8, device="cuda")
+    w[:, 5:] = 0
+    W = api.Q8Rows(w, torch.ones(N, device="cuda"), 5)
+    q = torch.zeros((1, 16), dtype=torch.int8, device="cuda")
+    q[0, :5] = torch.tensor([3, -7, 127, 0, -127])
+    out = api.linear_q8(api.Q8Rows(q, torch.ones(1, device="cuda"), 5), W, dtype=torch.float32)
+    torch.cuda.synchronize()
+    # whole numbers below 2^24: exact
+    assert torch.equal(out[0], sum(float(q[0, k]) * w[:, k].float() for k in range(5)))
 
 
 def test_linear_q8_extremes_are_exact():

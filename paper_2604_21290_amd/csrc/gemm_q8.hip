@@ -105,6 +105,10 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
 //     consecutive columns of a row in tiles 2p and 2p + 1: results go from the
 //     accumulators to memory 16 bytes (bf16) a lane, 64 a row, with no trip
 //     through LDS.
+//   - Small tiles, for few outputs, have KG groups of waves, which take every KG-th stage
+//     into buffers of their own and add their sums in LDS.  A stage takes 0.27 us where
+//     one wave a SIMD has the tile (64 x 64), 0.2 with two groups (64 x 32), 0.12 with
+//     four (32 x 32).
 // Tiles are walked so that the 32 that an XCD works on at a time are 8 x 4.
 // What bounds it: at 8192 x 8192 x 8192 (420-430 us, 2.6 POP/s; the library's int8
 // product 440) the matrix cores are busy 66 % of the cycles, at a clock that falls to
@@ -114,17 +118,19 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
 // bytes in four buffers (446), 256 x 128 tiles in three buffers (478), four waves of
 // 128 x 128 (886: operands move between the register files).
 // ---------------------------------------------------------------------------
-template <int BM_, int BN_, int WR_, int WC_, int NBUF_>
+template <int BM_, int BN_, int WR_, int WC_, int NBUF_, int KG_ = 1>
 struct PipeCfg {
-  static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, NBUF = NBUF_, STEP = 128;
-  static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+  static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, NBUF = NBUF_, KG = KG_, STEP = 128;
+  static constexpr int kWaves = WR * WC;  // of one of KG groups, which take every KG-th stage
+  static constexpr int kThreads = 64 * kWaves * KG;
   static constexpr int kStage = (BM + BN) * STEP;
   static constexpr int kRPL = 1024 / STEP;  // rows of a wave's load
   static constexpr int kLoadsA = BM / kRPL / kWaves, kLoadsW = BN / kRPL / kWaves;  // per wave and stage
   static constexpr int TM = BM / WR / 16, TN = BN / WC / 16;
   static constexpr int kVec = BM + 2 * BN;  // a tile's scales and bias
-  static constexpr size_t kSmem = (size_t)NBUF * kStage + 2 * kVec * 4;
-  static constexpr int kPerCU = (int)(160 * 1024 / kSmem) * kWaves <= 16 ? (int)(160 * 1024 / kSmem) : 16 / kWaves;
+  static constexpr int kSums = BM * BN * 4;  // the tile's sums of a group
+  static constexpr size_t kBufs = (size_t)KG * NBUF * kStage, kSmem = kBufs + 2 * kVec * 4 + (KG - 1) * kSums;
+  static constexpr int kFit = (int)(160 * 1024 / kSmem), kPerCU = kFit * kWaves * KG <= 16 ? kFit : 16 / (kWaves * KG);
   static_assert(BM % (kRPL * kWaves) == 0 && BN % (kRPL * kWaves) == 0, "whole loads per wave");
   static_assert(TN % 2 == 0, "pairs of column tiles");
   static_assert(BM <= kThreads && BN <= kThreads, "a thread loads one of each vector");
@@ -154,16 +160,17 @@ __device__ __forceinline__ void dma_wait_barrier_but() {
 }
 
 template <class G, int DT, int ACT_OUT>
-__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(G::kWaves * G::kPerCU / 4, G::kWaves * G::kPerCU / 4)))
+__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(G::kThreads * G::kPerCU / 256, G::kThreads * G::kPerCU / 256)))
 void gemm_q8_pipe_kernel(GemmQ8Args a) {
   extern __shared__ __align__(16) char smem[];
   constexpr int BM = G::BM, BN = G::BN, STEP = G::STEP, TM = G::TM, TN = G::TN, NA = G::kLoadsA, NB = G::kLoadsW;
   constexpr int NL = NA + NB, NBUF = G::NBUF;
   constexpr int WROWS = 16 * TM, WCOLS = 16 * TN;
   const int R = a.R, Cout = a.Cout, rowb = a.Kp;
-  const int nstages = (rowb + STEP - 1) / STEP;
+  const int nstages = (rowb + STEP * G::KG - 1) / (STEP * G::KG);  // of each group
   const int ntm = (R + BM - 1) / BM, ntn = (Cout + BN - 1) / BN, ntiles = ntm * ntn;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = G::KG > 1 ? wv / G::kWaves : 0, w = wv - kg * G::kWaves;
   const int g = lane >> 4, t = lane & 15;
   const int wm = w / G::WC, wn = w % G::WC;
 
@@ -181,7 +188,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   // 16 bytes land at place l % 8 of row l / 8 and hold slot place ^ key, where a row
   // of A has key row % 8 and one of W, whose rows are read in fours of every other
   // eight, row % 4 + 4 (row / 8 % 2).  Rows past R or Cout repeat the last one.
-  const uint32_t lds0 = lds_offset(smem) + w * 1024;
+  const uint32_t lds0 = lds_offset(smem) + kg * NBUF * G::kStage + w * 1024;
   constexpr int RPL = G::kRPL;
   const int lr = lane >> 3;
   const int slot_a = ((lane & 7) ^ lr) * 16;
@@ -203,7 +210,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   };
   // past the end of a row, W reads zeros, and A its last slot again
   auto load = [&](int i, int buf) {
-    const int off = s_load * STEP;
+    const int off = (s_load * G::KG + kg) * STEP;
     const uint32_t d = lds0 + buf * G::kStage + i * G::kWaves * 1024;
     if (i < NA) {
       lds_dma16_base(base_a, src_a[i < NA ? i : 0] + min(off, lim_a), d);
@@ -228,8 +235,8 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   uint4 fa[2][TM], fb[2][TN];
   // (the second half of a stage's row is 64 bytes off: the slot's permutation is an
   // exclusive or)
-  const int rd_a = (wm * WROWS + t) * STEP + (g ^ (t & 7)) * 16;
-  const int rd_b = (BM + wn * WCOLS + (t >> 2) * 8 + (t & 3)) * STEP + (g ^ (t & 7)) * 16;
+  const int rd_a = kg * NBUF * G::kStage + (wm * WROWS + t) * STEP + (g ^ (t & 7)) * 16;
+  const int rd_b = kg * NBUF * G::kStage + (BM + wn * WCOLS + (t >> 2) * 8 + (t & 3)) * STEP + (g ^ (t & 7)) * 16;
   auto read = [&](int set, int pa, int pb, int i) {  // TM of A, then TN of W
     if (i < TM)
       fa[set][i < TM ? i : 0] = *reinterpret_cast<const uint4*>(smem + pa + i * 16 * STEP);
@@ -243,7 +250,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
   constexpr int kSpread = TM > 2 ? TM / 2 : TM;  // row tiles that the loads are spread over
   auto half = [&](auto KK, int buf, int lbuf) {
     constexpr int kk = decltype(KK)::value;
-    constexpr int kPer = (TM + TN + TM - 2) / (TM - 1), kLPer = (NL + kSpread - 1) / kSpread;
+    constexpr int kPer = TM > 1 ? (TM + TN + TM - 2) / (TM > 1 ? TM - 1 : 1) : TM + TN, kLPer = (NL + kSpread - 1) / kSpread;
     const int pa = buf * G::kStage + (fresh(rd_a) ^ ((kk ^ 1) * 64));
     const int pb = buf * G::kStage + (fresh(rd_b) ^ ((kk ^ 1) * 64));
 #pragma unroll
@@ -272,7 +279,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
 #pragma unroll
   for (int i = 0; i < TM + TN; ++i) read(0, rd_a, rd_b, i);
 
-  float* const vec0 = reinterpret_cast<float*>(smem + NBUF * G::kStage);
+  float* const vec0 = reinterpret_cast<float*>(smem + G::kBufs);
   int buf = 0, turn = 0;
   for (int L = blockIdx.x; L < ntiles; L += gridDim.x, turn ^= 1) {
     int m0, n0;
@@ -302,7 +309,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
         if (row < R && n + 8 <= Cout) res[i % kAhead][p].load(a.residual, (size_t)row * Cout + n);
       }
     };
-    if (kEarly && a.residual) {
+    if (kEarly && a.residual && kg == 0) {
       const int lane_e = fresh(lane);
 #pragma unroll
       for (int i = 0; i < TM; ++i) load_res(i, lane_e);
@@ -327,6 +334,20 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
       buf = buf + 1 == NBUF ? 0 : buf + 1;
       half(integral_constant<int, 1>(), buf, free);
       next_load();
+    }
+
+    if (G::KG > 1) {  // the groups' sums meet in LDS; the first group has the rest
+      i32x4* const sums = reinterpret_cast<i32x4*>(smem + G::kBufs + 2 * G::kVec * 4) + w * TM * TN * 64 + lane;
+      if (kg > 0) {
+#pragma unroll
+        for (int u = 0; u < TM * TN; ++u) sums[(kg - 1) * (G::kSums / 16) + u * 64] = acc[u / TN][u % TN];
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (kg > 0) continue;
+#pragma unroll
+      for (int q = 0; q < G::KG - 1; ++q)
+#pragma unroll
+        for (int u = 0; u < TM * TN; ++u) acc[u / TN][u % TN] += sums[q * (G::kSums / 16) + u * 64];
     }
 
     // lane (g, t) of MFMA tiles (i, 2p) and (i, 2p + 1): eight columns of row t.  Row
@@ -610,10 +631,15 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
 // kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
 // 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
 // 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
-// 3.4 (3.9); at 196x2560x640 8.0 (7.4).  And where its own estimate, by the bytes that its
-// units read (rows a multiple of 512 bytes apart meet in the same channels), is below the
-// tiles': 1910x2993x57 5.7 (8.6), 1885x2699x81 6.7 (9.4), 300x6000x300 11.6 (16.2); not
-// at 784x4096x200 12.9 (10.3).
+// 3.4 (3.9).  And where its own estimate, by the bytes that its units read (rows a multiple
+// of 512 bytes apart meet in the same channels), is below the tiles': 777x1001x333 4.9 (5.2).
+// Tiles for few outputs, 64 x 32 with K between two groups and 32 x 32 between four (us,
+// against 64 x 64, 2 a CU, and 16 x 16):
+//   64x4096x4096      7.9   7.3   (10.2, 16.9)      500x3000x500   7.7  6.0  (9.0,  9.3)
+//   128x4096x4096     8.1  10.5   (10.2, 30.4)      196x2560x640   5.8  5.3  (7.4,  8.1)
+//   871x4336x320     10.4  12.3   (13.2, 16.5)      784x4096x200   7.8  6.7 (10.1, 12.7)
+//   531x5531x891     11.9  14.1   (15.7, 30.1)      300x6000x300  12.6  9.4 (16.3, 11.6)
+//   256x4096x4096    13.1  17.8   (11.3, 58.8)
 //
 // Strips where K is short, against the best of the tiles (us, plain / GELU / residual):
 //   100352x320x80    11.7/16.0/13.7    15.0/18.6/16.3
@@ -631,28 +657,33 @@ template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
   const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);
   // (a launch has fewer than 2^32 threads)
-  if ((a.R <= 16 && units < 1 << 22) || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 20))
+  if ((a.R <= 16 && units < 1 << 22) || units <= 256 || (units <= 1280 && units * a.Kp <= 1 << 19))
     return launch_rows_q8<DT>(a, stream);
   const double bytes = (double)a.R * a.Cout * (DT ? 2 : 4);
   if (a.Kp <= 320 && a.Kp != 256 && a.Cout <= 2048 && bytes <= 1 << 26)
     return a.Cout > 64 && a.Cout <= 96 ? launch_strips_q8<DT, 6>(a, stream) : launch_strips_q8<DT, 4>(a, stream);
   const double n = (a.Kp + 127) / 128, gelu = a.act_out ? 1 : 0, res = a.residual ? 1 : 0;
-  auto cost = [&](int edge, int per_cu, double round, double tile) {
-    const long t = ((long)(a.R + edge - 1) / edge) * ((a.Cout + edge - 1) / edge);
-    return std::max((double)((t + 255) / 256) / per_cu * round, tile);
+  auto rounds = [&](int bm, int bn) {
+    return (double)((((long)(a.R + bm - 1) / bm) * ((a.Cout + bn - 1) / bn) + 255) / 256);
   };
-  const double c[4] = {cost(256, 1, 1.5 * n + 7.5 + 6 * gelu + 10 * res, 0),
+  auto cost = [&](int edge, int per_cu, double round, double tile) {
+    return std::max(rounds(edge, edge) / per_cu * round, tile);
+  };
+  const double c[6] = {cost(256, 1, 1.5 * n + 7.5 + 6 * gelu + 10 * res, 0),
                        cost(128, 2, 1.0 * n + 2.5 + 2.1 * gelu + 3 * res, 0.7 * n + 2),
                        cost(64, 4, 0.78 * n + 1.2 + 1.2 * gelu + 1.7 * res, 0.45 * n + 1.5),
-                       cost(64, 2, 0.37 * n + 1.15 + 0.6 * gelu + 0.95 * res, 0.27 * n + 1.5)};
-  const double* best = std::min_element(c, c + 4);
+                       cost(64, 2, 0.37 * n + 1.15 + 0.6 * gelu + 0.95 * res, 0.27 * n + 1.5),
+                       rounds(64, 32) * (0.2 * n + 1.9), rounds(32, 32) * (0.12 * n + 2.4)};
+  const double* best = std::min_element(c, c + 6);
   const double mb = 1e-6 * units * a.Kp * (a.Kp % 512 ? 1 : 1.4);
   if (units <= 4096 && 1.2 + 3.2 * mb < *best) return launch_rows_q8<DT>(a, stream);
   switch (best - c) {
     case 0: return launch_pipe_q8<PipeCfg<256, 256, 2, 4, 2>, DT>(a, stream);
     case 1: return launch_pipe_q8<PipeCfg<128, 128, 2, 4, 2>, DT>(a, stream);
     case 2: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 2>, DT>(a, stream);
-    default: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 4>, DT>(a, stream);
+    case 3: return launch_pipe_q8<PipeCfg<64, 64, 2, 2, 4>, DT>(a, stream);
+    case 4: return launch_pipe_q8<PipeCfg<64, 32, 4, 1, 4, 2>, DT>(a, stream);
+    default: return launch_pipe_q8<PipeCfg<32, 32, 2, 1, 4, 4>, DT>(a, stream);
   }
 }
 

@@ -315,6 +315,11 @@ SHORT_CASES = [
 # few outputs of long rows, more rows than columns and the other way round
 SHORT_CASES += [(1910, 2993, 57, True, True, True), (1885, 2699, 81, False, False, True), (300, 6000, 300, False, True, True),
                 (1200, 2560, 96, True, False, False), (33, 4100, 1000, False, True, True), (5000, 1000, 3, True, True, True)]
+# K split between groups of waves: fewer stages than groups, a rest of them, several tiles
+# a workgroup
+SHORT_CASES += [(500, 3000, 500, True, True, True), (871, 4336, 320, False, True, True), (100, 1000, 2000, True, False, True),
+                (64, 4096, 4096, False, True, False), (129, 3969, 4033, True, True, True), (130, 400, 2050, False, True, True),
+                (783, 4097, 201, False, False, True), (1100, 5000, 333, True, True, True), (40, 513, 3001, False, True, True)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])

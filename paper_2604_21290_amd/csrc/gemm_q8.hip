@@ -569,9 +569,14 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
   // columns first; where there are more rows, an XCD takes a stretch of them with all
   // columns (1885x2699x81 6.8 us for 8.5), and elsewhere most widths give it its own
   // columns with all rows as they are (196x192x768 2.5, 3.1 by stretches)
-  const int ntm = (R + 15) / 16, ntn = (Cout + 15) / 16;
-  const int blk = ntm > ntn ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x, mb = blk / ntn;
-  const int n0 = (blk - mb * ntn) * 16, m0 = mb * 16;
+  const int ntn = (int)gridDim.x, ntm = (int)gridDim.y;
+  int nb = blockIdx.x, mb = blockIdx.y;
+  if (ntm > ntn) {
+    const int blk = xcd_remap(mb * ntn + nb, ntm * ntn);
+    mb = blk / ntn;
+    nb = blk - mb * ntn;
+  }
+  const int n0 = nb * 16, m0 = mb * 16;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, t = lane & 15;
   const char* pw = reinterpret_cast<const char*>(a.W) + (size_t)min(n0 + t, Cout - 1) * rowb;
@@ -610,7 +615,7 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
 template <int DT>
 hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
   const void* fn = a.act_out ? (const void*)&gemm_q8_rows_kernel<DT, 1> : (const void*)&gemm_q8_rows_kernel<DT, 0>;
-  return launch_with_smem(fn, dim3((unsigned)((a.Cout + 15) / 16 * ((a.R + 15) / 16))), dim3(512), 0, stream, nullptr, nullptr, a);
+  return launch_with_smem(fn, dim3((a.Cout + 15) / 16, (a.R + 15) / 16), dim3(512), 0, stream, nullptr, nullptr, a);
 }
 
 // The tile for a layer, by what each takes for one round of all CUs, in us: so much for

@@ -6,8 +6,8 @@
 // sums of its own over all rows that it meets.  A workgroup then adds its lanes'
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
 // Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
-// 103 (4.9), 100352 x 320 39 (4.9), 100352 x 80 15.0 (3.2, of which the second kernel and
-// the gap before it take 4), 8193 x 1001 15.7 (3.1).  Few rows take one launch.
+// 96 (5.2; 111 in a first run), 100352 x 320 39 (4.9), 100352 x 80 14.0 (3.4, of which the second kernel
+// and the gap before it take 4), 8193 x 1001 15.1 (3.2).  Few rows take one launch.
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"
@@ -411,6 +411,12 @@ Plan plan(int R, int C) {
   if (n <= 128) return make((const void*)&norm_grad_kernel<DT, 64, 2, 512>, 512, 64, 512);
   if (n <= 192) return make((const void*)&norm_grad_kernel<DT, 64, 3, 256>, 256, 64, 512);
   if (n <= 256) return make((const void*)&norm_grad_kernel<DT, 64, 4, 256>, 256, 64, 512);
+  // Few turns: a chunk a lane, so that twice as many loads are under way, and half as many
+  // sums where those weigh.  us, this (two chunks a lane of 256, 512 workgroups): bf16
+  // 1500 x 2560 12.9 (14.2), 2754 x 3000 17.6 (19.7), 5001 x 2201 22.9 (24.2), 10000 x 4096
+  // 46.7 (48.2), 32768 x 2560 99.7 (95.7); fp32 20000 x 1500 69.0 (68.2)
+  if (n <= 512 && R <= 12288)
+    return make((const void*)&norm_grad_kernel<DT, 512, 1, 512>, 512, 512, R < 4096 ? 256 : 512);
   if (n <= 512) return make((const void*)&norm_grad_kernel<DT, 256, 2, 256>, 256, 256, 512);
   if (n <= 768) return make((const void*)&norm_grad_kernel<DT, 256, 3, 256>, 256, 256, 512);
   // (10000 x 8192 bf16: 101 us, 114 with four chunks a lane of 256)

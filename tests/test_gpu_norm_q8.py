@@ -89,6 +89,8 @@ NORM_CASES += [("bf16", 80, 4099, 0, 0, True), ("f32", 192, 1000, 0, 0, True), (
 NORM_CASES += [("bf16", 100, 799, 0, 1, True), ("f32", 37, 513, 3, 0, False), ("bf16", 1003, 640, 0, 0, True),
                ("bf16", 3001, 1024, 1, 0, True), ("f32", 1999, 1030, 0, 0, True), ("bf16", 2561, 1100, 0, 1, True),
                ("bf16", 5423, 1027, 0, 0, True), ("bf16", 7000, 1029, 8, 0, False), ("f32", 5001, 1040, 0, 1, True)]
+# rows of 257 to 512 chunks: more than one turn, and more rows than one chunk a lane takes
+NORM_CASES += [("bf16", 4093, 1037, 0, 1, True), ("bf16", 2051, 4101, 3, 0, True), ("f32", 1025, 12289, 0, 0, True)]
 
 
 @pytest.mark.parametrize("dt,C,R,gap,shift,affine", NORM_CASES)

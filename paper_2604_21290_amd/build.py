@@ -66,7 +66,8 @@ def build_calls(verbose: bool = True) -> str:
 
 
 def build_library(verbose: bool = True, jobs: int | None = None) -> str:
-    """Compile each source to an object in parallel, then link the library."""
+    """Compile each source to an object in parallel, link the library, then look at
+    what became of the binding's shortcut, which the library does not use."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objdir = os.path.join(ROOT, "_build")
     os.makedirs(objdir, exist_ok=True)
@@ -83,7 +84,6 @@ def build_library(verbose: bool = True, jobs: int | None = None) -> str:
     with cf.ThreadPoolExecutor(jobs + 1) as ex:
         calls = ex.submit(build_calls, verbose)
         results = list(ex.map(lambda c: _run(c[0]), cmds))
-        calls.result()
     for (cmd, _), (rc, err) in zip(cmds, results):
         if rc != 0:
             raise RuntimeError(f"hipcc failed ({rc}) on {cmd[-3]}:\n{err}")
@@ -97,6 +97,14 @@ def build_library(verbose: bool = True, jobs: int | None = None) -> str:
     if rc != 0:
         raise RuntimeError(f"link failed ({rc}):\n{err}")
     os.replace(tmp, LIB)
+    # the library is whole without the binding's shortcut, whose failure is told last; an
+    # older one, which may have been built for other signatures, does not stay beside it
+    failed = calls.exception()
+    if failed is not None:
+        if os.path.exists(CALLS):
+            os.remove(CALLS)
+        raise RuntimeError(f"{LIB} is built and complete, but not the binding's shortcut {CALLS}, "
+                           "without which the short calls are marshalled in Python") from failed
     return LIB
 
 

@@ -95,3 +95,23 @@ def test_other_forms_are_left():
     with pytest.raises(TypeError):
         n.layer_norm(x, None, None, "eps", False)
     torch.cuda.synchronize()
+
+
+def test_calls_without_the_shortcut_have_the_same_bits(monkeypatch):
+    """Where _calls.so cannot be loaded, the Python path takes the ordinary forms too."""
+    api = _api()
+    x, dy = torch.randn(9, 72, device="cuda"), torch.randn(9, 72, device="cuda")
+    gamma, beta = torch.randn(72, device="cuda"), torch.randn(72, device="cuda")
+
+    def every():
+        y, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
+        q, n = api.quantize_rows(x), api.layer_norm_q8(x, gamma, beta)
+        out = api.linear_q8(n, q, act_out=api.GL_ACT_GELU, dtype=torch.float32)
+        return [y, mean, rstd, *api.layer_norm_backward(dy, x, mean, rstd, gamma), q.q, q.scale, n.q, n.scale, out]
+
+    api._calls()
+    want = every()
+    monkeypatch.setattr(api, "_native", api._NoCalls)
+    got = every()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -508,7 +508,8 @@ gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const voi
  * gl_linear_q8 -- one fully connected layer on 8-bit rows:
  *   out[r, o] = act_out( (sum_k q[r, k] Wq[o, k]) scale[r] w_scale[o] + bias[o] )
  *               + residual[r, o]
- * The sum is exact (int32); the rest is fp32, rounded once to dt.
+ * The sum is exact (int32); the rest is fp32 in the order above (the sum times the
+ * row's scale, then the channel's), rounded once to dt.
  *   q [R, Kp], scale [R]: 8-bit rows of K values; Wq [Cout, Kp], w_scale [Cout]:
  *   the weights likewise.  bias [Cout] (dt) or NULL; residual [R, Cout] (dt) or
  *   NULL, and may be `out` itself; out [R, Cout] (dt), must not overlap the

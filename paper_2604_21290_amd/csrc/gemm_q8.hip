@@ -1,6 +1,8 @@
 // Fully connected layers on 8-bit rows:
 //   out[r, o] = act_out( (sum_k A[r, k] W[o, k]) sa[r] sw[o] + bias[o] ) + residual[r, o]
-// The sums are exact (int32, at most 131071 terms); then fp32 and one rounding.
+// The sums are exact (int32, at most 131071 terms); then fp32 and one rounding.  A sum meets
+// the row's scale first: the two scales' product alone may overflow (a zero sum would make it
+// a NaN) or lose bits below 2^-126 where the result does neither.
 //   - Staging: 16 bytes a lane straight into LDS, a row's 16-byte slots permuted by
 //     its number so that the rows an operand read touches lie in all banks.
 //   - MFMA 16x16x64: a lane's 16 bytes of a row are one operand.  Operands are
@@ -370,7 +372,7 @@ void gemm_q8_pipe_kernel(GemmQ8Args a) {
         float y[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-          y[v] = fmaf((float)acc[i][2 * p + (v >> 2)][v & 3], sar * vec[BM + c + v], vec[BM + BN + c + v]);
+          y[v] = fmaf((float)acc[i][2 * p + (v >> 2)][v & 3] * sar, vec[BM + c + v], vec[BM + BN + c + v]);
           if (ACT_OUT) y[v] = gelu_q8(y[v]);
         }
         if (row >= R || n >= Cout) continue;
@@ -511,7 +513,7 @@ void gemm_q8_strip_kernel(GemmQ8Args a) {
       float y[8];
 #pragma unroll
       for (int v = 0; v < 8; ++v) {
-        y[v] = fmaf((float)acc[2 * p + (v >> 2)][v & 3], sa * vec[c + v], vec[BN + c + v]);
+        y[v] = fmaf((float)acc[2 * p + (v >> 2)][v & 3] * sa, vec[c + v], vec[BN + c + v]);
         if (ACT_OUT) y[v] = gelu_q8(y[v]);
       }
       if (row >= R || n >= Cout) continue;
@@ -605,7 +607,7 @@ __global__ __launch_bounds__(512) void gemm_q8_rows_kernel(GemmQ8Args a) {
   int s = 0;
 #pragma unroll
   for (int k = 0; k < NW; ++k) s += part[k][tid];
-  float y = fmaf((float)s, a.sa[row] * a.sw[n], a.bias ? load1<DT>(a.bias, n) : 0.f);
+  float y = fmaf((float)s * a.sa[row], a.sw[n], a.bias ? load1<DT>(a.bias, n) : 0.f);
   if (ACT_OUT) y = gelu_q8(y);
   const size_t at = (size_t)row * Cout + n;
   if (a.residual) y += load1<DT>(a.residual, at);

@@ -596,3 +596,38 @@ def test_gradient_against_differences():
         # the step's own rounding, fp32 of the outputs, and the third derivative
         near = float(dy.abs().double().sum())
         assert abs((loss(*up) - loss(*dn)) / (2 * step) - want) <= near * (16 * E32 / step + 4 * step ** 2), which
+
+
+# one size for each of the layer's kernels: few rows, strips, tiles
+@pytest.mark.parametrize("R,K,Cout", [(3, 100, 24), (1000, 100, 1000), (1000, 1000, 1000)])
+def test_linear_q8_scales_whose_product_leaves_fp32(R, K, Cout):
+    """The sum meets the row's scale first: a zero sum stays zero where the scales' product
+    would overflow, and none of its bits are lost where that product would be subnormal."""
+    api = _api()
+    _say("linear_q8, scales", R, K, Cout)
+    g = np.random.default_rng(R)
+    x, W, b, _ = _layer(g, api, R, K, Cout, torch.float32, False, False, True)
+    x.q[:, :K:2] = 0
+    W.q[1::2, 1:K:2] = 0  # every other column's sums are zero
+    x.scale.fill_(3e38)
+    W.scale.fill_(1e6)
+    out = api.linear_q8(x, W, b, dtype=torch.float32)
+    gelu = api.linear_q8(x, W, act_out=api.GL_ACT_GELU, dtype=torch.float32)
+    torch.cuda.synchronize()
+    ref = x.q[:, :K].double() @ W.q[:, :K].double().t()
+    assert (ref == 0).sum() >= R * (Cout // 2)
+    assert torch.equal(out[ref == 0], b.expand(R, Cout)[ref == 0])
+    assert not gelu[ref == 0].any()
+    # scales of a product near 2^-140, sums of 2^19 and more: three roundings, as of any other scales
+    x, W, _, _ = _layer(g, api, R, K, Cout, torch.float32, False, False, False)
+    for t in (x.q, W.q):
+        t[:, :K] = t[:, :K].clamp(min=-127).abs() | 64
+    x.scale.mul_(2.0 ** -64)
+    W.scale.mul_(2.0 ** -62)
+    out = api.linear_q8(x, W, dtype=torch.float32)
+    torch.cuda.synchronize()
+    assert float(x.scale.max()) * float(W.scale.max()) < 2.0 ** -126
+    ref = Q.linear_q8_ref(x.q[:, :K].cpu().numpy(), _f64(x.scale), W.q[:, :K].cpu().numpy(), _f64(W.scale))
+    some = np.abs(ref) >= 2.0 ** -125
+    assert some.mean() > 0.9
+    assert (np.abs(_f64(out) - ref) <= 3 * E32 * np.abs(ref) + 2.0 ** -149)[some].all()

@@ -510,6 +510,9 @@ gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const voi
  *               + residual[r, o]
  * The sum is exact (int32); the rest is fp32 in the order above (the sum times the
  * row's scale, then the channel's), rounded once to dt.
+ * GL_ACT_GELU is y Phi(y) for its argument y: in fp32 within (13 + |y| + 2 y^2) 2^-24 of
+ * itself, down to results of 1e-36; in bf16, before that rounding, within 5.7e-7
+ * e^(1.5 |y|) more of itself, but never more than 2.8e-3.
  *   q [R, Kp], scale [R]: 8-bit rows of K values; Wq [Cout, Kp], w_scale [Cout]:
  *   the weights likewise.  bias [Cout] (dt) or NULL; residual [R, Cout] (dt) or
  *   NULL, and may be `out` itself; out [R, Cout] (dt), must not overlap the

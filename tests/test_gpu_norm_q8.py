@@ -631,3 +631,41 @@ def test_linear_q8_scales_whose_product_leaves_fp32(R, K, Cout):
     some = np.abs(ref) >= 2.0 ** -125
     assert some.mean() > 0.9
     assert (np.abs(_f64(out) - ref) <= 3 * E32 * np.abs(ref) + 2.0 ** -149)[some].all()
+
+
+def _gelu_sweep(api, R, n, dtype):
+    """The GELU of n arguments of -12.5 .. 12.5 and of some of either end, in R rows: sums
+    and rows' scales of one, so that an argument is its channel's scale."""
+    v = torch.linspace(-12.5, 12.5, n - 8, dtype=torch.float64).float()
+    ends = torch.tensor([0.0, -0.0, 1e-30, -1e-30, -14.0, -40.0, 1e30, -1e30])
+    v = torch.cat([v, ends]).cuda()
+    one = torch.zeros((max(R, n), 16), dtype=torch.int8, device="cuda")
+    one[:, 0] = 1
+    x, W = api.Q8Rows(one[:R], torch.ones(R, device="cuda"), 1), api.Q8Rows(one[:n], v, 1)
+    return v.double().cpu(), api.linear_q8(x, W, act_out=api.GL_ACT_GELU, dtype=dtype)
+
+
+# few rows, strips, tiles
+@pytest.mark.parametrize("R,n", [(3, 20011), (500, 2048), (600, 20011)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_gelu_over_its_range(dt, R, n):
+    """Relative to x Phi(x), tail and all.  fp32: t 3 e, its polynomial 4 e and a fit of
+    0.64 (1 + |x|) e, two products 2 e, the exponential 2 e, the sum e, and the exponent's
+    rounding of 4 e relative to x^2 / 2; bf16: a fit within min(5.7e-7 e^(1.5 |x|), 2.8e-3)."""
+    api = _api()
+    _say("gelu", dt, R, n)
+    v, out = _gelu_sweep(api, R, n, DT[dt])
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[0], out[r]) for r in range(1, R))
+    got = out[0].double().cpu()
+    ref = 0.5 * v * torch.special.erfc(-v * 0.5 ** 0.5)
+    a = v.abs()
+    bound = (13 + a + 2 * a * a) * E32
+    if dt == "bf16":
+        bound = bound + torch.clamp(5.7e-7 * torch.exp(1.5 * a), max=2.8e-3) + U[DT[dt]]
+    off = (got - ref).abs() / ref.abs().clamp(min=1e-300)
+    mid = slice(0, n - 8)
+    assert (off <= bound)[mid].all(), (v[mid][(off > bound)[mid]][:4], float((off / bound)[mid].max()))
+    assert got[-8:].tolist()[:2] == [0.0, 0.0] and (got[-8:] - ref[-8:]).abs()[:4].max() <= 2e-32
+    assert got[-4:-2].abs().max() <= 1e-36 and got[-1] == 0
+    assert got[-2] == v[-2].to(DT[dt]).double()

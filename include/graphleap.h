@@ -469,7 +469,8 @@ gl_status gl_layer_norm(const void* x, int R, int C, long long ldx, const void* 
  *   dx [R, C] (dt), contiguous; dgamma, dbeta [C] fp32.  Any of the three may
  *   be NULL (not all): it is then not computed.
  *   workspace: gl_layer_norm_backward_workspace_bytes(R, C, dt) bytes (0 for few
- *   rows: NULL will do), 16-byte aligned, disjoint from every other argument; not
+ *   rows: NULL will do; at most 32 MiB, or R C / 4 for rows of more than 2048 vectors
+ *   of 16 bytes), 16-byte aligned, disjoint from every other argument; not
  *   needed (NULL) when dgamma and dbeta are NULL.
  * Outputs must not overlap inputs or each other.  Limits and errors as
  * gl_layer_norm, and GL_ERR_WORKSPACE.

@@ -326,7 +326,8 @@ __global__ __launch_bounds__(512) void norm_grad_few_kernel(NormGradArgs a, int 
 }
 
 // Rows shorter than a chunk or longer than the largest tile: dx a workgroup a row,
-// value by value; the sums over rows by columns, a thread each.
+// value by value; the sums over rows by columns, a thread each, eight rows under way at a
+// time.  A single group of rows has all of them, and writes the sums themselves.
 template <int DT>
 __global__ __launch_bounds__(256) void norm_grad_any_kernel(NormGradArgs a) {
   using T = Chunk<DT>;
@@ -358,11 +359,27 @@ __global__ __launch_bounds__(256) void norm_grad_any_cols_kernel(NormGradArgs a)
   const int c = blockIdx.x * 256 + threadIdx.x, C = a.C;
   if (c >= C) return;
   float sg = 0.f, sb = 0.f;
-  for (long long r = blockIdx.y; r < a.R; r += gridDim.y) {
-    const float d = T::load1(static_cast<const char*>(a.dy) + r * a.lddy * T::kSize, c);
-    const float f = T::load1(static_cast<const char*>(a.x) + r * a.ldx * T::kSize, c);
-    sg = fmaf(d, (f - a.mean[r]) * a.rstd[r], sg);
-    sb += d;
+  constexpr int U = 8;
+  for (long long r0 = blockIdx.y; r0 < a.R; r0 += U * (long long)gridDim.y) {
+    float d[U], f[U], mean[U], rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long r = min(r0 + u * (long long)gridDim.y, a.R - 1LL);
+      d[u] = T::load1(static_cast<const char*>(a.dy) + r * a.lddy * T::kSize, c);
+      f[u] = T::load1(static_cast<const char*>(a.x) + r * a.ldx * T::kSize, c);
+      mean[u] = a.mean[r], rstd[u] = a.rstd[r];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + u * (long long)gridDim.y < a.R) {
+        sg = fmaf(d[u], (f[u] - mean[u]) * rstd[u], sg);
+        sb += d[u];
+      }
+  }
+  if (gridDim.y == 1) {
+    if (a.dgamma) a.dgamma[c] = sg;
+    if (a.dbeta) a.dbeta[c] = sb;
+    return;
   }
   float* p = a.part + (size_t)blockIdx.y * 2 * C;
   p[c] = sg;
@@ -373,7 +390,7 @@ namespace {
 
 struct Plan {
   const void* fn;  // null: value by value
-  int threads, groups, grid;  // grid 0: the one launch for few rows
+  int threads, groups, grid;  // grid 0: the one launch for few rows; value by value: groups of rows
 };
 
 // Up to so many rows take one launch.  Its column workgroups add R / 64 rows a lane, so
@@ -396,7 +413,13 @@ Plan plan(int R, int C) {
     const int g = most > 256 ? std::min(std::max(R / 8, 256), most) : most;
     return Plan{fn, threads, groups, (int)std::min<long long>(((long long)R + groups - 1) / groups, g)};
   };
-  if (C < E || n > 2048) return Plan{nullptr, 256, 1, std::min(R, 256)};
+  if (C < E) return Plan{nullptr, 256, 1, std::min(R, 256)};
+  // Wide rows fill the GPU by their columns (33 workgroups and more): 32 rows and more a group, so
+  // that the groups' sums stay within an eighth of x and dy.  us, this (a group a row, up to
+  // 256 of them, which at 256 x 2^20 takes 2 GiB of sums):
+  //   256 x 2^20   bf16 4160 (5290)  fp32 4250 (5300)    100 x 40000  bf16 76 (108)  fp32 89 (99)
+  //   300 x 20000  bf16 54 (76)      fp32 68 (77)        40 x 8200    bf16 10.8 (10.6)  fp32 17 (20)
+  if (n > 2048) return Plan{nullptr, 256, 1, std::min(std::max(R / 32, 1), 256)};
   if (R <= (n > 128 ? kFewWide : n > 96 ? kFewMid : kFewRows) && n <= 1024) {
     if (n <= 16) return Plan{(const void*)&norm_grad_few_kernel<DT, 16, 1>, 512, 32, 0};
     if (n <= 64) return Plan{(const void*)&norm_grad_few_kernel<DT, 64, 1>, 512, 8, 0};
@@ -455,7 +478,7 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
       e = hipLaunchKernel((const void*)&norm_grad_any_cols_kernel<DT>, dim3((a.C + 255) / 256, p.grid),
                           dim3(256), argv, 0, stream);
   }
-  if (e != hipSuccess || !sums) return e;
+  if (e != hipSuccess || !sums || (!p.fn && p.grid == 1)) return e;
   constexpr int kMost = 1 << 20;  // workgroups a launch: fewer than 2^32 threads
   for (int c = 0; c < 2 * a.C; c += 32 * kMost)
     norm_grad_sum_kernel<<<std::min((2 * a.C - c + 31) / 32, kMost), 1024, 0, stream>>>(part, p.grid, a.C, c,
@@ -466,8 +489,8 @@ hipError_t launch_grad(NormGradArgs a, hipStream_t stream) {
 }  // namespace
 
 size_t norm_grad_ws_bytes(int R, int C, int dt_bf16) {
-  const int grid = dt_bf16 ? plan<1>(R, C).grid : plan<0>(R, C).grid;
-  return (size_t)grid * 2 * C * 4;
+  const Plan p = dt_bf16 ? plan<1>(R, C) : plan<0>(R, C);
+  return !p.fn && p.grid == 1 ? 0 : (size_t)p.grid * 2 * C * 4;
 }
 
 hipError_t launch_norm_grad(const NormGradArgs& a, int dt_bf16, hipStream_t stream) {

@@ -669,3 +669,30 @@ def test_gelu_over_its_range(dt, R, n):
     assert got[-8:].tolist()[:2] == [0.0, 0.0] and (got[-8:] - ref[-8:]).abs()[:4].max() <= 2e-32
     assert got[-4:-2].abs().max() <= 1e-36 and got[-1] == 0
     assert got[-2] == v[-2].to(DT[dt]).double()
+
+
+# rows wider than the tiles: one group of rows, several with and without a rest, and more
+# columns than one launch of the sums' kernel has threads for
+@pytest.mark.parametrize("dt,R,C", [("bf16", 33, 16385), ("f32", 63, 8193), ("bf16", 64, 16391), ("f32", 300, 9001),
+                                    ("bf16", 1001, 17000), ("bf16", 64, 2 ** 24 + 9)])
+def test_gradient_of_wide_rows_in_groups(dt, R, C):
+    api = _api()
+    _say("gradient, wide rows", dt, R, C)
+    g = torch.Generator(device="cuda").manual_seed(R)
+    x, dy = (torch.randn(R, C, generator=g, device="cuda").to(DT[dt]) for _ in range(2))
+    gamma = (1 + 0.3 * torch.randn(C, generator=g, device="cuda")).to(DT[dt])
+    _, mean, rstd = api.layer_norm(x, gamma, stats=True)
+    dx, dg, db = api.layer_norm_backward(dy, x, mean, rstd, gamma)
+    only_g = api.layer_norm_backward(dy, x, mean, rstd, gamma, need=(False, True, False))[1]
+    only_b = api.layer_norm_backward(dy, x, mean, rstd, gamma, need=(False, False, True))[2]
+    torch.cuda.synchronize()
+    assert torch.equal(dg, only_g) and torch.equal(db, only_b)
+    n = (R / 16 + 259) * E32
+    step = 2 ** 20
+    for c in range(0, C, step):
+        cols = slice(c, c + step)
+        d = dy[:, cols].double()
+        xh = (x[:, cols].double() - mean.double()[:, None]) * rstd.double()[:, None]
+        assert ((dg[cols].double() - (d * xh).sum(0)).abs() <= n * (d * xh).abs().sum(0)).all(), c
+        assert ((db[cols].double() - d.sum(0)).abs() <= n * d.abs().sum(0)).all(), c
+    assert torch.isfinite(dx).all()

@@ -113,3 +113,18 @@ def test_linear_q8_refusals():
     for bad in (dict(out=P(0, 16)), dict(out=P(1, 16)), dict(out=P(2, 16)), dict(out=P(3, 16)), dict(out=P(4, 16)),
                 dict(res=P(5, 16))):
         assert _lin(**bad) == "GL_ERR_ALIAS", bad
+
+
+def test_layer_norm_backward_workspace_stays_small():
+    """32 MiB, or an eighth of dy and x (as bf16) where rows are wider than 2048 vectors."""
+    f = api.lib().gl_layer_norm_backward_workspace_bytes
+    widths = sorted({w + d for e in range(27) for w in (1 << e,) for d in (-1, 0, 1) if w + d > 0} | {80, 1001, 2560, 20000})
+    for dt, wide in ((0, 2048 * 4), (1, 2048 * 8)):
+        for C in widths:
+            for R in (1, 2, 31, 32, 33, 63, 64, 100, 256, 1000, 5000, 100352, 1 << 20, 1 << 30):
+                if R * C > 1 << 40:
+                    continue
+                n = f(R, C, dt)
+                assert 0 <= n <= max(32 << 20, R * C // 4 if C > wide else 0), (R, C, dt, n)
+                if C > wide and R < 64:
+                    assert n == 0, (R, C, dt, n)

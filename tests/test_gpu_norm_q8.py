@@ -696,3 +696,28 @@ def test_gradient_of_wide_rows_in_groups(dt, R, C):
         assert ((dg[cols].double() - (d * xh).sum(0)).abs() <= n * (d * xh).abs().sum(0)).all(), c
         assert ((db[cols].double() - d.sum(0)).abs() <= n * d.abs().sum(0)).all(), c
     assert torch.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [5, 77, 192, 1000, 1001, 2561, 6000, 20000, 65535])
+def test_rows_of_one_value_are_beta(dt, C):
+    """Values of eight bits: up to 2^16 of them add up exactly in fp32, the mean is their
+    value, and nothing is left of the row but beta."""
+    api = _api()
+    _say("rows of one value", dt, C)
+    vals = torch.tensor([3.0, -1000.0, 99840.0, 2.0 ** 60 * 1.9921875, 1.5 * 2.0 ** -60, 0.0], device="cuda")
+    x = vals[:, None].expand(6, C).to(DT[dt]).contiguous()
+    g = np.random.default_rng(C)
+    gamma, beta = _vec(g, C, DT[dt], 1.0), _vec(g, C, DT[dt])
+    y, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
+    n, b = api.layer_norm_q8(x, gamma, beta), api.quantize_rows(beta)
+    torch.cuda.synchronize()
+    assert torch.equal(mean, vals)
+    assert ((rstd - 1e-5 ** -0.5).abs() <= 4 * E32 * 1e-5 ** -0.5).all()
+    assert torch.equal(y, beta.expand(6, C))
+    assert (n.scale == b.scale).all() and (n.q[:, :C] - b.q[:C]).abs().max() <= 1
+    # the mean of a row with an infinity is that infinity
+    x[1, C // 2], x[2, 0] = float("inf"), float("-inf")
+    y, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
+    torch.cuda.synchronize()
+    assert torch.isposinf(mean[1]) and torch.isneginf(mean[2]) and torch.isnan(y[1:3]).all()

@@ -325,6 +325,12 @@ def q8_row_bytes(K: int) -> int:
     return n
 
 
+def _count(name: str, *ns: int):
+    """The library's counts are 32 bits: a larger one is refused here, not passed on cut short."""
+    if max(ns) > 0x7fffffff:
+        raise GraphLeapError(name, 2, f"counts {ns} past 2^31 - 1")
+
+
 def _rows(x: torch.Tensor):
     """(R, C, ld) of a device tensor whose leading axes are rows a uniform stride apart."""
     if not x.is_cuda or x.dim() < 1:
@@ -333,8 +339,10 @@ def _rows(x: torch.Tensor):
         raise ValueError(f"tensors are on {x.device}, the current device is {torch.cuda.current_device()}")
     sh = x.shape
     C = sh[-1]
+    R = x.numel() // C if C else 0
+    _count("rows", R, C)
     if x.is_contiguous():
-        return (x.numel() // C if C else 0), C, C
+        return R, C, C
     st = x.stride()
     if C > 1 and st[-1] != 1:
         raise ValueError("the last axis of rows must be contiguous")
@@ -348,7 +356,7 @@ def _rows(x: torch.Tensor):
             rows *= n
         else:
             raise ValueError(f"rows of shape {tuple(sh)} and strides {st} are not a uniform stride apart")
-    return x.numel() // C if C else 0, C, C if ld is None else ld
+    return R, C, C if ld is None else ld
 
 
 def _like(name: str, t, shape: tuple, dtype, x: torch.Tensor):
@@ -512,6 +520,7 @@ def linear_q8(x: Q8Rows, W: Q8Rows, bias: torch.Tensor | None = None, act_out: i
     if W.q.dim() != 2 or x.K != W.K:
         raise ValueError(f"linear_q8: rows {tuple(x.shape)} do not match weights {tuple(W.shape)}")
     Cout, lead = W.q.shape[0], x.q.shape[:-1]
+    _count("linear_q8", Cout)
     want = (x.K + 15) // 16 * 16
     _like("x.q", x.q, lead + (want,), torch.int8, x.q)
     _like("x.scale", x.scale, lead, torch.float32, x.q)

@@ -128,3 +128,56 @@ def test_layer_norm_backward_workspace_stays_small():
                 assert 0 <= n <= max(32 << 20, R * C // 4 if C > wide else 0), (R, C, dt, n)
                 if C > wide and R < 64:
                     assert n == 0, (R, C, dt, n)
+
+
+class _Big:
+    """Stands in for a contiguous device tensor of any size; its address is never read."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, shape, dtype, at):
+        self.shape, self.dtype, self.at = torch.Size(shape), dtype, at
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def is_neg(self):
+        return False
+
+    def data_ptr(self):
+        return self.at
+
+    def record_stream(self, s):
+        pass
+
+
+def test_counts_past_32_bits_are_refused(monkeypatch):
+    """2^32 + 5 rows are not taken for 5: ctypes cuts a count to 32 bits without a word."""
+    class Stream:
+        cuda_stream = 0
+    monkeypatch.setattr(api, "_native", type("No", (), {}))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    n, bf, far = (1 << 32) + 5, torch.bfloat16, 1 << 45
+    x, out = _Big((n, 1), bf, far), _Big((n, 1), bf, 2 * far)
+    q = api.Q8Rows(_Big((n, 16), torch.int8, 3 * far), _Big((n,), torch.float32, 4 * far), 1)
+    few = api.Q8Rows(_Big((3, 16), torch.int8, 5 * far), _Big((3,), torch.float32, 6 * far), 1)
+    calls = [lambda: api.layer_norm(x, out=out, stream=Stream),
+             lambda: api.layer_norm_backward_workspace(x),
+             lambda: api.layer_norm_backward(x, x, q.scale, q.scale, need=(False, True, True),
+                                             ws=api.Workspace(0, "cpu"), stream=Stream),
+             lambda: api.quantize_rows(x, out=q, stream=Stream),
+             lambda: api.layer_norm_q8(x, out=q, stream=Stream),
+             lambda: api.linear_q8(q, few, out=_Big((n, 3), bf, 7 * far), stream=Stream),
+             lambda: api.linear_q8(few, q, out=_Big((3, n), bf, 7 * far), stream=Stream)]
+    for i, call in enumerate(calls):
+        with pytest.raises(api.GraphLeapError) as e:
+            call()
+        assert e.value.status == 2, i

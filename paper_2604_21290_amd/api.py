@@ -337,6 +337,8 @@ def _rows(x: torch.Tensor):
         raise ValueError("rows must be a device tensor")
     if x.get_device() != torch.cuda.current_device():
         raise ValueError(f"tensors are on {x.device}, the current device is {torch.cuda.current_device()}")
+    if x.is_neg():
+        raise ValueError("rows are a negated view: resolve_neg() makes them a plain tensor")
     sh = x.shape
     C = sh[-1]
     R = x.numel() // C if C else 0
@@ -362,7 +364,9 @@ def _rows(x: torch.Tensor):
 def _like(name: str, t, shape: tuple, dtype, x: torch.Tensor):
     """An argument that must be contiguous and have this shape and type, on x's device."""
     if t is not None and (t.shape != shape or t.dtype != dtype or t.get_device() != x.get_device()
-                          or not t.is_contiguous()):
+                          or not t.is_contiguous() or t.is_neg()):
+        if t.is_neg():
+            raise ValueError(f"{name} is a negated view: resolve_neg() makes it a plain tensor")
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
                          f"{x.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t

@@ -115,3 +115,19 @@ def test_calls_without_the_shortcut_have_the_same_bits(monkeypatch):
     got = every()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_negated_views_are_refused():
+    """A view that torch holds as the negative of its memory is not read without its sign."""
+    api = _api()
+    x = torch.randn(6, 64, device="cuda")
+    neg, v = torch._neg_view(x), torch.randn(64, device="cuda")
+    _, mean, rstd = api.layer_norm(x, stats=True)
+    q = api.quantize_rows(x)
+    for call in (lambda: api.layer_norm(neg), lambda: api.quantize_rows(neg), lambda: api.layer_norm_q8(neg),
+                 lambda: api.layer_norm(x, torch._neg_view(v)), lambda: api.layer_norm_backward(neg, x, mean, rstd),
+                 lambda: api.layer_norm_backward(x, x, torch._neg_view(mean), rstd),
+                 lambda: api.linear_q8(q, q, bias=torch._neg_view(v[:6]), dtype=torch.float32)):
+        with pytest.raises(ValueError, match="negat"):
+            call()
+    assert torch.equal(api.layer_norm(neg.resolve_neg()), api.layer_norm(-x))

@@ -4,6 +4,7 @@
 #include <stdio.h>
 
 #include <climits>
+#include <cmath>
 #include <initializer_list>
 #include <mutex>
 #include <string>
@@ -1267,6 +1268,8 @@ gl::RowArgs row_args(const void* x, int R, int C, long long ldx, const void* gam
   a.C = C;
   a.eps = eps;
   a.inv_c = (float)(1.0 / C);
+  a.mean_hi = std::nextafterf((float)(1.0 / C), 0.f);
+  a.mean_lo = (float)(1.0 / C - a.mean_hi);
   return a;
 }
 

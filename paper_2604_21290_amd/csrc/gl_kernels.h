@@ -72,6 +72,7 @@ struct RowArgs {
   float* scale;              // [R]
   int R, C, Kp;
   float eps, inv_c;          // inv_c = 1 / C
+  float mean_hi, mean_lo;    // 1 / C in two parts: 24 bits that stay below it, and the rest
 };
 
 struct NormGradArgs {

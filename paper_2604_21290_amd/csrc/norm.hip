@@ -19,13 +19,12 @@ namespace gl {
 
 enum { kNorm = 0, kNormQ8 = 1, kQ8 = 2 };
 
-// sum / C, rounded once: the product with 1 / C, which is rounded itself, and a step on its
-// remainder.  So a row of equal values whose sum is exact has them as its mean (by the product
-// alone 1000 channels of 1e5 were 0.008 off it, and the norm 0.93 for 0).  An infinite
-// sum, whose remainder is a NaN, stays one.
+// sum / C by 1 / C in two parts, so that the quotient is rounded as if once and a row of
+// equal values whose sum is exact has them as its mean (by a rounded 1 / C alone 1000
+// channels of 1e5 were 0.008 off it, and the norm 0.93 for 0).  Both parts are positive: an
+// infinite sum stays one.
 __device__ __forceinline__ float row_mean(float sum, const RowArgs& a) {
-  const float m = sum * a.inv_c;
-  return fmaf(fmaxf(fmaf(-m, (float)a.C, sum), -3.4e38f), a.inv_c, m);
+  return fmaf(sum, a.mean_hi, sum * a.mean_lo);
 }
 
 // LPR lanes hold a row, VPL chunks each.  A workgroup takes many rows: gamma and beta

@@ -450,7 +450,7 @@ gl_status gl_vig_stack(gl_lookahead_t h, const void* x0, int B, int H, int W, in
  *   out [R, C] (dt), contiguous.  mean, rstd [R] fp32 or NULL: what
  *   gl_layer_norm_backward needs.  Outputs must not overlap x, gamma or beta.
  * A row with a NaN or an infinity is NaN.  Squares are fp32: deviations past 1e19
- * overflow.
+ * overflow, and below 1e-19 (which matter where eps is as small) lose bits.
  * Limits: 1 <= R <= 2^30, 1 <= C <= 2^29, R * C <= 2^40.
  * Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype), GL_ERR_BAD_SHAPE (sizes,
  * ldx < C, eps negative or not finite), GL_ERR_ALIGNMENT, GL_ERR_ALIAS, GL_ERR_HIP.

@@ -27,9 +27,22 @@ __device__ __forceinline__ float row_mean(float sum, const RowArgs& a) {
   return fmaf(sum, a.mean_hi, sum * a.mean_lo);
 }
 
+// 1 / sqrt(var + eps) of the sum of squares.  The hardware's root takes a subnormal for zero:
+// where eps leaves room for one (TINY), a small argument is scaled by a power of four first.
+// A variant of its own, since the four instructions a row take 3 % of 100352 x 80 (7.70 us
+// for 7.50), and a branch on eps in their place as much.
+constexpr float kTinyEps = 0x1p-100f;
+template <bool TINY>
+__device__ __forceinline__ float row_rstd(float sq, const RowArgs& a) {
+  const float v = fmaf(sq, a.inv_c, a.eps);
+  if (!TINY) return __builtin_amdgcn_rsqf(v);
+  const bool tiny = v < kTinyEps;
+  return __builtin_amdgcn_rsqf(tiny ? v * 0x1p100f : v) * (tiny ? 0x1p50f : 1.f);
+}
+
 // LPR lanes hold a row, VPL chunks each.  A workgroup takes many rows: gamma and beta
 // stay in registers, and a row's loads are under way while the one before is worked on.
-template <int DT, int MODE, int LPR, int VPL>
+template <int DT, int MODE, int LPR, int VPL, bool TINY>
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, GROUPS = 256 / LPR;
@@ -102,8 +115,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
       for (int v = 0; v < VPL; ++v)
 #pragma unroll
         for (int j = 0; j < E; ++j) f[v][j] -= mean;
-      const float sq = sum([](float s, float x) { return fmaf(x, x, s); }, slots[turn][1]);
-      const float rstd = __builtin_amdgcn_rsqf(fmaf(sq, a.inv_c, a.eps));
+      const float rstd = row_rstd<TINY>(sum([](float s, float x) { return fmaf(x, x, s); }, slots[turn][1]), a);
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
         float w[E], b[E];
@@ -162,7 +174,7 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
       const float d = T::load1(x, c) - mean;
       s = fmaf(d, d, s);
     }
-    rstd = __builtin_amdgcn_rsqf(fmaf(sum_row<256>(s, slots[1]), a.inv_c, a.eps));
+    rstd = row_rstd<true>(sum_row<256>(s, slots[1]), a);
   }
   auto value = [&](int c) {
     const float v = T::load1(x, c);
@@ -194,8 +206,8 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
 // wave where that leaves one chunk a lane (100352 x 40 bf16, norm 6.0 us for 7.6), and
 // for 8 bits alone, which need no weights, up to three (100352 x 192 11.1 for 12.3; the
 // norm would take 17.4 for 15.3).
-template <int DT, int MODE>
-hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
+template <int DT, int MODE, bool TINY>
+hipError_t launch_row_tiny(const RowArgs& a, hipStream_t stream) {
   constexpr int E = Chunk<DT>::E;
   const int n = (a.C + E - 1) / E;
   void* argv[] = {const_cast<RowArgs*>(&a)};
@@ -205,7 +217,7 @@ hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
     const long long turns = (units + most - 1) / most;
     return hipLaunchKernel(fn, dim3((unsigned)((units + turns - 1) / turns)), dim3(256), argv, 0, stream);
   };
-#define GL_ROW(LPR, VPL) go((const void*)&row_kernel<DT, MODE, LPR, VPL>, 256 / LPR)
+#define GL_ROW(LPR, VPL) go((const void*)&row_kernel<DT, MODE, LPR, VPL, TINY>, 256 / LPR)
   if (a.C < E || n > 2048) return go((const void*)&row_any_kernel<DT, MODE>, 1);
   // the eight rows of a wave lie within 32 bits of the first
   const bool near = a.R == 1 || a.ldx < 1 << 27;
@@ -221,8 +233,15 @@ hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
   if (n <= 1024) return n <= 512 ? GL_ROW(256, 2) : n <= 768 ? GL_ROW(256, 3) : GL_ROW(256, 4);
   // two waves a SIMD: more workgroups would load gamma and beta for a row each (4096 x 8192
   // fp32: 55 us, 91 with 16 a CU)
-  return go((const void*)&row_kernel<DT, MODE, 256, 8>, 1, 2);
+  return go((const void*)&row_kernel<DT, MODE, 256, 8, TINY>, 1, 2);
 #undef GL_ROW
+}
+
+template <int DT, int MODE>
+hipError_t launch_row_mode(const RowArgs& a, hipStream_t stream) {
+  if constexpr (MODE != kQ8)
+    if (a.eps < kTinyEps) return launch_row_tiny<DT, MODE, true>(a, stream);
+  return launch_row_tiny<DT, MODE, false>(a, stream);
 }
 
 hipError_t launch_layer_norm(const RowArgs& a, int dt_bf16, hipStream_t stream) {

@@ -721,3 +721,25 @@ def test_rows_of_one_value_are_beta(dt, C):
     y, mean, rstd = api.layer_norm(x, gamma, beta, stats=True)
     torch.cuda.synchronize()
     assert torch.isposinf(mean[1]) and torch.isneginf(mean[2]) and torch.isnan(y[1:3]).all()
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40])
+@pytest.mark.parametrize("C,R", [(3, 4), (80, 4), (192, 4), (2560, 4), (20000, 4), (20, 16400), (120, 5000), (1001, 1000)])
+def test_variances_below_the_normal_range(C, R, eps):
+    """A subnormal variance with an eps as small has a root: squares and their sum are then
+    off by 2^-150 each, 2^-148 of the variance altogether at most."""
+    api = _api()
+    _say("subnormal variances", C, R, eps)
+    g = np.random.default_rng(C)
+    size = np.resize([1e-17, 1e-18, 1e-19, 1e-20], (R, 1))
+    x = torch.from_numpy(g.standard_normal((R, C)) * size).float().cuda()
+    y, mean, rstd = api.layer_norm(x, eps=eps, stats=True)
+    q = api.layer_norm_q8(x, eps=eps)
+    torch.cuda.synchronize()
+    xf = _f64(x)
+    ry, rm, rr = Q.layer_norm_ref(xf, None, None, float(np.float32(eps)))
+    low = 2.0 ** -148 * rr ** 2
+    _within("rstd", _f64(rstd), rr, (80 + C / 256 + 8) * E32 * rr + low * rr
+            + rr ** 3 * ((80 + C / 256) * E32 * np.abs(xf).mean(-1)) ** 2)
+    _within("y", _f64(y), ry, _y_bound(xf, ry, rm, rr, None, None) + (low[:, None] + E32) * np.abs(ry))
+    assert (q.q[:, :C].abs().amax(1) == 127).all() and torch.isfinite(q.scale).all()

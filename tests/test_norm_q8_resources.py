@@ -53,3 +53,20 @@ def test_no_spills(tmp_path):
             if "PipeCfgILi128ELi128E" in name or "PipeCfgILi64ELi64ELi2ELi2ELi2E" in name:
                 assert waves >= 4, (name, waves)
     assert all(counts.values()), counts
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
+def test_strips_have_the_waves_they_ask_for(tmp_path):
+    """A strip kernel's workgroups of four waves are as many a CU as StripCfg reckons, by the
+    LDS of W's columns and by the registers: so many waves a SIMD."""
+    found = 0
+    for name, (scratch, waves, _) in _kernels("gemm_q8.hip", tmp_path).items():
+        m = re.search(r"StripCfgILi(\d+)ELi(\d+)ELi(\d+)E", name)
+        if not m:
+            continue
+        found += 1
+        bf16, ks, tn = map(int, m.groups())
+        lds = (ks + 1) // 2 * 16 * tn * 128 + 2 * 16 * tn * 4
+        regs = 4 * (ks + 2 * tn) + 2 * tn * (1 if bf16 else 2) + 24
+        assert scratch == 0 and waves >= min(160 * 1024 // lds, 512 // regs), (name, waves)
+    assert found == 2 * 2 * 5 * 2  # types, with and without GELU, steps of K, columns

@@ -489,7 +489,8 @@ int gl_q8_row_bytes(int K);
 /* ---------------------------------------------------------------------------
  * gl_quantize_rows -- rows to 8 bits, symmetric, each with its own scale:
  *   top = max_k |x[r, k]|;  scale[r] = top / 127;  q[r, k] = rne(127 x[r, k] / top)
- * (the correctly rounded fp32 quotient, ties to even).  A row with top < 2^-118
+ * (the correctly rounded fp32 quotient, ties to even; of fp32 rows 127 x is rounded to
+ * fp32 before it is divided).  A row with top < 2^-118
  * counts as zero: q = 0, scale = 0.  A row with a NaN or an infinity has q = 0
  * and scale = NaN, so that what is computed from it is NaN.
  *   x [R, K] (dt), rows ldx apart; q [R, Kp] int8, scale [R] fp32; neither may

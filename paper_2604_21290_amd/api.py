@@ -1,7 +1,9 @@
 """Thin ctypes binding of libgraphleap.so (include/graphleap.h).
 
 Argument marshalling only: tensors are passed as device pointers, streams as
-hipStream_t; every step of the path runs in the library's HIP kernels.  The
+hipStream_t; every step of the path runs in the library's HIP kernels.  No call
+is recorded by autograd: its outputs are detached, also where an input requires
+a gradient.  The
 binding allocates outputs and workspaces with torch when the caller does not
 pass them (PyTorch supplies device memory and streams, nothing else).
 
@@ -298,7 +300,8 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None,
 # ---------------------------------------------------------------------------
 # layer norm and 8-bit layers: these calls take a few microseconds on the device, so
 # their ordinary form (current stream, outputs allocated here) goes through native
-# marshalling first, which returns None for anything else
+# marshalling first, which returns None for anything else.  Like every call of this module
+# they are not recorded by autograd: a gradient is asked for by layer_norm_backward
 # ---------------------------------------------------------------------------
 class Q8Rows:
     """8-bit rows (gl_quantize_rows): q [..., Kp] int8, whose last Kp - K bytes
@@ -397,7 +400,8 @@ def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None,
                out: torch.Tensor | None = None, stream=None):
     """(x - mean) * rstd * gamma + beta over the last axis (gl_layer_norm).  x may
     be a slice of wider rows.  stats: return (out, mean, rstd), the row statistics
-    in float32 that layer_norm_backward takes."""
+    in float32 that layer_norm_backward takes.  The outputs are detached: inside an autograd
+    graph, call this and layer_norm_backward from a torch.autograd.Function."""
     if stream is None and out is None:
         r = (_native or _calls()).layer_norm(x, gamma, beta, eps, stats)
         if r is not None:
@@ -514,7 +518,8 @@ def linear_q8(x: Q8Rows, W: Q8Rows, bias: torch.Tensor | None = None, act_out: i
               residual: torch.Tensor | None = None, dtype=torch.bfloat16,
               out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """out[..., Cout] = act_out(x W^T + bias) + residual of 8-bit rows x and weights
-    W [Cout, K] (gl_linear_q8); bias, residual and out are in `dtype`."""
+    W [Cout, K] (gl_linear_q8); bias, residual and out are in `dtype`.  The output is
+    detached; 8-bit rows have no gradient."""
     if stream is None and out is None and (dtype is torch.bfloat16 or dtype is torch.float32):
         r = (_native or _calls()).linear_q8(x.q, x.scale, x.K, W.q, W.scale, W.K, bias, act_out, residual,
                                             dtype is torch.bfloat16)

@@ -130,13 +130,14 @@ __device__ __forceinline__ void store1(void* p, size_t i, float f) {
 //     one wave a SIMD has the tile (64 x 64), 0.2 with two groups (64 x 32), 0.12 with
 //     four (32 x 32).
 // Tiles are walked so that the 32 that an XCD works on at a time are 8 x 4.
-// What bounds it: at 8192 x 8192 x 8192 (420-430 us, 2.6 POP/s; the library's int8
+// What bounds it: at 8192 x 8192 x 8192 (420-435 us, 2.6 POP/s; the library's int8
 // product 440) the matrix cores are busy 66 % of the cycles, at a clock that falls to
 // 1.7-1.8 GHz on random data; with all loads from L2's hottest lines 397 us, so the trip
 // to memory costs 8 %.  Its loads alone take 360 us, its products alone 346: each stage's
 // loads take about as long as its products, and LDS holds one stage ahead.  Tried and slower there: MFMA 32x32x32 (471 us), stages of 64
-// bytes in four buffers (446), 256 x 128 tiles in three buffers (478), four waves of
-// 128 x 128 (886: operands move between the register files).
+// bytes in four buffers (446), 256 x 128 tiles in three buffers (478; also 28.0-30.8 at
+// 12544 x 2560 x 640, where 128 x 128 take 26.9-28.1, and no faster at ten sizes more), four
+// waves of 128 x 128 (886: operands move between the register files).
 // ---------------------------------------------------------------------------
 template <int BM_, int BN_, int WR_, int WC_, int NBUF_, int KG_ = 1>
 struct PipeCfg {
@@ -431,10 +432,11 @@ hipError_t launch_pipe_q8(const GemmQ8Args& a, hipStream_t stream) {
 // waves take strips of 16 rows, each for itself, with no barrier between them.  A strip
 // goes straight to registers; each 64 bytes of K of the wave's next strip are requested
 // when this one's have been multiplied, and its residual after this one's results.  So
-// every wave has a strip on its way from memory (5 to 7 waves a SIMD), where the tiles
-// above load W with every tile and meet at a barrier every 128 bytes of K.
-//   100352x320x80 with residual 13.7 us (16.4 by tiles), 64 MB of memory traffic;
-//   6272x192x768 with GELU 7.3 (8.3), of which 3.4 are the GELU's instructions.
+// every wave has a strip on its way from memory (room for 4 to 7 waves a SIMD), where the
+// tiles above load W with every tile and meet at a barrier every 128 bytes of K.
+//   100352x320x80 with residual 13.7 us (16.3 by tiles), 64 MB of memory traffic, three waves
+//   a SIMD of room for four; 6272x192x768 with GELU 7.5 (8.4), of which 3.4 are the GELU's
+//   instructions.
 // Loading both halves of a 128-byte line together changed nothing; strips of 32 rows
 // leave too few waves (6272x192x192 4.0 for 3.6).
 // ---------------------------------------------------------------------------
@@ -641,43 +643,45 @@ hipError_t launch_rows_q8(const GemmQ8Args& a, hipStream_t stream) {
 // The tile for a layer, by what each takes for one round of all CUs, in us: so much for
 // every 128 bytes of K, for the rest of a tile, and for a GELU or a residual in its
 // epilogue.  A CU's tiles share it, so part of a round takes its part of the time, but
-// no less than the latency of one tile.  Fitted to (us, plain / GELU / residual):
+// no less than the latency of one tile.  Fitted to these (us a call in a row of calls on
+// three inputs in turn, bf16, plain / GELU / residual):
 //                    256 x 256         128 x 128          64 x 64, 4 a CU    64 x 64, 2 a CU
-//   8192x8192x8192   420               528                853                874
-//   16384x4096x4096  237               284                434                447
-//   12544x640x2560   32.5/46.0/57.9 *  32.9/42.7/50.4 *   40.8/52.7/60.7     50.0/59.2/65.3
-//   12544x2560x640   37.1/42.4/41.1    26.4/28.3/28.4 *   36.4/37.3/39.5     36.5/39.5/38.8
-//   25088x192x768    21.0/31.4/36.9    14.9/19.8/19.1     17.0/21.6/20.2     20.5/25.8/24.1
-//   100352x80x320    29.2/51.0/65.2    20.2/31.9/37.1     20.5/29.8/37.2     26.7/35.6/44.8
-//   6272x192x768     11.6/17.0/17.0     8.0/ 9.7/ 9.7      7.4/ 8.4/ 8.8      8.3/ 9.7/ 9.9
-//   1000x8000x1000   77.5              45.6               31.1               19.8 *
+//   8192x8192x8192   435               549                834                852
+//   16384x4096x4096  232               287                423                433
+//   12544x640x2560   32.5/45.0/57.5 *  35.0/43.8/49.4 *   43.1/49.5/60.7     48.9/57.0/64.9
+//   12544x2560x640   35.9/42.0/40.0    27.2/28.8/28.4 *   38.4/39.4/39.7     38.7/40.0/40.2
+//   25088x192x768    21.3/33.3/34.5    15.6/22.1/20.7     17.9/23.6/21.5     20.9/26.6/24.4
+//   100352x80x320    29.2/54.2/64.6    20.9/34.0/36.4     21.7/31.0/36.4     27.0/37.6/43.5
+//   6272x192x768     11.5/18.0/17.0     8.0/10.1/ 9.8      7.3/ 8.4/ 8.8      8.1/ 9.5/ 9.7
+//   1000x8000x1000   85.7              47.1               31.2               18.7 *
 // (* the one taken: at 12544x640x2560 the larger tile without GELU or residual; strips
 // take three of the others).  The
 // kernel for few rows where its 16 x 16 outputs are few or K is short (us, against
-// 64 x 64 tiles): 1x640x2560 2.4 (4.0), 1x8192x8192 12.8 (16.7), 64x2560x640 4.3 (7.3),
-// 128x8192x512 9.6 (16.5), 196x192x768 2.5 (3.7), 1024x2560x64 4.8 (7.3), 196x320x1280
-// 3.4 (3.9).  And where its own estimate, by the bytes that its units read (rows a multiple
-// of 512 bytes apart meet in the same channels), is below the tiles': 777x1001x333 4.9 (5.2).
+// the better 64 x 64 tiles): 1x640x2560 2.5 (4.4), 1x8192x8192 13.0 (16.9), 64x2560x640
+// 4.3 (7.4), 128x8192x512 9.6 (16.8), 196x192x768 2.6 (3.5), 1024x2560x64 4.6 (7.4),
+// 196x320x1280 3.5 (3.7).  And where its own estimate, by the bytes that its units read (rows
+// a multiple of 512 bytes apart meet in the same channels), is below the tiles': 777x1001x333
+// 4.9 (5.1).
 // Tiles for few outputs, 64 x 32 with K between two groups and 32 x 32 between four (us,
 // against 64 x 64, 2 a CU, and 16 x 16):
-//   64x4096x4096      7.9   7.3   (10.2, 16.9)      500x3000x500   7.7  6.0  (9.0,  9.3)
-//   128x4096x4096     8.1  10.5   (10.2, 30.4)      196x2560x640   5.8  5.3  (7.4,  8.1)
-//   871x4336x320     10.4  12.3   (13.2, 16.5)      784x4096x200   7.8  6.7 (10.1, 12.7)
-//   531x5531x891     11.9  14.1   (15.7, 30.1)      300x6000x300  12.6  9.4 (16.3, 11.6)
-//   256x4096x4096    13.1  17.8   (11.3, 58.8)
+//   64x4096x4096      8.0   7.5   (10.3, 17.0)      500x3000x500   7.7  6.1  (9.1,  9.6)
+//   128x4096x4096     8.2  10.8   (10.7, 30.9)      196x2560x640   5.8  5.2  (7.5,  8.1)
+//   871x4336x320     10.6  12.5   (13.2, 16.3)      784x4096x200   7.8  6.8 (10.3, 13.1)
+//   531x5531x891     12.1  14.3   (15.6, 29.8)      300x6000x300  12.6  9.4 (16.3, 11.2)
+//   256x4096x4096    14.4  17.9   (11.0, 58.9)
 //
 // Strips where K is short, against the best of the tiles (us, plain / GELU / residual):
-//   100352x320x80    11.7/16.0/13.7    15.0/18.6/16.3
-//   100352x80x320    17.1/27.2/36.9    20.8/31.1/37.5
-//   6272x192x768      5.9/ 7.3/ 7.7     7.2/ 8.4/ 8.8
-//   25088x320x320     9.7/11.8/10.9    11.6/13.5/13.3
-//   6272x192x192      3.6/ 4.4/ 4.1     4.3/ 4.9/ 4.5
+//   100352x320x80    11.9/15.9/13.7    14.8/18.0/16.3
+//   100352x80x320    17.9/27.6/35.3    20.5/30.6/36.5
+//   6272x192x768      6.0/ 7.5/ 7.8     7.3/ 8.4/ 8.8
+//   25088x320x320    10.8/12.3/11.0    12.2/13.9/13.7
+//   6272x192x192      3.5/ 4.3/ 4.1     4.3/ 4.9/ 4.5
 //   1200x320x320      3.5/ 3.9/ 3.6     3.7/ 4.2/ 3.9
 // Not taken: K past 320 (6272x384x384 6.1/7.0/7.1 for 5.7/6.4/6.7: each strip reads all of
-// W from LDS), rows of 256 bytes (25088x256x512 14.1/17.4/17.7 for 13.2/17.4/15.2), and
+// W from LDS), rows of 256 bytes (25088x256x512 14.9/17.8/17.5 for 13.6/17.8/15.9), and
 // wide or large outputs, which tiles of 128 columns write in longer runs (4096x128x4096
-// 13.0/17.6/17.3 for 12.2/17.0/16.5, 100352x80x320 fp32 45/46/66 for 36/41/64).  96
-// columns where one such strip is all (100352x320x80 by 64: 12.4/16.9/14.8).
+// 12.8/18.6/17.9 for 12.1/17.3/16.6, 100352x80x320 fp32 42/43/67 for 37/42/64).  96
+// columns where one such strip is all (100352x320x80 by 64: 12.6/16.8/15.4).
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t stream) {
   const long units = (long)((a.R + 15) / 16) * ((a.Cout + 15) / 16);

@@ -4,12 +4,12 @@
 // One kernel: a row is read once and stays in registers, in fp32, while its
 // statistics are taken (the mean first, then the squares of what is left, which
 // loses nothing to cancellation) and its top is found; then it is written once.
-// Memory bounds it: us (and TB/s of what it has to read and write; a copy of 1 GiB
-// reaches 5.3) in bf16, norm, 8 bits, norm to 8 bits:
-//   32768 x 2560   62.2 (5.4)   47.9 (5.3)   60.5 (4.2)
-//   100352 x 320   28.0 (4.6)   18.5 (5.2)   27.5 (3.5)
-//   100352 x 80     8.4 (3.8)    8.0 (3.0)   10.3 (2.3)
-//   6272 x 192      3.8 (1.3)    3.3 (1.1)    4.1 (0.9)
+// Memory bounds it: us a call in a row of calls on three inputs in turn (and TB/s of what it
+// has to read and write; a copy of 1 GiB reaches 5.3) in bf16, norm, 8 bits, norm to 8 bits:
+//   32768 x 2560   62.0 (5.4)   47.9 (5.3)   59.1 (4.3)
+//   100352 x 320   26.2 (4.9)   17.3 (5.6)   25.3 (3.8)
+//   100352 x 80     7.7 (4.2)    6.6 (3.7)    9.4 (2.6)
+//   6272 x 192      3.3 (1.5)    2.5 (1.4)    3.5 (1.0)
 // Small inputs take a launch and one trip to memory, about 3 us; the norm to 8 bits
 // has twice the arithmetic of the norm, which then shows.
 #include "gl_kernels.h"
@@ -200,12 +200,13 @@ __global__ __launch_bounds__(256) void row_any_kernel(RowArgs a) {
   }
 }
 
-// The lanes and chunks for rows of n chunks: at most three a lane, whose registers leave
-// three waves a SIMD and more.  Many short rows lie four to a wave, 16 lanes each: their
-// sums take four steps within 16 lanes, and a wave has more bytes in flight.  Eight to a
-// wave where that leaves one chunk a lane (100352 x 40 bf16, norm 6.0 us for 7.6), and
-// for 8 bits alone, which need no weights, up to three (100352 x 192 11.1 for 12.3; the
-// norm would take 17.4 for 15.3).
+// The lanes and chunks for rows of n chunks: at most three a lane up to 768 chunks, whose
+// registers leave four waves a SIMD and more; four up to 1024 (three and more) and eight
+// past that (two and more), where a workgroup has no more lanes.  Many short rows lie four
+// to a wave, 16 lanes each: their sums take four steps within 16 lanes, and a wave has more
+// bytes in flight.  Eight to a wave where that leaves one chunk a lane (100352 x 40 bf16,
+// norm 6.0 us for 7.6), and for 8 bits alone, which need no weights, up to three
+// (100352 x 192 11.1 for 12.3; the norm would take 17.4 for 15.3).
 template <int DT, int MODE, bool TINY>
 hipError_t launch_row_tiny(const RowArgs& a, hipStream_t stream) {
   constexpr int E = Chunk<DT>::E;
@@ -231,7 +232,7 @@ hipError_t launch_row_tiny(const RowArgs& a, hipStream_t stream) {
   if (n <= 192) return n <= 64 ? GL_ROW(64, 1) : n <= 128 ? GL_ROW(64, 2) : GL_ROW(64, 3);
   if (n <= 384) return n <= 256 ? GL_ROW(128, 2) : GL_ROW(128, 3);
   if (n <= 1024) return n <= 512 ? GL_ROW(256, 2) : n <= 768 ? GL_ROW(256, 3) : GL_ROW(256, 4);
-  // two waves a SIMD: more workgroups would load gamma and beta for a row each (4096 x 8192
+  // two workgroups a CU: more of them would load gamma and beta for a row each (4096 x 8192
   // fp32: 55 us, 91 with 16 a CU)
   return go((const void*)&row_kernel<DT, MODE, 256, 8, TINY>, 1, 2);
 #undef GL_ROW

@@ -5,10 +5,10 @@
 // averages, write dx, and each lane adds its channels' terms of dgamma and dbeta to
 // sums of its own over all rows that it meets.  A workgroup then adds its lanes'
 // sums and writes them to the workspace, and a second kernel adds the workgroups'.
-// Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16 32768 x 2560
-// 96 (5.2; 111 in a first run), 100352 x 320 39 (4.9), 100352 x 80 14.0 (3.4, of which
-// the second kernel and the gap before it take 4), 8193 x 1001 15.1 (3.2).  Few rows take
-// one launch.
+// Memory bounds it where rows are many: us (TB/s of dy, x and dx) in bf16, a call in a row of
+// calls on three inputs in turn, 32768 x 2560 98 (5.1; 111 in a first run), 100352 x 320
+// 43 (4.5), 100352 x 80 14.6 (3.3, of which the second kernel and the gap before it take 4),
+// 8193 x 1001 15.3 (3.2).  Few rows take one launch.
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"

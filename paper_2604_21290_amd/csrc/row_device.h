@@ -192,8 +192,8 @@ __device__ __forceinline__ uint32_t max_row(uint32_t v, uint32_t* slot) {
 // magnitude.  The quotient is the correctly rounded one, so that it ties exactly where
 // 127 x / top does: 127 / top is held in two parts, hi + lo, and fma(x, hi, x lo) rounds
 // their sum once (for bf16 the quotient is never nearer to a tie than 2^-17 of itself
-// without being one).  Stored fp32 (F32) takes the quotient of the rounded 127 x, as the
-// definition in fp32 does; 2^-e, e top's exponent, keeps it in range.  Adding 1.5 2^23
+// without being one).  Stored fp32 (F32) takes the quotient of the rounded 127 x, which is
+// the definition computed in fp32; 2^-e, e top's exponent, keeps it in range.  Adding 1.5 2^23
 // rounds to the nearest even whole number and leaves it in the low byte.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kTopMin = 0x04800000u;  // 2^-118: a row below it counts as zero

@@ -131,3 +131,17 @@ def test_negated_views_are_refused():
         with pytest.raises(ValueError, match="negat"):
             call()
     assert torch.equal(api.layer_norm(neg.resolve_neg()), api.layer_norm(-x))
+
+
+def test_outputs_are_detached():
+    """No call is recorded by autograd, by the shortcut or by the Python path."""
+    api = _api()
+    x = torch.randn(6, 64, device="cuda", requires_grad=True)
+    w = torch.nn.Parameter(torch.randn(64, device="cuda"))
+    cur = torch.cuda.current_stream()
+    for stream in (None, cur):
+        for t in (*api.layer_norm(x, w, stats=True, stream=stream), api.quantize_rows(x, stream=stream).scale,
+                  api.layer_norm_q8(x, w, stream=stream).scale,
+                  api.linear_q8(api.quantize_rows(x), api.quantize_rows(x), stream=stream)):
+            assert not t.requires_grad
+    torch.cuda.synchronize()

@@ -338,7 +338,8 @@ int gl_version(void);
  * leap-ahead graph, MRConv, FC2 + residual and the FFN + residual.
  * ========================================================================= */
 
-typedef enum { GL_ACT_NONE = 0, GL_ACT_GELU = 1 } gl_act;
+/* GL_ACT_SILU, x sigmoid(x), is the gated layer's alone. */
+typedef enum { GL_ACT_NONE = 0, GL_ACT_GELU = 1, GL_ACT_SILU = 2 } gl_act;
 
 /* ---------------------------------------------------------------------------
  * gl_linear -- one fully connected layer over the channel axis (FC1, FC2 and
@@ -524,6 +525,114 @@ gl_status gl_layer_norm_q8(const void* x, int R, int C, long long ldx, const voi
 gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const int8_t* Wq,
                        const float* w_scale, const void* bias, int Cout, gl_act act_out,
                        const void* residual, gl_dtype dt, void* out, hipStream_t stream);
+
+/* ===========================================================================
+ * Training an FFN: the gated layer, the backward passes of the layers, and the
+ * end of a block with its gradients.
+ *
+ * Matrices of the layers are contiguous and 16-byte aligned (x, W, dy, dh, pre
+ * and the workspace), in dt, of any size: rows that are not whole 16-byte
+ * vectors are copied to the workspace first.  Vectors (bias) and outputs need
+ * their elements' alignment.  Sums are fp32, in an order that depends on the
+ * sizes alone: a call repeats its bits.  dW is rounded once to dt; the sums
+ * over rows (dbias, the norms' and the scale's gradients) are fp32.
+ * Limits of the layers: 1 <= R <= 2^28; 1 <= K, Cout, 2 F <= 2^20; R times each
+ * of them <= 2^36.  No output may overlap an input, the workspace or another.
+ * ========================================================================= */
+
+/* ---------------------------------------------------------------------------
+ * gl_gated_linear -- a gated fully connected layer (the first of a gated FFN):
+ *   g[r, f] = sum_k x[r, k] W[f, k] + bias[f]          the gate, f < F
+ *   u[r, f] = sum_k x[r, k] W[F + f, k] + bias[F + f]
+ *   h = act(g) u                                       (fp32, rounded once to dt)
+ *   x [R, K]; W [2 F, K]; bias [2 F] or NULL; h [R, F]
+ *   pre [R, 2 F] or NULL: [g | u], what gl_gated_linear_backward needs.
+ *   act: GL_ACT_GELU (g Phi(g)), GL_ACT_SILU (g sigmoid(g)) or GL_ACT_NONE; GELU and SiLU
+ *   of infinities are their limits.
+ *   workspace: gl_gated_linear_workspace_bytes(R, K, F, dt) bytes (0 for rows of whole
+ *   vectors, and for few rows), 16-byte aligned.
+ * Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype, activation), GL_ERR_BAD_SHAPE,
+ * GL_ERR_ALIGNMENT, GL_ERR_ALIAS, GL_ERR_WORKSPACE, GL_ERR_HIP.
+ * -------------------------------------------------------------------------*/
+size_t gl_gated_linear_workspace_bytes(int R, int K, int F, gl_dtype dt);
+gl_status gl_gated_linear(const void* x, int R, int K, const void* W, const void* bias, int F,
+                          gl_act act, gl_dtype dt, void* h, void* pre, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * gl_linear_backward -- the gradients of out = x W^T + bias (gl_linear without
+ * activations; a residual's gradient is dy itself):
+ *   dx = dy W [R, K];  dW = dy^T x [Cout, K];  dbias = sum_r dy [Cout] fp32
+ *   dy [R, Cout]; x [R, K]; W [Cout, K].  Any of the three may be NULL (not all): it is
+ *   then not computed.  x is read for dW alone and W for dx alone: NULL will do otherwise.
+ *   workspace: gl_linear_backward_workspace_bytes(R, K, Cout, dt) bytes.
+ * gl_gated_linear_backward -- the gradients of gl_gated_linear from dh [R, F] and pre:
+ *   d = [dh u act'(g) | dh act(g)];  dx = d W;  dW = d^T x [2 F, K];  dbias = sum_r d [2 F]
+ *   d is rounded to dt as the products' operand, and not for dbias.
+ * Limits and errors as gl_gated_linear.
+ * -------------------------------------------------------------------------*/
+size_t gl_linear_backward_workspace_bytes(int R, int K, int Cout, gl_dtype dt);
+gl_status gl_linear_backward(const void* dy, const void* x, int R, int K, const void* W, int Cout,
+                             gl_dtype dt, void* dx, void* dW, float* dbias, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+size_t gl_gated_linear_backward_workspace_bytes(int R, int K, int F, gl_dtype dt);
+gl_status gl_gated_linear_backward(const void* dh, const void* x, int R, int K, const void* W,
+                                   const void* pre, int F, gl_act act, gl_dtype dt, void* dx,
+                                   void* dW, float* dbias, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * gl_residual_norm -- the end of a block and the norm before the next one, per row:
+ *   n = norm(b) post_gamma + post_beta    if post is 1, else n = b
+ *   s = x + gate scale n
+ *   y = norm(s) gamma + beta              if y is given
+ * (all fp32; s and y are each rounded once to dt, y's norm is of the unrounded sum).
+ * norm: GL_NORM_LAYER as gl_layer_norm, GL_NORM_RMS v / sqrt(avg v^2 + eps).
+ *   x, b [R, C] (dt), rows ldx and ldb elements apart, of any alignment of their
+ *   elements, as gl_layer_norm.  post_gamma, post_beta, scale, gamma, beta [C] (dt) or
+ *   NULL for ones (betas: zeros).  gate: fp32, one value for each rows_per_gate rows,
+ *   ceil(R / rows_per_gate) of them, or NULL for ones.  A gate of 0 times a NaN or an
+ *   infinity is a NaN.
+ *   s [R, C] (dt), contiguous; y likewise, or NULL for none.
+ *   mean_b, rstd_b (post), mean_s, rstd_s (y) [R] fp32 or NULL: the norms' statistics,
+ *   which gl_residual_norm_backward needs (the means for GL_NORM_LAYER alone; zeros
+ *   are written there otherwise).
+ * Limits as gl_layer_norm.  Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype, norm),
+ * GL_ERR_BAD_SHAPE (sizes, strides, rows_per_gate < 1, eps), GL_ERR_ALIGNMENT,
+ * GL_ERR_ALIAS, GL_ERR_HIP.
+ * -------------------------------------------------------------------------*/
+typedef enum { GL_NORM_LAYER = 0, GL_NORM_RMS = 1 } gl_norm;
+
+gl_status gl_residual_norm(const void* x, long long ldx, const void* b, long long ldb, int R, int C,
+                           gl_norm norm, float eps, int post, const void* post_gamma,
+                           const void* post_beta, const void* scale, const float* gate,
+                           int rows_per_gate, const void* gamma, const void* beta, gl_dtype dt,
+                           void* s, void* y, float* mean_b, float* rstd_b, float* mean_s,
+                           float* rstd_s, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * gl_residual_norm_backward -- its gradients, from those of s (ds) and of y (dy).
+ *   ds, dy [R, C] (dt), rows ldds and lddy apart; one of them may be NULL.
+ *   b, s as in and out of the forward pass, with rows ldb and lds apart (s is needed with
+ *   dy alone); the statistics that it wrote; its vectors and gates.
+ *   dx, db [R, C] (dt), contiguous, or NULL.
+ *   dgate (fp32, as gate; rows_per_gate rows each), dscale, dpost_gamma, dpost_beta,
+ *   dgamma, dbeta [C] fp32, or NULL: they may be asked for where the vector was NULL too,
+ *   but for dpost_* without post and for dgamma and dbeta without dy.
+ *   workspace: gl_residual_norm_backward_workspace_bytes(R, C, dt) bytes, 16-byte
+ *   aligned; needed (NULL will do otherwise) if any of the last six is asked for.
+ * Outputs must not overlap inputs, the workspace or each other; NULL for all of them is
+ * an error.
+ * -------------------------------------------------------------------------*/
+size_t gl_residual_norm_backward_workspace_bytes(int R, int C, gl_dtype dt);
+gl_status gl_residual_norm_backward(
+    const void* ds, long long ldds, const void* dy, long long lddy, const void* b, long long ldb,
+    const void* s, long long lds, int R, int C, gl_norm norm, int post, const float* mean_b,
+    const float* rstd_b, const float* mean_s, const float* rstd_s, const void* post_gamma,
+    const void* post_beta, const void* scale, const float* gate, int rows_per_gate,
+    const void* gamma, gl_dtype dt, void* dx, void* db, float* dgate, float* dscale,
+    float* dpost_gamma, float* dpost_beta, float* dgamma, float* dbeta, void* workspace,
+    size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -15,6 +15,7 @@ from __future__ import annotations
 import ctypes
 import os
 import warnings
+from typing import NamedTuple
 
 import torch
 
@@ -24,7 +25,8 @@ LIB_PATH = os.path.join(_HERE, "libgraphleap.so")
 GL_F32, GL_BF16 = 0, 1
 GL_SCHED_LOOKAHEAD, GL_SCHED_STANDARD, GL_SCHED_LOOKAHEAD_FUSED = 0, 1, 2
 GL_TIME_BUILD, GL_TIME_UPDATE, GL_TIME_FUSED, GL_TIME_LINEAR = 0, 1, 2, 3
-GL_ACT_NONE, GL_ACT_GELU = 0, 1
+GL_ACT_NONE, GL_ACT_GELU, GL_ACT_SILU = 0, 1, 2
+GL_NORM_LAYER, GL_NORM_RMS = 0, 1
 GL_MAX_KD, GL_MAX_M, GL_MAX_K = 64, 4096, 64
 GL_MAX_Q8_K = 131071
 
@@ -76,6 +78,18 @@ SIGNATURES = {
     "gl_quantize_rows": [_vp, _i, _i, _ll, _i, _vp, _vp, _vp],
     "gl_layer_norm_q8": [_vp, _i, _i, _ll, _vp, _vp, _f, _i, _vp, _vp, _vp],
     "gl_linear_q8": [_vp, _vp, _i, _i, _vp, _vp, _vp, _i, _i, _vp, _i, _vp, _vp],
+    "gl_gated_linear_workspace_bytes": [_i, _i, _i, _i],
+    "gl_gated_linear": [_vp, _i, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _sz, _vp],
+    "gl_linear_backward_workspace_bytes": [_i, _i, _i, _i],
+    "gl_linear_backward": [_vp, _vp, _i, _i, _vp, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp],
+    "gl_gated_linear_backward_workspace_bytes": [_i, _i, _i, _i],
+    "gl_gated_linear_backward": [_vp, _vp, _i, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp],
+    "gl_residual_norm": [_vp, _ll, _vp, _ll, _i, _i, _i, _f, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i,
+                         _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+    "gl_residual_norm_backward_workspace_bytes": [_i, _i, _i],
+    "gl_residual_norm_backward": [_vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp, _vp, _vp,
+                                  _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  _vp, _vp, _vp, _sz, _vp],
     "gl_status_string": [_i],
     "gl_last_error": [],
     "gl_version": [],
@@ -84,6 +98,10 @@ RESTYPES = {"gl_status_string": ctypes.c_char_p, "gl_last_error": ctypes.c_char_
             "gl_vig_workspace_bytes": ctypes.c_size_t, "gl_mrconv_workspace_bytes": ctypes.c_size_t,
             "gl_mrconv_heads_workspace_bytes": ctypes.c_size_t,
             "gl_layer_norm_backward_workspace_bytes": ctypes.c_size_t,
+            "gl_gated_linear_workspace_bytes": ctypes.c_size_t,
+            "gl_linear_backward_workspace_bytes": ctypes.c_size_t,
+            "gl_gated_linear_backward_workspace_bytes": ctypes.c_size_t,
+            "gl_residual_norm_backward_workspace_bytes": ctypes.c_size_t,
             "gl_graphleap_workspace_bytes": ctypes.c_size_t}
 
 _lib = None
@@ -546,6 +564,264 @@ def linear_q8(x: Q8Rows, W: Q8Rows, bias: torch.Tensor | None = None, act_out: i
           W.scale.data_ptr(), _ptr(bias), Cout, act_out, _ptr(residual), _dt(out), out.data_ptr(),
           _s(stream))
     return out
+
+
+# ---------------------------------------------------------------------------
+# training an FFN: the gated layer, the layers' backward passes, and the end of a block with
+# its gradients.  Nothing is recorded by autograd here either: a forward pass returns what
+# its backward pass takes
+# ---------------------------------------------------------------------------
+def _matrix(name: str, t: torch.Tensor, shape: tuple | None, x: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of the layer x -> ...: of this shape, or of any (x itself)."""
+    if not t.is_cuda or t.dim() < 1:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return _like(name, t, t.shape if shape is None else shape, x.dtype, x)
+
+
+def _scratch(nbytes: int, x: torch.Tensor, ws, stream):
+    """The pointer and size of a call's workspace, and its buffer if it is allocated here."""
+    if ws is not None:
+        if stream is not None:
+            ws.record_stream(stream)
+        return ws.ptr, ws.nbytes, None
+    if not nbytes:
+        return None, 0, None
+    buf = _new((nbytes,), torch.uint8, x, stream)
+    return buf.data_ptr(), nbytes, buf
+
+
+def _layer(name: str, x: torch.Tensor, W: torch.Tensor):
+    """(R, K, outputs) of a layer's input rows and weight."""
+    _matrix("x", x, None, x)
+    K = x.shape[-1]
+    if W.dim() != 2 or W.shape[1] != K:
+        raise ValueError(f"{name}: W {tuple(W.shape)} does not match rows {tuple(x.shape)}")
+    _matrix("W", W, W.shape, x)
+    R = x.numel() // K if K else 0
+    _count(name, R, K, W.shape[0])
+    return R, K, W.shape[0]
+
+
+def _halves(name: str, W: torch.Tensor) -> int:
+    if W.shape[0] % 2:
+        raise ValueError(f"{name}: W's rows are the gate's and as many others, got {W.shape[0]}")
+    return W.shape[0] // 2
+
+
+def gated_linear_workspace(x: torch.Tensor, W: torch.Tensor) -> Workspace:
+    """Workspace of gl_gated_linear for this layer (empty for rows of whole vectors)."""
+    R, K, N = _layer("gated_linear", x, W)
+    return Workspace(lib().gl_gated_linear_workspace_bytes(R, K, _halves("gated_linear", W), _dt(x)), x.device)
+
+
+def gated_linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None,
+                 act: int = GL_ACT_SILU, keep: bool = False, out: torch.Tensor | None = None,
+                 ws: Workspace | None = None, stream=None):
+    """h[..., F] = act(g) * u with [g | u] = x W^T + bias over the last axis, W [2F, K]
+    (gl_gated_linear).  keep: return (h, pre), pre [..., 2F] the products that
+    gated_linear_backward takes.  The outputs are detached."""
+    R, K, N = _layer("gated_linear", x, W)
+    F = _halves("gated_linear", W)
+    _like("bias", bias, (N,), x.dtype, x)
+    lead = x.shape[:-1]
+    if out is None:
+        out = _new(lead + (F,), x.dtype, x, stream)
+    else:
+        _like("out", out, lead + (F,), x.dtype, x)
+    pre = _new(lead + (N,), x.dtype, x, stream) if keep else None
+    dt = _dt(x)
+    wp, wn, _buf = _scratch(0 if ws is not None else lib().gl_gated_linear_workspace_bytes(R, K, F, dt), x, ws, stream)
+    _hold(stream, x, W, bias, out)
+    _call("gl_gated_linear", x.data_ptr(), R, K, W.data_ptr(), _ptr(bias), F, act, dt, out.data_ptr(), _ptr(pre), wp,
+          wn, _s(stream))
+    return (out, pre) if keep else out
+
+
+def linear_backward_workspace(x: torch.Tensor, W: torch.Tensor) -> Workspace:
+    """Workspace of gl_linear_backward for this layer."""
+    R, K, N = _layer("linear_backward", x, W)
+    return Workspace(lib().gl_linear_backward_workspace_bytes(R, K, N, _dt(x)), x.device)
+
+
+def gated_linear_backward_workspace(x: torch.Tensor, W: torch.Tensor) -> Workspace:
+    """Workspace of gl_gated_linear_backward for this layer."""
+    R, K, N = _layer("gated_linear_backward", x, W)
+    return Workspace(lib().gl_gated_linear_backward_workspace_bytes(R, K, _halves("gated_linear_backward", W), _dt(x)),
+                     x.device)
+
+
+def _layer_grads(need, x, W, N, stream):
+    if not any(need):
+        raise ValueError("no gradient is asked for")
+    return (_new(x.shape, x.dtype, x, stream) if need[0] else None,
+            _new(W.shape, x.dtype, x, stream) if need[1] else None,
+            _new((N,), torch.float32, x, stream) if need[2] else None)
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, need=(True, True, True),
+                    ws: Workspace | None = None, stream=None):
+    """(dx, dW, dbias) of linear without activations, out = x W^T + bias, from its output's
+    gradient dy [..., Cout] (gl_linear_backward); dW in x's type, dbias a float32 sum over
+    all rows.  need: which of the three to compute (None for the others).  ws: the call's
+    workspace (allocated here when not given)."""
+    R, K, N = _layer("linear_backward", x, W)
+    _matrix("dy", dy, x.shape[:-1] + (N,), x)
+    dt = _dt(x)
+    dx, dW, db = _layer_grads(need, x, W, N, stream)
+    wp, wn, _buf = _scratch(0 if ws is not None else lib().gl_linear_backward_workspace_bytes(R, K, N, dt), x, ws, stream)
+    _hold(stream, dy, x, W)
+    _call("gl_linear_backward", dy.data_ptr(), x.data_ptr(), R, K, W.data_ptr(), N, dt, _ptr(dx), _ptr(dW), _ptr(db), wp,
+          wn, _s(stream))
+    return dx, dW, db
+
+
+def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: torch.Tensor,
+                          act: int = GL_ACT_SILU, need=(True, True, True), ws: Workspace | None = None,
+                          stream=None):
+    """(dx, dW, dbias) of gated_linear from its output's gradient dh [..., F], its input and
+    weight, and the products that it kept (gl_gated_linear_backward); dW in x's type,
+    dbias [2F] a float32 sum over all rows.  need and ws as in linear_backward."""
+    R, K, N = _layer("gated_linear_backward", x, W)
+    F = _halves("gated_linear_backward", W)
+    _matrix("dh", dh, x.shape[:-1] + (F,), x)
+    _matrix("pre", pre, x.shape[:-1] + (N,), x)
+    dt = _dt(x)
+    dx, dW, db = _layer_grads(need, x, W, N, stream)
+    wp, wn, _buf = _scratch(0 if ws is not None else lib().gl_gated_linear_backward_workspace_bytes(R, K, F, dt), x, ws,
+                            stream)
+    _hold(stream, dh, x, W, pre)
+    _call("gl_gated_linear_backward", dh.data_ptr(), x.data_ptr(), R, K, W.data_ptr(), pre.data_ptr(), F, act, dt,
+          _ptr(dx), _ptr(dW), _ptr(db), wp, wn, _s(stream))
+    return dx, dW, db
+
+
+class ResidualStats(NamedTuple):
+    """The rows' statistics of residual_norm's norms, float32 (None: there is none)."""
+    mean_b: torch.Tensor | None
+    rstd_b: torch.Tensor | None
+    mean_s: torch.Tensor | None
+    rstd_s: torch.Tensor | None
+
+
+class ResidualGrads(NamedTuple):
+    """The gradients of residual_norm (None: of an argument that was None).  dpost and dnorm
+    are (gamma's, beta's); all but dx and db are float32."""
+    dx: torch.Tensor
+    db: torch.Tensor
+    dgate: torch.Tensor | None
+    dscale: torch.Tensor | None
+    dpost: tuple | None
+    dnorm: tuple | None
+
+
+def _norm_pair(name: str, w, C: int, x: torch.Tensor):
+    if w is None:
+        return None, None
+    gamma, beta = w
+    _like(f"{name}'s gamma", gamma, (C,), x.dtype, x)
+    _like(f"{name}'s beta", beta, (C,), x.dtype, x)
+    return gamma, beta
+
+
+def _rows_per_gate(gate, x: torch.Tensor, R: int) -> int:
+    """A gate's axes are x's first ones: one for each image, or for each row."""
+    if gate is None:
+        return 1
+    if gate.dim() < 1 or gate.dim() >= x.dim() or not gate.numel():
+        raise ValueError(f"gate {tuple(gate.shape)}: its axes must be the first of {tuple(x.shape)}, without the last")
+    _like("gate", gate, x.shape[:gate.dim()], torch.float32, x)
+    return R // gate.numel()
+
+
+def residual_norm(x: torch.Tensor, b: torch.Tensor, post=None, scale: torch.Tensor | None = None,
+                  gate: torch.Tensor | None = None, norm=None, kind: int = GL_NORM_LAYER, eps: float = 1e-5,
+                  stats: bool = False, stream=None):
+    """(s, y): s = x + gate * scale * n, y = norm(s) for the next block (gl_residual_norm),
+    where n is a block's output b, normalised first if post is given.  post, norm: (gamma,
+    beta) of a norm over the last axis, either None for ones and zeros; None for no norm (y
+    is None without norm).  scale [C]; gate: float32, of x's first axes (an image's, or a
+    row's).  kind: GL_NORM_LAYER or GL_NORM_RMS.  x and b may be slices of wider rows.
+    stats: return (s, y, ResidualStats), which residual_norm_backward takes.  The outputs
+    are detached."""
+    R, C, ldx = _rows(x)
+    Rb, Cb, ldb = _rows(b)
+    if b.shape != x.shape or b.dtype != x.dtype or b.get_device() != x.get_device():
+        raise ValueError(f"b {b.dtype} {tuple(b.shape)} does not match x {x.dtype} {tuple(x.shape)}")
+    g1, b1 = _norm_pair("post", post, C, x)
+    g2, b2 = _norm_pair("norm", norm, C, x)
+    _like("scale", scale, (C,), x.dtype, x)
+    per = _rows_per_gate(gate, x, R)
+    dt = _dt(x)
+    s = _new(x.shape, x.dtype, x, stream)
+    y = _new(x.shape, x.dtype, x, stream) if norm is not None else None
+
+    def kept(on):
+        return _new(x.shape[:-1], torch.float32, x, stream) if stats and on else None
+    st = ResidualStats(kept(post is not None and kind == GL_NORM_LAYER), kept(post is not None),
+                       kept(norm is not None and kind == GL_NORM_LAYER), kept(norm is not None))
+    _hold(stream, x, b, g1, b1, g2, b2, scale, gate)
+    _call("gl_residual_norm", x.data_ptr(), ldx, b.data_ptr(), ldb, R, C, kind, eps, post is not None, _ptr(g1),
+          _ptr(b1), _ptr(scale), _ptr(gate), per, _ptr(g2), _ptr(b2), dt, s.data_ptr(), _ptr(y), _ptr(st.mean_b),
+          _ptr(st.rstd_b), _ptr(st.mean_s), _ptr(st.rstd_s), _s(stream))
+    return (s, y, st) if stats else (s, y)
+
+
+def residual_norm_backward_workspace(b: torch.Tensor) -> Workspace:
+    """Workspace of gl_residual_norm_backward for rows shaped like b."""
+    R, C, _ = _rows(b)
+    return Workspace(lib().gl_residual_norm_backward_workspace_bytes(R, C, _dt(b)), b.device)
+
+
+def residual_norm_backward(ds: torch.Tensor | None, dy: torch.Tensor | None, b: torch.Tensor,
+                           s: torch.Tensor | None, stats, post=None, scale: torch.Tensor | None = None,
+                           gate: torch.Tensor | None = None, norm=None, kind: int = GL_NORM_LAYER,
+                           ws: Workspace | None = None, stream=None) -> ResidualGrads:
+    """The gradients of residual_norm, from those of its outputs (either may be None), what
+    it was given and returned, and its ResidualStats (gl_residual_norm_backward).  ws: the
+    call's workspace (allocated here when not given)."""
+    R, C, ldb = _rows(b)
+    if ds is None and dy is None:
+        raise ValueError("ds or dy is required")
+    if (dy is None) != (norm is None):
+        raise ValueError("dy and norm belong together")
+    ld = [0, 0, 0]
+    for i, (name, t) in enumerate((("ds", ds), ("dy", dy), ("s", s if dy is not None else None))):
+        if t is None:
+            if name == "s" and dy is not None:
+                raise ValueError("s is required with dy")
+            continue
+        ld[i] = _rows(t)[2]
+        if t.shape != b.shape or t.dtype != b.dtype or t.get_device() != b.get_device():
+            raise ValueError(f"{name} {t.dtype} {tuple(t.shape)} does not match b {b.dtype} {tuple(b.shape)}")
+    g1, b1 = _norm_pair("post", post, C, b)
+    g2, b2 = _norm_pair("norm", norm, C, b)
+    _like("scale", scale, (C,), b.dtype, b)
+    per = _rows_per_gate(gate, b, R)
+    mean_b, rstd_b, mean_s, rstd_s = stats
+    for name, t, on in (("mean_b", mean_b, post is not None and kind == GL_NORM_LAYER), ("rstd_b", rstd_b, post is not None),
+                        ("mean_s", mean_s, norm is not None and kind == GL_NORM_LAYER), ("rstd_s", rstd_s, norm is not None)):
+        if on and t is None:
+            raise ValueError(f"{name} is required")
+        _like(name, t, b.shape[:-1], torch.float32, b)
+    dt = _dt(b)
+
+    def vec(on, n=(C,)):
+        return _new(n, torch.float32, b, stream) if on else None
+    dx, db = _new(b.shape, b.dtype, b, stream), _new(b.shape, b.dtype, b, stream)
+    dgate, dscale = vec(gate is not None, () if gate is None else gate.shape), vec(scale is not None)
+    dg1, db1, dg2, db2 = (vec(t is not None) for t in (g1, b1, g2, b2))
+    want = any(t is not None for t in (dgate, dscale, dg1, db1, dg2, db2))
+    need = lib().gl_residual_norm_backward_workspace_bytes(R, C, dt) if want and ws is None else 0
+    wp, wn, _buf = _scratch(need, b, ws, stream)
+    _hold(stream, ds, dy, b, s, mean_b, rstd_b, mean_s, rstd_s, g1, b1, g2, scale, gate)
+    _call("gl_residual_norm_backward", _ptr(ds), ld[0], _ptr(dy), ld[1], b.data_ptr(), ldb,
+          None if dy is None else s.data_ptr(), ld[2], R, C, kind, post is not None, _ptr(mean_b), _ptr(rstd_b),
+          _ptr(mean_s), _ptr(rstd_s), _ptr(g1), _ptr(b1), _ptr(scale), _ptr(gate), per, _ptr(g2), dt, dx.data_ptr(),
+          db.data_ptr(), _ptr(dgate), _ptr(dscale), _ptr(dg1), _ptr(db1), _ptr(dg2), _ptr(db2), wp, wn, _s(stream))
+    return ResidualGrads(dx, db, dgate, dscale, None if post is None else (dg1, db1),
+                         None if norm is None else (dg2, db2))
 
 
 def vig_params(p: dict) -> VigParams:

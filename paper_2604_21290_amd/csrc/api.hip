@@ -1414,3 +1414,209 @@ gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const 
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// training an FFN
+// ---------------------------------------------------------------------------
+namespace {
+
+bool layer_sizes_ok(int R, int K, long long N) {
+  constexpr long long most = 1LL << 36;
+  return R >= 1 && K >= 1 && N >= 1 && R <= 1 << 28 && K <= 1 << 20 && N <= 1 << 20 && R * (long long)K <= most && R * N <= most;
+}
+
+// Every tensor of a call as bytes from its start: those that are written, then the rest.
+gl_status check_layer(const char* who, int R, int K, long long N, gl_dtype dt, std::initializer_list<const void*> matrices,
+                      std::initializer_list<const void*> vectors) {
+  if (!dtype_ok(dt)) return fail(GL_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, (int)dt);
+  if (!layer_sizes_ok(R, K, N)) return fail(GL_ERR_BAD_SHAPE, "%s: bad shape R=%d K=%d, %lld outputs", who, R, K, N);
+  for (const void* p : matrices)
+    if (p && !aligned(p, 16)) return fail(GL_ERR_ALIGNMENT, "%s: matrices need 16-byte alignment", who);
+  for (const void* p : vectors)
+    if (p && !aligned(p, esize(dt))) return fail(GL_ERR_ALIGNMENT, "%s: tensors need their elements' alignment", who);
+  return GL_OK;
+}
+
+Range given(const void* p, size_t n) { return {p, p ? n : 0}; }
+
+gl_status layer_backward(const char* who, const gl::LinearGradArgs& g, int F, gl_dtype dt, size_t ws_bytes, hipStream_t stream) {
+  if (!g.dx && !g.dW && !g.db) return fail(GL_ERR_NULL_PTR, "%s: an output is required", who);
+  if (!g.dy || (g.dx && !g.W) || (g.dW && !g.x))
+    return fail(GL_ERR_NULL_PTR, "%s: the output's gradient, W for dx and x for dW are required", who);
+  gl_status s = check_layer(who, g.R, g.K, g.N, dt, {g.dy, g.x, g.W, g.pre}, {g.dx, g.dW});
+  if (s != GL_OK) return s;
+  if (g.db && !aligned(g.db, 4)) return fail(GL_ERR_ALIGNMENT, "%s: dbias needs 4-byte alignment", who);
+  const size_t es = esize(dt), rk = (size_t)g.R * g.K * es, nk = (size_t)g.N * g.K * es, rn = (size_t)g.R * g.N * es;
+  const Range dy = given(g.dy, (size_t)g.R * F * es), x = given(g.x, rk), W = given(g.W, nk), pre = given(g.pre, rn),
+              dx = given(g.dx, rk), dW = given(g.dW, nk), db = given(g.db, (size_t)g.N * 4);
+  if ((s = check_apart(who, {dx, dW, db}, {dy, x, W, pre})) != GL_OK) return s;
+  const size_t need = gl::linear_grad_ws_bytes(g.R, g.K, g.N, dt == GL_BF16, g.pre != nullptr);
+  if ((s = check_ws(who, need, g.ws, ws_bytes, {dy, x, W, pre, dx, dW, db})) != GL_OK) return s;
+  hipError_t e = gl::launch_linear_grad(g, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, who);
+}
+
+gl_status check_residual(const char* who, const void* x, long long ldx, const void* b, long long ldb, int R, int C,
+                         gl_norm norm, int rows_per_gate, gl_dtype dt) {
+  gl_status s = GL_OK;
+  if (x) s = check_rows(who, x, R, C, ldx, dt);
+  if (s == GL_OK && b) s = check_rows(who, b, R, C, ldb, dt);
+  if (s != GL_OK) return s;
+  if (norm != GL_NORM_LAYER && norm != GL_NORM_RMS) return fail(GL_ERR_UNSUPPORTED, "%s: unknown norm %d", who, (int)norm);
+  if (rows_per_gate < 1) return fail(GL_ERR_BAD_SHAPE, "%s: rows_per_gate=%d", who, rows_per_gate);
+  return GL_OK;
+}
+
+gl_status check_elements(const char* who, size_t es, std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (p && !aligned(p, es)) return fail(GL_ERR_ALIGNMENT, "%s: tensors need their elements' alignment", who);
+  return GL_OK;
+}
+
+size_t gate_bytes(int R, int per) { return ((size_t)R + per - 1) / per * 4; }
+
+}  // namespace
+
+extern "C" {
+
+size_t gl_gated_linear_workspace_bytes(int R, int K, int F, gl_dtype dt) {
+  return dtype_ok(dt) && layer_sizes_ok(R, K, 2LL * F) ? gl::gated_ws_bytes(R, K, F, dt == GL_BF16) : 0;
+}
+
+gl_status gl_gated_linear(const void* x, int R, int K, const void* W, const void* bias, int F, gl_act act, gl_dtype dt,
+                          void* h, void* pre, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const char* who = "gated_linear";
+  if (!x || !W || !h) return fail(GL_ERR_NULL_PTR, "%s: x, W and h are required", who);
+  if (act != GL_ACT_NONE && act != GL_ACT_GELU && act != GL_ACT_SILU)
+    return fail(GL_ERR_UNSUPPORTED, "%s: unknown activation %d", who, (int)act);
+  gl_status s = check_layer(who, R, K, 2LL * F, dt, {x, W}, {bias, h, pre});
+  if (s != GL_OK) return s;
+  const size_t es = esize(dt), rf = (size_t)R * F * es;
+  const Range xr = given(x, (size_t)R * K * es), wr = given(W, 2 * (size_t)F * K * es), br = given(bias, 2 * (size_t)F * es),
+              hr = given(h, rf), pr = given(pre, 2 * rf);
+  if ((s = check_apart(who, {hr, pr}, {xr, wr, br})) != GL_OK) return s;
+  if ((s = check_ws(who, gl::gated_ws_bytes(R, K, F, dt == GL_BF16), workspace, workspace_bytes, {xr, wr, br, hr, pr})) != GL_OK)
+    return s;
+  hipError_t e = gl::launch_gated({x, W, bias, h, pre, workspace, R, K, F, (int)act}, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, who);
+}
+
+size_t gl_linear_backward_workspace_bytes(int R, int K, int Cout, gl_dtype dt) {
+  return dtype_ok(dt) && layer_sizes_ok(R, K, Cout) ? gl::linear_grad_ws_bytes(R, K, Cout, dt == GL_BF16, false) : 0;
+}
+
+gl_status gl_linear_backward(const void* dy, const void* x, int R, int K, const void* W, int Cout, gl_dtype dt, void* dx,
+                             void* dW, float* dbias, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  gl::LinearGradArgs g{dy, x, W, nullptr, dx, dW, dbias, workspace, R, K, Cout, 0};
+  return layer_backward("linear_backward", g, Cout, dt, workspace_bytes, stream);
+}
+
+size_t gl_gated_linear_backward_workspace_bytes(int R, int K, int F, gl_dtype dt) {
+  return dtype_ok(dt) && layer_sizes_ok(R, K, 2LL * F) ? gl::linear_grad_ws_bytes(R, K, 2 * F, dt == GL_BF16, true) : 0;
+}
+
+gl_status gl_gated_linear_backward(const void* dh, const void* x, int R, int K, const void* W, const void* pre, int F,
+                                   gl_act act, gl_dtype dt, void* dx, void* dW, float* dbias, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+  const char* who = "gated_linear_backward";
+  if (!pre) return fail(GL_ERR_NULL_PTR, "%s: pre is required", who);
+  if (act != GL_ACT_NONE && act != GL_ACT_GELU && act != GL_ACT_SILU)
+    return fail(GL_ERR_UNSUPPORTED, "%s: unknown activation %d", who, (int)act);
+  if (F < 1 || F > 1 << 19) return fail(GL_ERR_BAD_SHAPE, "%s: F=%d", who, F);
+  gl::LinearGradArgs g{dh, x, W, pre, dx, dW, dbias, workspace, R, K, 2 * F, (int)act};
+  return layer_backward(who, g, F, dt, workspace_bytes, stream);
+}
+
+gl_status gl_residual_norm(const void* x, long long ldx, const void* b, long long ldb, int R, int C, gl_norm norm, float eps,
+                           int post, const void* post_gamma, const void* post_beta, const void* scale, const float* gate,
+                           int rows_per_gate, const void* gamma, const void* beta, gl_dtype dt, void* s, void* y, float* mean_b,
+                           float* rstd_b, float* mean_s, float* rstd_s, hipStream_t stream) {
+  const char* who = "residual_norm";
+  if (!x || !b || !s) return fail(GL_ERR_NULL_PTR, "%s: x, b and s are required", who);
+  gl_status st = check_residual(who, x, ldx, b, ldb, R, C, norm, rows_per_gate, dt);
+  if (st != GL_OK) return st;
+  if (!(eps >= 0.f) || eps > 3.4e38f) return fail(GL_ERR_BAD_SHAPE, "%s: bad eps %g", who, eps);
+  const size_t es = esize(dt), rc = (size_t)R * C * es, v = C * es, r4 = (size_t)R * 4;
+  if ((st = check_elements(who, es, {post_gamma, post_beta, scale, gamma, beta, s, y})) != GL_OK ||
+      (st = check_elements(who, 4, {gate, mean_b, rstd_b, mean_s, rstd_s})) != GL_OK)
+    return st;
+  st = check_apart(who, {given(s, rc), given(y, rc), given(mean_b, r4), given(rstd_b, r4), given(mean_s, r4), given(rstd_s, r4)},
+                   {given(x, span(R, C, ldx, es)), given(b, span(R, C, ldb, es)), given(post_gamma, v), given(post_beta, v),
+                    given(scale, v), given(gamma, v), given(beta, v), given(gate, gate_bytes(R, rows_per_gate))});
+  if (st != GL_OK) return st;
+  const gl::RowArgs of = row_args(x, R, C, ldx, gamma, beta, eps);
+  gl::ResidualArgs a{};
+  a.x = x, a.b = b, a.ldx = ldx, a.ldb = ldb;
+  a.gamma1 = post_gamma, a.beta1 = post_beta, a.scale = scale, a.gamma2 = gamma, a.beta2 = beta;
+  a.gate = gate;
+  a.s = s, a.y = y;
+  a.mean_b = post ? mean_b : nullptr, a.rstd_b = post ? rstd_b : nullptr;
+  a.mean_s = y ? mean_s : nullptr, a.rstd_s = y ? rstd_s : nullptr;
+  a.R = R, a.C = C, a.per_gate = rows_per_gate;
+  a.post = post != 0, a.rms = norm == GL_NORM_RMS;
+  a.eps = eps, a.inv_c = of.inv_c, a.mean_hi = of.mean_hi, a.mean_lo = of.mean_lo;
+  hipError_t e = gl::launch_residual(a, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, who);
+}
+
+size_t gl_residual_norm_backward_workspace_bytes(int R, int C, gl_dtype dt) {
+  if (!dtype_ok(dt) || R < 1 || C < 1 || R > 1 << 30 || C > 1 << 29 || !size_ok(R, 1, C)) return 0;
+  return gl::residual_grad_ws_bytes(R, C, dt == GL_BF16);
+}
+
+gl_status gl_residual_norm_backward(const void* ds, long long ldds, const void* dy, long long lddy, const void* b, long long ldb,
+                                    const void* s, long long lds, int R, int C, gl_norm norm, int post, const float* mean_b,
+                                    const float* rstd_b, const float* mean_s, const float* rstd_s, const void* post_gamma,
+                                    const void* post_beta, const void* scale, const float* gate, int rows_per_gate,
+                                    const void* gamma, gl_dtype dt, void* dx, void* db, float* dgate, float* dscale,
+                                    float* dpost_gamma, float* dpost_beta, float* dgamma, float* dbeta, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream) {
+  const char* who = "residual_norm_backward";
+  const bool layer = norm == GL_NORM_LAYER, sums = dscale || dpost_gamma || dpost_beta || dgamma || dbeta;
+  if ((!ds && !dy) || !b || (!dx && !db && !dgate && !sums))
+    return fail(GL_ERR_NULL_PTR, "%s: ds or dy, b and an output are required", who);
+  if (dy && (!s || !rstd_s || (layer && !mean_s)))
+    return fail(GL_ERR_NULL_PTR, "%s: s and its statistics are required with dy", who);
+  if (post && (!rstd_b || (layer && !mean_b))) return fail(GL_ERR_NULL_PTR, "%s: b's statistics are required with post", who);
+  if ((!post && (dpost_gamma || dpost_beta)) || (!dy && (dgamma || dbeta)))
+    return fail(GL_ERR_UNSUPPORTED, "%s: the gradient of a norm that is not there", who);
+  gl_status st = check_residual(who, ds, ldds, b, ldb, R, C, norm, rows_per_gate, dt);
+  if (st == GL_OK && dy) st = check_residual(who, dy, lddy, s, lds, R, C, norm, rows_per_gate, dt);
+  if (st != GL_OK) return st;
+  const size_t es = esize(dt), rc = (size_t)R * C * es, v = C * es, c4 = (size_t)C * 4, r4 = (size_t)R * 4;
+  if ((st = check_elements(who, es, {post_gamma, post_beta, scale, gamma, dx, db})) != GL_OK ||
+      (st = check_elements(who, 4, {gate, mean_b, rstd_b, mean_s, rstd_s, dgate, dscale, dpost_gamma, dpost_beta, dgamma,
+                                    dbeta})) != GL_OK)
+    return st;
+  const size_t gb = gate_bytes(R, rows_per_gate);
+  const Range in[] = {given(ds, ds ? span(R, C, ldds, es) : 0), given(dy, dy ? span(R, C, lddy, es) : 0), given(b, span(R, C, ldb, es)),
+                      given(dy ? s : nullptr, dy ? span(R, C, lds, es) : 0), given(mean_b, r4), given(rstd_b, r4),
+                      given(mean_s, r4), given(rstd_s, r4), given(post_gamma, v), given(post_beta, v), given(scale, v),
+                      given(gamma, v), given(gate, gb)};
+  const Range out[] = {given(dx, rc), given(db, rc), given(dgate, gb), given(dscale, c4), given(dpost_gamma, c4),
+                       given(dpost_beta, c4), given(dgamma, c4), given(dbeta, c4)};
+  st = check_apart(who, {out[0], out[1], out[2], out[3], out[4], out[5], out[6], out[7]},
+                   {in[0], in[1], in[2], in[3], in[4], in[5], in[6], in[7], in[8], in[9], in[10], in[11], in[12]});
+  if (st != GL_OK) return st;
+  if (sums || dgate) {
+    st = check_ws(who, gl::residual_grad_ws_bytes(R, C, dt == GL_BF16), workspace, workspace_bytes,
+                  {in[0], in[1], in[2], in[3], in[4], in[5], in[6], in[7], in[8], in[9], in[10], in[11], in[12], out[0], out[1],
+                   out[2], out[3], out[4], out[5], out[6], out[7]});
+    if (st != GL_OK) return st;
+  }
+  gl::ResidualGradArgs a{};
+  a.ds = ds, a.dy = dy, a.b = b, a.s = dy ? s : nullptr;
+  a.ldds = ds ? ldds : 0, a.lddy = dy ? lddy : 0, a.ldb = ldb, a.lds = dy ? lds : 0;
+  a.mean_b = mean_b, a.rstd_b = rstd_b, a.mean_s = mean_s, a.rstd_s = rstd_s;
+  a.gamma1 = post_gamma, a.beta1 = post_beta, a.scale = scale, a.gamma2 = gamma;
+  a.gate = gate;
+  a.dx = dx, a.db = db;
+  a.dgate = dgate, a.dscale = dscale, a.dgamma1 = dpost_gamma, a.dbeta1 = dpost_beta, a.dgamma2 = dgamma, a.dbeta2 = dbeta;
+  a.R = R, a.C = C, a.per_gate = rows_per_gate;
+  a.post = post != 0, a.rms = !layer;
+  a.inv_c = (float)(1.0 / C);
+  hipError_t e = gl::launch_residual_grad(a, workspace, dt == GL_BF16, stream);
+  return e == hipSuccess ? GL_OK : hip_fail(e, who);
+}
+
+}  // extern "C"

@@ -1,0 +1,142 @@
+// The gated fully connected layer
+//   pre = x W^T + b,  W [2 F, K];  h = act(pre[:, :F]) * pre[:, F:]
+// in one pass: a wave's tile holds as many columns of the gate as of the other product, the
+// same ones, so that both of an output's products end in the same lane's registers and only
+// h (and, for a backward pass, pre) is written.  Many rows: product.h.  Few rows (serving):
+// the kernel below, which reads W once straight into registers.
+#include "product.h"
+
+namespace gl {
+
+namespace {
+
+// Up to 16 RT rows.  A workgroup takes 16 columns of the gate and the same of the other
+// product; its eight waves share the contraction, 128 bytes of every row at a time: a lane
+// has 32 consecutive bytes of one row of W, and of one row of x, whose place in the
+// instruction's contraction both agree on.  Rows of x are few and stay in the caches;
+// W's bytes bound it.
+template <int DT, int RT>
+__global__ __launch_bounds__(512) void gated_few_kernel(ProductArgs a) {
+  using T = Chunk<DT>;
+  constexpr int E = T::E, ES = DT ? 2 : 4, BK = 128 / ES, NW = 8;
+  __shared__ float sums[NW][2][RT * 16][17];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, t = lane & 15;
+  const int n0 = blockIdx.x * 16, K = a.K;
+  const char* wg = static_cast<const char*>(a.B) + (size_t)min(n0 + t, a.N - 1) * K * ES;
+  const char* wu = wg + (size_t)a.N * K * ES;
+  const char* x[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) x[r] = static_cast<const char*>(a.A) + (size_t)min(r * 16 + t, a.M - 1) * K * ES;
+  f32x4 acc[2][RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) acc[0][r] = acc[1][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // E values from k on, zeros past the row's end
+  auto load = [&](const char* p, int k) {
+    if (k + E <= K) return T::raw(p, k);
+    uint32_t v[4] = {0, 0, 0, 0};
+    for (int j = 0; k + j < K && j < E; ++j) {
+      if (DT) v[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[k + j] << (j % 2 * 16);
+      else v[j] = reinterpret_cast<const uint32_t*>(p)[k + j];
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  };
+  for (int k0 = w * BK; k0 < K; k0 += NW * BK) {
+    const int k = k0 + g * 2 * E;
+    uint4 wf[2][2], xf[RT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      wf[0][h] = load(wg, k + h * E);
+      wf[1][h] = load(wu, k + h * E);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) xf[r][h] = load(x[r], k + h * E);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        acc[0][r] = product_mma<DT>(wf[0][h], xf[r][h], acc[0][r]);
+        acc[1][r] = product_mma<DT>(wf[1][h], xf[r][h], acc[1][r]);
+      }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sums[w][h][r * 16 + t][4 * g + v] = acc[h][r][v];
+  __syncthreads();
+  for (int i = threadIdx.x; i < RT * 256; i += 512) {
+    const int r = i >> 4, c = i & 15, n = n0 + c;
+    if (r >= a.M || n >= a.N) continue;
+    float y = 0.f, u = 0.f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) y += sums[q][0][r][c], u += sums[q][1][r][c];
+    if (a.bias) y += T::load1(a.bias, n), u += T::load1(a.bias, (size_t)a.N + n);
+    if (a.pre) {
+      T::store1(a.pre, (size_t)r * 2 * a.N + n, y);
+      T::store1(a.pre, (size_t)r * 2 * a.N + a.N + n, u);
+    }
+    T::store1(a.out, (size_t)r * a.N + n, gate_act<DT>(a.act, y) * u);
+  }
+}
+
+constexpr int kFewRows = 64;
+
+// bytes of a row brought to whole 16-byte vectors
+size_t packed_row(int C, int dt_bf16) { return ((size_t)C * (dt_bf16 ? 2 : 4) + 15) & ~(size_t)15; }
+size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+template <int DT>
+hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
+  const void* fn = a.M <= 16   ? (const void*)&gated_few_kernel<DT, 1>
+                   : a.M <= 32 ? (const void*)&gated_few_kernel<DT, 2>
+                               : (const void*)&gated_few_kernel<DT, 4>;
+  void* argv[] = {const_cast<ProductArgs*>(&a)};
+  return hipLaunchKernel(fn, dim3((a.N + 15) / 16), dim3(512), argv, 0, stream);
+}
+
+template <int DT>
+hipError_t launch_tiles(const ProductArgs& a, hipStream_t stream) {
+  auto tiles = [&](int b) { return ((long long)(a.M + b - 1) / b) * ((2LL * a.N + b - 1) / b); };
+  if constexpr (DT == 1)
+    if (tiles(256) >= 200) return launch_product<ProductCfg<1, false, false, 256, 256, 2, 4>, kProductGated>(a, stream);
+  if (tiles(128) >= 200) return launch_product<ProductCfg<DT, false, false, 128, 128, 2, 2>, kProductGated>(a, stream);
+  return launch_product<ProductCfg<DT, false, false, 64, 64, 2, 2>, kProductGated>(a, stream);
+}
+
+}  // namespace
+
+size_t gated_ws_bytes(int R, int K, int F, int dt_bf16) {
+  if (R <= kFewRows || K % (dt_bf16 ? 8 : 4) == 0) return 0;
+  const size_t row = packed_row(K, dt_bf16);
+  return whole256(R * row) + 2 * (size_t)F * row;
+}
+
+hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream) {
+  const int es = dt_bf16 ? 2 : 4;
+  ProductArgs a{};
+  a.A = g.x;
+  a.B = g.W;
+  a.lda = a.ldb = (long long)g.K * es;
+  a.M = g.R;
+  a.N = g.F;
+  a.K = g.K;
+  a.out = g.h;
+  a.bias = g.bias;
+  a.pre = g.pre;
+  a.act = g.act;
+  if (g.R <= kFewRows) return dt_bf16 ? launch_few<1>(a, stream) : launch_few<0>(a, stream);
+  if (g.K % (16 / es)) {  // rows of whole vectors in the workspace
+    const size_t row = packed_row(g.K, dt_bf16);
+    char *x = static_cast<char*>(g.ws), *W = x + whole256(g.R * row);
+    hipError_t e = launch_pack_rows(g.x, g.R, g.K, x, dt_bf16, stream);
+    if (e == hipSuccess) e = launch_pack_rows(g.W, 2 * g.F, g.K, W, dt_bf16, stream);
+    if (e != hipSuccess) return e;
+    a.A = x;
+    a.B = W;
+    a.lda = a.ldb = (long long)row;
+  }
+  return dt_bf16 ? launch_tiles<1>(a, stream) : launch_tiles<0>(a, stream);
+}
+
+}  // namespace gl

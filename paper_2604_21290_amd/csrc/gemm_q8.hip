@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "gl_device.h"
+#include "act_device.h"
 #include "gl_kernels.h"
 
 namespace gl {
@@ -21,38 +22,13 @@ __device__ __forceinline__ i32x4 mfma_i8(const uint4& a, const uint4& b, i32x4 a
                                                __builtin_bit_cast(i32x4, b), acc, 0, 0, 0);
 }
 
-// GELU x Phi(x) = max(x, 0) - |x| Phi(-|x|), where Phi(-a) e^(a^2 / 2) falls like 1 / a for
-// large a: with t = 1 / (1 + p a) it is t q(t), q a smooth function on (0, 1].  q is a
-// polynomial fitted in float64 to the least largest error relative to Phi(-a), weighted by
-// what the output's type shows of it, so that the tail's small results have their bits too:
-//   bf16  five terms, within 5.7e-7 e^(1.5 a), never more than 2.8e-3 (2^-8 is its rounding)
-//   fp32  eight terms, within 3.8e-8 (1 + a)
-// The rest is fp32's own rounding, at most (13 + a + 2 a^2) 2^-24 with the fit (the
-// argument's last bit alone moves Phi(-a) by a^2 of its own).  The three terms more cost an
-// fp32 layer up to 5 % (100352x80x320 34.2 us for 32.8, 6272x192x768 8.5 for 8.1); in bf16
-// they would change one output in a thousand.  Its limits at the infinities.
+// The GELU and its error: act_device.h.  The rest is fp32's own rounding, at most
+// (13 + a + 2 a^2) 2^-24 with the fit (the argument's last bit alone moves Phi(-a) by a^2 of
+// its own).  The three terms more cost an fp32 layer up to 5 % (100352x80x320 34.2 us for
+// 32.8, 6272x192x768 8.5 for 8.1); in bf16 they would change one output in a thousand.
 template <int DT>
 __device__ __forceinline__ float gelu_q8(float x) {
-  const float a = fabsf(x);
-  const float t = __builtin_amdgcn_rcpf(fmaf(DT ? 0.34400001f : 0.3f, a, 1.f));
-  float q;
-  if (DT) {
-    q = fmaf(t, -0.100211024f, 0.2995327891f);
-    q = fmaf(t, q, -0.005176517668f);
-    q = fmaf(t, q, 0.1722774513f);
-    q = fmaf(t, q, 0.1335771899f);
-  } else {
-    q = fmaf(t, 0.03661797821f, -0.1609455123f);
-    q = fmaf(t, q, 0.212445229f);
-    q = fmaf(t, q, -0.0589276667f);
-    q = fmaf(t, q, 0.1311242333f);
-    q = fmaf(t, q, 0.09920725217f);
-    q = fmaf(t, q, 0.1208549423f);
-    q = fmaf(t, q, 0.1196235572f);
-  }
-  const float y = x * 0.84932180028801907f;  // sqrt(log2(e) / 2)
-  const float e = __builtin_amdgcn_exp2f(-y * y);
-  return fmaf(-fminf(a, 3.4e38f), t * q * e, fmaxf(x, 0.f));
+  return gelu_tail<DT>(x);
 }
 
 typedef uint32_t u32x4_w __attribute__((ext_vector_type(4), aligned(4), may_alias));

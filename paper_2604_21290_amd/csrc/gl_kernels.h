@@ -98,6 +98,55 @@ struct GemmQ8Args {
   int act_out;
 };
 
+// The end of a block (residual.hip): with n = norm(b) gamma1 + beta1 (post) or b,
+//   s = x + gate scale n,  y = norm(s) gamma2 + beta2
+struct ResidualArgs {
+  const void *x, *b;        // [R, C], rows ldx and ldb elements apart
+  long long ldx, ldb;
+  const void *gamma1, *beta1, *scale, *gamma2, *beta2;  // [C] or null
+  const float* gate;        // a value for each `per_gate` rows, or null
+  void *s, *y;              // [R, C]; y: or null
+  float *mean_b, *rstd_b, *mean_s, *rstd_s;  // [R] or null
+  int R, C, per_gate;
+  int post, rms;
+  float eps, inv_c, mean_hi, mean_lo;
+};
+
+// Its gradients.  dv = ds + the norm's from dy (either may be null).
+struct ResidualGradArgs {
+  const void *ds, *dy, *b, *s;  // [R, C] or null (not b)
+  long long ldds, lddy, ldb, lds;
+  const float *mean_b, *rstd_b, *mean_s, *rstd_s;
+  const void *gamma1, *beta1, *scale, *gamma2;
+  const float* gate;
+  void *dx, *db;            // [R, C]
+  float *dgate, *dscale, *dgamma1, *dbeta1, *dgamma2, *dbeta2;  // or null
+  float *part, *dots, *rows;  // workspace: the groups' sums; a row's part of dgate; a row's averages
+  int R, C, per_gate;
+  int post, rms;
+  float inv_c;
+};
+
+// The gated layer: h = act(g) u, pre = [g | u] = x W^T + bias.
+struct GatedArgs {
+  const void *x, *W;   // [R, K], [2 F, K]
+  const void* bias;    // [2 F] or null
+  void *h, *pre;       // [R, F]; [R, 2 F] or null
+  void* ws;
+  int R, K, F, act;
+};
+
+// The gradients of a layer of N outputs; pre != null: of a gated one with N = 2 F, whose
+// dy is [R, F], that of h.
+struct LinearGradArgs {
+  const void *dy, *x, *W;  // [R, N], [R, K], [N, K]
+  const void* pre;         // [R, N] or null
+  void *dx, *dW;           // [R, K], [N, K] or null
+  float* db;               // [N] or null
+  void* ws;
+  int R, K, N, act;
+};
+
 // Workgroups are dispatched round-robin over the 8 XCDs (workgroup id mod 8).
 // Map dispatch ids so that consecutive logical ids (neighbouring tiles of the
 // same image, which share key rows) land on the same XCD and its L2.
@@ -219,5 +268,17 @@ hipError_t launch_norm_grad(const NormGradArgs& a, int dt_bf16, hipStream_t stre
 // Bytes of an 8-bit row of K values: whole 16-byte vectors.
 constexpr long long q8_row_bytes(long long K) { return (K + 15) / 16 * 16; }
 hipError_t launch_gemm_q8(const GemmQ8Args& a, int dt_bf16, hipStream_t stream);
+
+size_t residual_grad_ws_bytes(int R, int C, int dt_bf16);
+hipError_t launch_residual(const ResidualArgs& a, int dt_bf16, hipStream_t stream);
+hipError_t launch_residual_grad(const ResidualGradArgs& a, void* ws, int dt_bf16, hipStream_t stream);
+
+// The gated layer (gated.hip) and the backward passes of the layers (linear_grad.hip).
+size_t gated_ws_bytes(int R, int K, int F, int dt_bf16);
+hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream);
+size_t linear_grad_ws_bytes(int R, int K, int N, int dt_bf16, bool gated);
+hipError_t launch_linear_grad(const LinearGradArgs& g, int dt_bf16, hipStream_t stream);
+// rows [R, C] to rows of whole 16-byte vectors, zeros at their ends
+hipError_t launch_pack_rows(const void* src, int R, int C, void* dst, int dt_bf16, hipStream_t stream);
 
 }  // namespace gl

@@ -1,0 +1,355 @@
+// Matrix products whose operands lie either way round in memory, on MFMA:
+//   C[m, n] = sum over k of A(m, k) B(n, k)
+// The passes of a trained layer are all of this form: the outputs take x [R, K] and
+// W [N, K], both with the contraction along their rows; the input's gradient takes
+// dy [R, N] and W, whose contraction goes down its columns; the weight's gradient takes
+// dy and x, where it goes down both.  Nothing is transposed in memory:
+//   - A stage of 128 bytes of the contraction (64 bf16, 32 fp32) of both operands moves
+//     to LDS by direct loads of 16 bytes a lane, as it lies in memory: rows of 128 bytes
+//     along the contraction, or one row of the tile's width for each of its steps.
+//   - Operands of the first kind are read back 16 bytes a lane.  Of the second kind bf16
+//     goes through the transposing read of gfx950 (ds_read_tr16: 16 lanes read four
+//     steps of 16 columns and each gets its column's four), fp32 word by word.
+//   - The places of a row's 16 bytes are permuted by the row's number, so that the rows
+//     that one read touches lie in different banks.  Direct loads fill LDS in lane
+//     order: it is their source that is permuted.
+//   - Two stages of LDS and one barrier a stage.  Each wave has the second half of a
+//     stage's operands in registers before the barrier that frees the stage, so that it
+//     multiplies those while the next stage's first reads are under way.
+// Contractions are cut by whole stages where there are too few tiles to fill the chip:
+// each part writes its sums in fp32 to the workspace, and product_join adds them in order.
+#pragma once
+
+#include "act_device.h"
+#include "gl_kernels.h"
+#include "row_device.h"
+
+namespace gl {
+
+enum { kProductStore = 0, kProductPart = 1, kProductGated = 2 };
+
+struct ProductArgs {
+  const void *A, *B;
+  long long lda, ldb;  // bytes from row to row, at most 2^22
+  int M, N, K;         // K: of the contraction, in elements; whole 16 bytes where it lies along rows
+  int cols_a, cols_b;  // 16-byte places of a row, where the contraction goes down the columns
+  void* out;           // [M, N], or h [M, N] of the gated layer, whose B has 2 N rows
+  float* part;         // [parts, M, N]
+  int parts;           // workgroups in z, each with its part of the stages
+  const void* bias;    // [2 N] or null (gated)
+  void* pre;           // [M, 2 N] or null (gated)
+  int act;             // gl_act (gated)
+};
+
+// DT 1: bf16, 0: fp32.  KA, KB: the operand's contraction goes down its columns.
+template <int DT_, bool KA_, bool KB_, int BM_, int BN_, int WR_, int WC_>
+struct ProductCfg {
+  static constexpr int DT = DT_, BM = BM_, BN = BN_, WR = WR_, WC = WC_;
+  static constexpr bool KA = KA_, KB = KB_;
+  static constexpr int ES = DT ? 2 : 4, STEP = 128, BK = STEP / ES;
+  static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+  static constexpr int kStage = (BM + BN) * STEP;
+  static constexpr int LA = BM / 8 / kWaves, LB = BN / 8 / kWaves;  // loads a lane and stage
+  static constexpr int TM = BM / WR / 16, TN = BN / WC / 16;
+  static constexpr int WROWS = 16 * TM, WCOLS = 16 * TN;
+  static constexpr size_t kSmem = (size_t)2 * kStage;
+  // rows of the wave's tile that its share of LDS holds in fp32
+  static constexpr int kShare = (int)kSmem / kWaves / (WCOLS * 4);
+  static constexpr int ER = kShare >= WROWS ? WROWS : kShare / 16 * 16;
+  static_assert(LA * 8 * kWaves == BM && LB * 8 * kWaves == BN && ER >= 16 && WROWS % ER == 0, "whole loads");
+};
+
+// A direct load from a uniform base and 32 bits a lane.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_dma16_at(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// One operand's part of a stage: ROWS rows of outputs, at `at` bytes of the stage.
+// DUAL > 0: of each DUAL rows the second half lies `up` bytes from the first.
+template <int DT, bool KO, int ROWS, int WAVES, int DUAL = 0>
+struct Staged {
+  static constexpr int ES = DT ? 2 : 4, NL = ROWS / 8 / WAVES, RB = ROWS * ES, BK = 128 / ES;
+  static_assert(!KO || 1024 % RB == 0, "a wave's load is whole rows");
+  // The permutation of the 16-byte places of contraction row k (KO).  A read of half a wave
+  // touches, bf16, 32 bytes of each of rows 8 g + 0 .. 3 for two g, fp32 64 bytes of rows
+  // 4 g + j; rows of 128 bytes lie two to a line of all banks.
+  __device__ __forceinline__ static int swap(int k) {
+    if (!DT) return ((k >> 2) & 3) << 2;
+    return RB >= 256 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : (((k >> 1) & 1) | ((k >> 3) & 1) << 1) << 1;
+  }
+  const char* base;   // of the first stage to load
+  uint32_t off[NL];   // the lane's places from it
+  long long advance;  // bytes from stage to stage
+  long long up = 0;
+  int wave;
+  int k_of;           // KO: the first load's contraction row; else its place in the 128 bytes
+
+  // row(r): bytes to the operand's row r of the tile (!KO); first, cols: the tile's first
+  // 16-byte place and the places there are (KO)
+  template <class Row>
+  __device__ __forceinline__ void init(const void* p, long long ld, int w, int lane, int first, int cols, Row row) {
+    base = static_cast<const char*>(p);
+    wave = w;
+    advance = KO ? ld * BK : 128;
+    k_of = KO ? (w * 1024 + lane * 16) / RB : ((lane & 7) ^ (lane >> 3)) * 16;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int q = w + WAVES * i;
+      if (KO) {
+        const int k = (q * 1024 + lane * 16) / RB, slot = (q * 1024 + lane * 16) % RB / 16;
+        off[i] = (uint32_t)k * (uint32_t)ld + (uint32_t)min(first + (slot ^ swap(k)), cols - 1) * 16u;
+      } else {
+        const int r = 8 * q + (lane >> 3);  // r & 7 is lane >> 3
+        off[i] = row(r) + k_of;
+      }
+    }
+  }
+  // stage s to LDS; `last`: the contraction may end within it, and what is past its end is zero
+  __device__ __forceinline__ void load(int s, bool last, int K, int kin, uint32_t lds) const {
+    // (whole loads of eight rows lie in either half)
+    auto from = [&](int i) {
+      return base + s * advance + (DUAL && 8 * (wave + WAVES * i) % (DUAL ? DUAL : 1) >= DUAL / 2 ? up : 0);
+    };
+    if (!last) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) lds_dma16_at(from(i), off[i], lds + WAVES * i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const bool in = KO ? s * BK + k_of + WAVES * i * (1024 / RB) < K : s * 128 + k_of < kin;
+        lds_dma16(in ? from(i) + off[i] : reinterpret_cast<const char*>(kZero16), lds + WAVES * i * 1024);
+      }
+    }
+  }
+};
+
+// A wave's operand registers: tile `blk` of 16 rows, half kk of the stage at `st`.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <int DT, bool KO, int ROWS>
+struct Fragment {
+  static constexpr int ES = DT ? 2 : 4, RB = ROWS * ES;
+  // where the lane reads of block 0 (KO: without the block's permuted place)
+  __device__ __forceinline__ static int lane_base(int g, int t) {
+    if (!KO) return t * 128;
+    return DT ? (8 * g + (t >> 2)) * RB + 8 * (t & 3) : 4 * g * RB + t * 4;
+  }
+  __device__ __forceinline__ static int lane_swap(int g, int t) {
+    if (!KO) return 0;
+    if (!DT) return g;
+    return RB >= 256 ? (t >> 2) | (g & 1) << 2 : ((t >> 3) & 1) | (g & 1) << 1;
+  }
+  __device__ __forceinline__ static uint4 read(const char* st, int base, int swap, int blk, int kk, int g, int t) {
+    if (!KO) return *reinterpret_cast<const uint4*>(st + base + blk * 2048 + ((kk * 4 + g) ^ (t & 7)) * 16);
+    if (DT) {
+      using P = __attribute__((address_space(3))) s16x4*;
+      const char* p = st + base + kk * 32 * RB + ((blk ^ swap) << 5);
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 4 * RB));
+      const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+      return make_uint4(x.x, x.y, y.x, y.y);
+    }
+    const char* p = st + base + kk * 16 * RB + ((blk ^ swap) << 6);
+    auto word = [&](int j) { return *reinterpret_cast<const uint32_t*>(p + j * RB); };
+    return make_uint4(word(0), word(1), word(2), word(3));
+  }
+};
+
+template <int DT>
+__device__ __forceinline__ f32x4 product_mma(const uint4& b, const uint4& a, f32x4 acc) {
+  if (DT) return mfma_bf16(b, a, acc);
+  acc = mfma_f32(__uint_as_float(b.x), __uint_as_float(a.x), acc);
+  acc = mfma_f32(__uint_as_float(b.y), __uint_as_float(a.y), acc);
+  acc = mfma_f32(__uint_as_float(b.z), __uint_as_float(a.z), acc);
+  return mfma_f32(__uint_as_float(b.w), __uint_as_float(a.w), acc);
+}
+
+template <class G, int EPI>
+__device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
+  constexpr int DT = G::DT, ES = G::ES, TM = G::TM, TN = G::TN, BM = G::BM, BN = G::BN;
+  constexpr int OUT = EPI == kProductGated ? BN / 2 : BN;  // output columns of a tile
+  const int ntm = (a.M + BM - 1) / BM, ntn = (a.N + OUT - 1) / OUT;
+  // tiles by bands of eight rows of them, so that what an XCD's workgroups share is in its L2
+  const int blk = xcd_remap(blockIdx.x, gridDim.x);
+  constexpr int BAND = 8;
+  const int band = blk / (BAND * ntn), in = blk - band * BAND * ntn, high = min(BAND, ntm - band * BAND);
+  const int nt = in / high, mt = band * BAND + in - nt * high;
+  const int m0 = mt * BM, n0 = nt * OUT;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, t = lane & 15;
+  const int wm = w / G::WC, wn = w % G::WC;
+
+  const int stages = (a.K + G::BK - 1) / G::BK;
+  int s0 = 0, s1 = stages;
+  if (EPI == kProductPart) {
+    s0 = (int)((long long)stages * blockIdx.y / a.parts);
+    s1 = (int)((long long)stages * (blockIdx.y + 1) / a.parts);
+  }
+  const int kin = (a.K * ES + 15) & ~15;
+  const bool ragged = a.K % G::BK != 0;
+
+  Staged<DT, G::KA, BM, G::kWaves> la;
+  Staged<DT, G::KB, BN, G::kWaves, EPI == kProductGated ? G::WCOLS : 0> lb;
+  // rows past the last repeat it; what they give is not stored
+  la.init(static_cast<const char*>(a.A) + (G::KA ? 0 : (long long)m0 * a.lda), a.lda, w, lane, m0 * ES / 16, a.cols_a,
+          [&](int r) { return (uint32_t)min(r, a.M - 1 - m0) * (uint32_t)a.lda; });
+  if (EPI == kProductGated) {
+    // a wave's columns: as many of the gate, then the same ones of the other product
+    constexpr int H = G::WCOLS / 2;
+    lb.up = (long long)a.N * a.ldb;
+    lb.init(static_cast<const char*>(a.B) + (long long)n0 * a.ldb, a.ldb, w, lane, 0, 0, [&](int r) {
+      const int f = r / G::WCOLS * H + r % H;
+      return (uint32_t)min(f, a.N - 1 - n0) * (uint32_t)a.ldb;
+    });
+  } else {
+    lb.init(static_cast<const char*>(a.B) + (G::KB ? 0 : (long long)n0 * a.ldb), a.ldb, w, lane, n0 * ES / 16, a.cols_b,
+            [&](int r) { return (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)a.ldb; });
+  }
+  const uint32_t lds0 = lds_offset(smem) + w * 1024;
+  auto stage = [&](int s) {
+    const bool last = ragged && s == stages - 1;
+    const uint32_t d = lds0 + (s & 1) * G::kStage;
+    la.load(s, last, a.K, kin, d);
+    lb.load(s, last, a.K, kin, d + BM * 128);
+  };
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  using FA = Fragment<DT, G::KA, BM>;
+  using FB = Fragment<DT, G::KB, BN>;
+  const int abase = FA::lane_base(g, t) + (G::KA ? 0 : wm * G::WROWS * 128), aswap = FA::lane_swap(g, t);
+  const int bbase = FB::lane_base(g, t) + (G::KB ? 0 : wn * G::WCOLS * 128), bswap = FB::lane_swap(g, t);
+  const int ablk = G::KA ? wm * TM : 0, bblk = G::KB ? wn * TN : 0;
+  auto read = [&](int s, int kk, uint4* af, uint4* bf) {
+    const char* st = smem + (s & 1) * G::kStage;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) bf[j] = FB::read(st + BM * 128, bbase, bswap, bblk + j, kk, g, t);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) af[i] = FA::read(st, abase, aswap, ablk + i, kk, g, t);
+  };
+  auto multiply = [&](const uint4* af, const uint4* bf) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = product_mma<DT>(bf[j], af[i], acc[i][j]);
+  };
+  uint4 a0[TM], b0[TN], a1[TM], b1[TN];
+  if (s0 < s1) {
+    stage(s0);
+    dma_wait_barrier();
+    if (s0 + 1 < s1) stage(s0 + 1);
+    read(s0, 0, a0, b0);
+    for (int s = s0; s < s1; ++s) {
+      read(s, 1, a1, b1);
+      multiply(a0, b0);
+      // stage s + 1 has landed, and every wave has stage s in registers
+      dma_wait_barrier();
+      if (s + 2 < s1) stage(s + 2);
+      if (s + 1 < s1) read(s + 1, 0, a0, b0);
+      multiply(a1, b1);
+    }
+  }
+
+  // -- epilogue: lane (g, t) of MFMA tile (i, j) holds columns 4g .. 4g+3 of row t.  ER
+  //    rows at a time the wave writes its tile to its own part of LDS in fp32 (16-byte
+  //    places permuted by the row) and reads it back in rows, 16 bytes of output a lane
+  using T = Chunk<DT>;
+  constexpr int E = EPI == kProductPart ? 4 : T::E;
+  constexpr int COLS = EPI == kProductGated ? G::WCOLS / 2 : G::WCOLS;
+  constexpr int LPR = COLS / E, RPP = 64 / LPR, ER = G::ER, CSW = G::WCOLS / 4 < 16 ? G::WCOLS / 4 - 1 : 15;
+  static_assert(ER % RPP == 0, "whole passes");
+  const int cq = lane % LPR, rq = lane / LPR;
+  const int n = n0 + wn * COLS + cq * E;
+  float bias[2][EPI == kProductGated ? E : 1] = {};
+  if (EPI == kProductGated && a.bias) {
+#pragma unroll
+    for (int v = 0; v < E; ++v) {
+      bias[0][v] = T::load1(a.bias, min(n + v, a.N - 1));
+      bias[1][v] = T::load1(a.bias, a.N + min(n + v, a.N - 1));
+    }
+  }
+  char* st = smem + w * ((int)G::kSmem / G::kWaves);
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < G::WROWS / ER; ++e) {
+    if (e) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront"), __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < ER / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        *reinterpret_cast<f32x4*>(st + (i * 16 + t) * (G::WCOLS * 4) + (((j * 4 + g) ^ (t & CSW)) * 16)) =
+            acc[e * (ER / 16) + i][j];
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < ER / RPP; ++p) {
+      const int r = p * RPP + rq, row = m0 + wm * G::WROWS + e * ER + r;
+      const char* sr = st + r * (G::WCOLS * 4);
+      auto from = [&](int col, float* y) {  // E sums from column `col` of the wave's tile
+#pragma unroll
+        for (int v = 0; v < E; v += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(sr + (((col + v) / 4) ^ (r & CSW)) * 16);
+          y[v] = x[0], y[v + 1] = x[1], y[v + 2] = x[2], y[v + 3] = x[3];
+        }
+      };
+      auto put = [&](void* out, size_t at, const float* y) {
+        if (n + E <= a.N) {
+          T::store(out, at, y);
+        } else {
+#pragma unroll
+          for (int v = 0; v < E; ++v)
+            if (n + v < a.N) T::store1(out, at + v, y[v]);
+        }
+      };
+      if (row >= a.M || n >= a.N) continue;
+      float y[E];
+      from(cq * E, y);
+      if (EPI == kProductStore) {
+        put(a.out, (size_t)row * a.N + n, y);
+      } else if (EPI == kProductPart) {
+        float* o = a.part + ((size_t)blockIdx.y * a.M + row) * a.N + n;
+        if (n + E <= a.N) {
+          Chunk<0>::store(o, 0, y);
+        } else {
+#pragma unroll
+          for (int v = 0; v < E; ++v)
+            if (n + v < a.N) o[v] = y[v];
+        }
+      } else {
+        float u[E];
+        from(COLS + cq * E, u);
+#pragma unroll
+        for (int v = 0; v < E; ++v) y[v] += bias[0][v], u[v] += bias[1][v];
+        if (a.pre) {
+          put(a.pre, (size_t)row * 2 * a.N + n, y);
+          put(a.pre, (size_t)row * 2 * a.N + a.N + n, u);
+        }
+#pragma unroll
+        for (int v = 0; v < E; ++v) y[v] = gate_act<DT>(a.act, y[v]) * u[v];
+        put(a.out, (size_t)row * a.N + n, y);
+      }
+    }
+  }
+}
+
+template <class G, int EPI>
+__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  product_tile<G, EPI>(a, smem);
+}
+
+template <class G, int EPI>
+hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
+  constexpr int OUT = EPI == kProductGated ? G::BN / 2 : G::BN;
+  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + OUT - 1) / OUT);
+  if (tiles > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
+  return launch_with_smem((const void*)&product_kernel<G, EPI>, dim3((unsigned)tiles, EPI == kProductPart ? a.parts : 1),
+                          dim3(G::kThreads), G::kSmem, stream, nullptr, nullptr, a);
+}
+
+}  // namespace gl

@@ -15,30 +15,30 @@ constexpr int kSumGroups = 256;  // most groups of rows whose sums are kept apar
 size_t packed_row(int C, int dt_bf16) { return ((size_t)C * (dt_bf16 ? 2 : 4) + 15) & ~(size_t)15; }
 size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// rows [R, C] to rows of `row` bytes, whole 16-byte vectors with zeros at their ends
+// rows [R, C] to rows of `row` bytes, whole 16-byte vectors with zeros at their ends: 64
+// vectors of four rows a workgroup and turn
 template <int DT>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const void* src, long long R, int C, char* dst, int row) {
+__global__ __launch_bounds__(256) void pack_rows_kernel(const void* src, int R, int C, char* dst, int row) {
   using T = Chunk<DT>;
   constexpr int ES = DT ? 2 : 4, E = T::E;
-  const int per = row / 16;
-  const long long n = R * per;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += 256LL * gridDim.x) {
-    const long long r = i / per;
-    const int c = (int)(i - r * per) * E;
+  const int v = blockIdx.x * 64 + (threadIdx.x & 63), c = v * E;
+  if (v * 16 >= row) return;
+  for (long long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < R; r += 4LL * gridDim.y) {
     const char* p = static_cast<const char*>(src) + r * C * ES;
-    uint32_t v[4] = {0, 0, 0, 0};
+    uint4 q;
     if (c + E <= C) {
-      const uint4 q = T::raw(p, c);
-      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+      q = T::raw(p, c);
     } else {
+      uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < E; ++j)
         if (c + j < C) {
-          if (DT) v[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[c + j] << (j % 2 * 16);
-          else v[j] = reinterpret_cast<const uint32_t*>(p)[c + j];
+          if (DT) w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[c + j] << (j % 2 * 16);
+          else w[j] = reinterpret_cast<const uint32_t*>(p)[c + j];
         }
+      q = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    *reinterpret_cast<uint4*>(dst + i * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<uint4*>(dst + r * row + v * 16) = q;
   }
 }
 
@@ -146,6 +146,29 @@ __global__ __launch_bounds__(256) void product_join_kernel(const float* part, in
       }
     }
   }
+}
+
+// out[c] = sum over the G rows of part [G, cols]: 32 columns a workgroup, 32 rows at a time,
+// in the same order always (a thread a column took 62 us for 256 x 1536).
+__global__ __launch_bounds__(1024) void sum_groups_kernel(const float* part, int G, int cols, float* out) {
+  constexpr int COLS = 32, ROWS = 1024 / COLS;
+  __shared__ float sums[ROWS][COLS + 1];
+  const int t = threadIdx.x % COLS, w = threadIdx.x / COLS, c = blockIdx.x * COLS + t;
+  float s = 0.f;
+  for (int g0 = w; g0 < G; g0 += 8 * ROWS) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = part[(size_t)min(g0 + u * ROWS, G - 1) * cols + min(c, cols - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += g0 + u * ROWS < G ? v[u] : 0.f;
+  }
+  sums[w][t] = s;
+#pragma unroll
+  for (int h = ROWS / 2; h >= 1; h /= 2) {
+    __syncthreads();
+    if (w < h) sums[w][t] += sums[w + h][t];
+  }
+  if (w == 0 && c < cols) out[c] = sums[0][t];
 }
 
 // How a product is cut: the tile, and the parts of its contraction.
@@ -257,8 +280,7 @@ hipError_t launch_grad(const LinearGradArgs& g, hipStream_t stream) {
   else if (g.db) gate_grad_kernel<DT, false><<<grid, 256, 0, stream>>>(s);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (g.db && p.groups > 1) {
-    product_join_kernel<0><<<(unsigned)std::min((g.N + 1023) / 1024, 4096), 256, 0, stream>>>(
-        reinterpret_cast<float*>(ws + p.sums), p.groups, g.N, g.db);
+    sum_groups_kernel<<<(g.N + 31) / 32, 1024, 0, stream>>>(reinterpret_cast<float*>(ws + p.sums), p.groups, g.N, g.db);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (!gated && p.pack_dy && (g.dx || g.dW)) e = launch_pack_rows(g.dy, g.R, g.N, ws + p.dy, DT, stream);
@@ -294,8 +316,7 @@ hipError_t launch_grad(const LinearGradArgs& g, hipStream_t stream) {
 
 hipError_t launch_pack_rows(const void* src, int R, int C, void* dst, int dt_bf16, hipStream_t stream) {
   const int row = (int)packed_row(C, dt_bf16);
-  const long long n = (long long)R * (row / 16);
-  const dim3 grid((unsigned)std::min<long long>((n + 255) / 256, 8192));
+  const dim3 grid((row / 16 + 63) / 64, std::min((R + 3) / 4, 4096));
   if (dt_bf16) pack_rows_kernel<1><<<grid, 256, 0, stream>>>(src, R, C, static_cast<char*>(dst), row);
   else pack_rows_kernel<0><<<grid, 256, 0, stream>>>(src, R, C, static_cast<char*>(dst), row);
   return hipGetLastError();

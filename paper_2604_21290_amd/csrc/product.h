@@ -13,10 +13,14 @@
 //   - The places of a row's 16 bytes are permuted by the row's number, so that the rows
 //     that one read touches lie in different banks.  Direct loads fill LDS in lane
 //     order: it is their source that is permuted.
-//   - Two stages of LDS and one barrier a stage.  Each wave has the second half of a
-//     stage's operands in registers before the barrier that frees the stage, so that it
-//     multiplies those while the next stage's first reads are under way.
-// Contractions are cut by whole stages where there are too few tiles to fill the chip:
+//   - The contraction goes by halves of a stage.  Operands along it lie in a ring of whole
+//     stages (their rows are whole cache lines), operands down it in a ring of halves, whose
+//     new rows at every half come from other pages and take the longer to arrive: with two
+//     whole stages, one under way, 8192 x 4096 x 4096 took 476 us for the weight's gradient
+//     and 249 for the input's, where the output took 200.
+//   - Each wave has the next half's operands on their way to registers while it multiplies
+//     this one's; one barrier for each piece of a ring that is freed and filled again.
+// Contractions are cut by halves of stages where there are too few tiles to fill the chip:
 // each part writes its sums in fp32 to the workspace, and product_join adds them in order.
 #pragma once
 
@@ -41,22 +45,25 @@ struct ProductArgs {
   int act;             // gl_act (gated)
 };
 
-// DT 1: bf16, 0: fp32.  KA, KB: the operand's contraction goes down its columns.
+// DT 1: bf16, 0: fp32.  KA, KB: the operand's contraction goes down its columns.  Rings: two
+// stages where both lie along it; else three, and four halves of the other, or five halves of
+// both, within 160 KB for the workgroups of a CU.
 template <int DT_, bool KA_, bool KB_, int BM_, int BN_, int WR_, int WC_>
 struct ProductCfg {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, WR = WR_, WC = WC_;
   static constexpr bool KA = KA_, KB = KB_;
-  static constexpr int ES = DT ? 2 : 4, STEP = 128, BK = STEP / ES;
+  static constexpr int ES = DT ? 2 : 4, HALF = 64 / ES;  // contraction of half a stage
   static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
-  static constexpr int kStage = (BM + BN) * STEP;
-  static constexpr int LA = BM / 8 / kWaves, LB = BN / 8 / kWaves;  // loads a lane and stage
+  static constexpr int RA = KA ? (KB ? 5 : 4) : KB ? 3 : 2, RB = KB ? (KA ? 5 : 4) : KA ? 3 : 2;
+  static constexpr int kPieceA = BM * (KA ? 64 : 128), kPieceB = BN * (KB ? 64 : 128);
+  static constexpr int kPlaceB = RA * kPieceA;  // of the second operand's ring
   static constexpr int TM = BM / WR / 16, TN = BN / WC / 16;
   static constexpr int WROWS = 16 * TM, WCOLS = 16 * TN;
-  static constexpr size_t kSmem = (size_t)2 * kStage;
+  static constexpr size_t kSmem = (size_t)RA * kPieceA + RB * kPieceB;
   // rows of the wave's tile that its share of LDS holds in fp32
-  static constexpr int kShare = (int)kSmem / kWaves / (WCOLS * 4);
-  static constexpr int ER = kShare >= WROWS ? WROWS : kShare / 16 * 16;
-  static_assert(LA * 8 * kWaves == BM && LB * 8 * kWaves == BN && ER >= 16 && WROWS % ER == 0, "whole loads");
+  static constexpr int kShare = (int)kSmem / kWaves;
+  static constexpr int ER = kShare >= WROWS * WCOLS * 4 ? WROWS : kShare >= WROWS * WCOLS * 2 ? WROWS / 2 : WROWS / 4;
+  static_assert(kShare >= ER * WCOLS * 4 && ER % 16 == 0 && kSmem <= 163840, "the epilogue's rows fit");
 };
 
 // A direct load from a uniform base and 32 bits a lane.
@@ -68,12 +75,21 @@ __device__ __forceinline__ void lds_dma16_at(const char* base, uint32_t off, uin
 }
 #pragma clang diagnostic pop
 
-// One operand's part of a stage: ROWS rows of outputs, at `at` bytes of the stage.
+// All but the last N of this wave's direct loads have landed and its LDS reads are done; then
+// the workgroup's barrier.
+template <int N>
+__device__ __forceinline__ void dma_wait_barrier() {
+  static_assert(N >= 0 && N < 64, "the counter has six bits");
+  // vmcnt(N) expcnt(7) lgkmcnt(0) as the instruction's number
+  asm volatile("s_waitcnt %0\n\ts_barrier" ::"i"((N & 15) | (N >> 4) << 14 | 7 << 4) : "memory");
+}
+
+// One operand's pieces: ROWS rows of outputs by half a stage (KO) or a stage.
 // DUAL > 0: of each DUAL rows the second half lies `up` bytes from the first.
 template <int DT, bool KO, int ROWS, int WAVES, int DUAL = 0>
 struct Staged {
-  static constexpr int ES = DT ? 2 : 4, NL = ROWS / 8 / WAVES, RB = ROWS * ES, BK = 128 / ES;
-  static_assert(!KO || 1024 % RB == 0, "a wave's load is whole rows");
+  static constexpr int ES = DT ? 2 : 4, RB = ROWS * ES, BK = (KO ? 64 : 128) / ES, NL = ROWS * BK * ES / 1024 / WAVES;
+  static_assert(NL >= 1 && NL * WAVES * 1024 == ROWS * BK * ES && (!KO || 1024 % RB == 0), "whole loads, of whole rows");
   // The permutation of the 16-byte places of contraction row k (KO).  A read of half a wave
   // touches, bf16, 32 bytes of each of rows 8 g + 0 .. 3 for two g, fp32 64 bytes of rows
   // 4 g + j; rows of 128 bytes lie two to a line of all banks.
@@ -81,9 +97,9 @@ struct Staged {
     if (!DT) return ((k >> 2) & 3) << 2;
     return RB >= 256 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : (((k >> 1) & 1) | ((k >> 3) & 1) << 1) << 1;
   }
-  const char* base;   // of the first stage to load
+  const char* base;   // of the first piece
   uint32_t off[NL];   // the lane's places from it
-  long long advance;  // bytes from stage to stage
+  long long advance;  // bytes from piece to piece
   long long up = 0;
   int wave;
   int k_of;           // KO: the first load's contraction row; else its place in the 128 bytes
@@ -108,26 +124,26 @@ struct Staged {
       }
     }
   }
-  // stage s to LDS; `last`: the contraction may end within it, and what is past its end is zero
-  __device__ __forceinline__ void load(int s, bool last, int K, int kin, uint32_t lds) const {
+  // piece s to LDS; what is past the contraction's end is zero
+  __device__ __forceinline__ void load(int s, int K, uint32_t lds) const {
     // (whole loads of eight rows lie in either half)
     auto from = [&](int i) {
       return base + s * advance + (DUAL && 8 * (wave + WAVES * i) % (DUAL ? DUAL : 1) >= DUAL / 2 ? up : 0);
     };
-    if (!last) {
+    if ((s + 1) * BK <= K) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) lds_dma16_at(from(i), off[i], lds + WAVES * i * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
-        const bool in = KO ? s * BK + k_of + WAVES * i * (1024 / RB) < K : s * 128 + k_of < kin;
+        const bool in = KO ? s * BK + k_of + WAVES * i * (1024 / RB) < K : s * 128 + k_of < ((K * ES + 15) & ~15);
         lds_dma16(in ? from(i) + off[i] : reinterpret_cast<const char*>(kZero16), lds + WAVES * i * 1024);
       }
     }
   }
 };
 
-// A wave's operand registers: tile `blk` of 16 rows, half kk of the stage at `st`.
+// A wave's operand registers: tile `blk` of 16 rows of the piece at `st` (!KO: its half kk).
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 template <int DT, bool KO, int ROWS>
 struct Fragment {
@@ -146,12 +162,12 @@ struct Fragment {
     if (!KO) return *reinterpret_cast<const uint4*>(st + base + blk * 2048 + ((kk * 4 + g) ^ (t & 7)) * 16);
     if (DT) {
       using P = __attribute__((address_space(3))) s16x4*;
-      const char* p = st + base + kk * 32 * RB + ((blk ^ swap) << 5);
+      const char* p = st + base + ((blk ^ swap) << 5);
       const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 4 * RB));
       const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
       return make_uint4(x.x, x.y, y.x, y.y);
     }
-    const char* p = st + base + kk * 16 * RB + ((blk ^ swap) << 6);
+    const char* p = st + base + ((blk ^ swap) << 6);
     auto word = [&](int j) { return *reinterpret_cast<const uint32_t*>(p + j * RB); };
     return make_uint4(word(0), word(1), word(2), word(3));
   }
@@ -181,14 +197,13 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
   const int g = lane >> 4, t = lane & 15;
   const int wm = w / G::WC, wn = w % G::WC;
 
-  const int stages = (a.K + G::BK - 1) / G::BK;
-  int s0 = 0, s1 = stages;
+  // halves h0 .. h1 of the contraction, whole stages (the last half may be all zeros)
+  const long long stages = (a.K + 2 * G::HALF - 1) / (2 * G::HALF);
+  int h0 = 0, h1 = 2 * (int)stages;
   if (EPI == kProductPart) {
-    s0 = (int)((long long)stages * blockIdx.y / a.parts);
-    s1 = (int)((long long)stages * (blockIdx.y + 1) / a.parts);
+    h0 = 2 * (int)(stages * blockIdx.y / a.parts);
+    h1 = 2 * (int)(stages * (blockIdx.y + 1) / a.parts);
   }
-  const int kin = (a.K * ES + 15) & ~15;
-  const bool ragged = a.K % G::BK != 0;
 
   Staged<DT, G::KA, BM, G::kWaves> la;
   Staged<DT, G::KB, BN, G::kWaves, EPI == kProductGated ? G::WCOLS : 0> lb;
@@ -207,14 +222,6 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
     lb.init(static_cast<const char*>(a.B) + (G::KB ? 0 : (long long)n0 * a.ldb), a.ldb, w, lane, n0 * ES / 16, a.cols_b,
             [&](int r) { return (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)a.ldb; });
   }
-  const uint32_t lds0 = lds_offset(smem) + w * 1024;
-  auto stage = [&](int s) {
-    const bool last = ragged && s == stages - 1;
-    const uint32_t d = lds0 + (s & 1) * G::kStage;
-    la.load(s, last, a.K, kin, d);
-    lb.load(s, last, a.K, kin, d + BM * 128);
-  };
-
   f32x4 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -225,33 +232,81 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
   const int abase = FA::lane_base(g, t) + (G::KA ? 0 : wm * G::WROWS * 128), aswap = FA::lane_swap(g, t);
   const int bbase = FB::lane_base(g, t) + (G::KB ? 0 : wn * G::WCOLS * 128), bswap = FB::lane_swap(g, t);
   const int ablk = G::KA ? wm * TM : 0, bblk = G::KB ? wn * TN : 0;
-  auto read = [&](int s, int kk, uint4* af, uint4* bf) {
-    const char* st = smem + (s & 1) * G::kStage;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) bf[j] = FB::read(st + BM * 128, bbase, bswap, bblk + j, kk, g, t);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) af[i] = FA::read(st, abase, aswap, ablk + i, kk, g, t);
-  };
   auto multiply = [&](const uint4* af, const uint4* bf) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = product_mma<DT>(bf[j], af[i], acc[i][j]);
   };
+  // -- the rings.  Half h is piece h of an operand of halves, and half h & 1 of piece h / 2 of
+  //    one of stages.  Once every wave has half h in registers, a piece that it was the last
+  //    of is filled with the one that comes a ring later.
+  constexpr bool HA = G::KA, HB = G::KB;  // by halves
+  constexpr int RA = G::RA, RB = G::RB, NA = decltype(la)::NL, NB = decltype(lb)::NL;
+  const uint32_t lds0 = lds_offset(smem) + w * 1024;
+  uint32_t pa = 0, pb = 0;  // where half h's pieces lie in the rings
+  auto next = [](uint32_t at, int piece, int ring) { return at + piece == (uint32_t)(piece * ring) ? 0u : at + piece; };
+  // after half h (odd: of its stage)
+  auto fill = [&](int h, bool odd) {
+    if (!HA && odd && 2 * ((h >> 1) + RA) < h1) la.load((h >> 1) + RA, a.K, lds0 + pa);
+    if (!HB && odd && 2 * ((h >> 1) + RB) < h1) lb.load((h >> 1) + RB, a.K, lds0 + G::kPlaceB + pb);
+    if (HA && h + RA < h1) la.load(h + RA, a.K, lds0 + pa);
+    if (HB && h + RB < h1) lb.load(h + RB, a.K, lds0 + G::kPlaceB + pb);
+  };
+  // Loads that may be under way while half h + 1 must have landed: those issued after its own.
+  // Each turn issues the stages' (odd turns) and then the halves'.
+  //   halves: h + 1's went out in turn h + 1 - ring; the ring - 2 turns up to h - 1 follow, of
+  //     which half are odd (rounded up after an even h, as h - 1 is odd)
+  //   stages: that of h + 1 (h odd) in turn h + 2 - 2 ring; 2 ring - 2 turns' halves follow,
+  //     its own turn's among them, and ring - 2 stages
+  constexpr int per_stage = (HA ? 0 : NA) + (HB ? 0 : NB), per_half = (HA ? NA : 0) + (HB ? NB : 0);
+  constexpr int rh = HA ? RA : RB, rs = HA ? RB : RA;
+  constexpr int by_half_even = (rh - 2) * per_half + (rh - 1) / 2 * per_stage;
+  constexpr int by_half_odd = (rh - 2) * per_half + (rh - 2) / 2 * per_stage;
+  constexpr int by_stage = (rs - 2) * per_stage + (2 * rs - 2) * per_half;
+  constexpr int after_even = by_half_even;
+  constexpr int after_odd = HA && HB ? by_half_odd : HA || HB ? (by_half_odd < by_stage ? by_half_odd : by_stage) : by_stage;
+  constexpr int LAST = 2 * (RA > RB ? RA : RB);  // turns before the last whose loads all go out
+  auto read = [&](uint32_t qa, uint32_t qb, int kk, uint4* af, uint4* bf) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) bf[j] = FB::read(smem + G::kPlaceB + qb, bbase, bswap, bblk + j, kk, g, t);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) af[i] = FA::read(smem + qa, abase, aswap, ablk + i, kk, g, t);
+  };
   uint4 a0[TM], b0[TN], a1[TM], b1[TN];
-  if (s0 < s1) {
-    stage(s0);
-    dma_wait_barrier();
-    if (s0 + 1 < s1) stage(s0 + 1);
-    read(s0, 0, a0, b0);
-    for (int s = s0; s < s1; ++s) {
-      read(s, 1, a1, b1);
+  if (h0 < h1) {
+    // the rings' first filling, in the order of the turns that would have made it
+#pragma unroll
+    for (int o = 2 - LAST; o <= 0; ++o) {  // the turn before half h0 + o
+      const bool odd = (o & 1) == 0;
+      if (!HA && odd && o / 2 - 1 + RA >= 0 && h0 + 2 * (o / 2 - 1 + RA) < h1)
+        la.load(h0 / 2 + o / 2 - 1 + RA, a.K, lds0 + (o / 2 - 1 + RA) * G::kPieceA);
+      if (!HB && odd && o / 2 - 1 + RB >= 0 && h0 + 2 * (o / 2 - 1 + RB) < h1)
+        lb.load(h0 / 2 + o / 2 - 1 + RB, a.K, lds0 + G::kPlaceB + (o / 2 - 1 + RB) * G::kPieceB);
+      if (HA && o - 1 + RA >= 0 && h0 + o - 1 + RA < h1) la.load(h0 + o - 1 + RA, a.K, lds0 + (o - 1 + RA) * G::kPieceA);
+      if (HB && o - 1 + RB >= 0 && h0 + o - 1 + RB < h1)
+        lb.load(h0 + o - 1 + RB, a.K, lds0 + G::kPlaceB + (o - 1 + RB) * G::kPieceB);
+    }
+    if (h0 + LAST < h1) dma_wait_barrier<after_odd>();
+    else dma_wait_barrier();
+    read(0, 0, 0, a0, b0);
+    for (int h = h0; h < h1; h += 2) {
+      uint32_t qa = HA ? next(pa, G::kPieceA, RA) : pa, qb = HB ? next(pb, G::kPieceB, RB) : pb;
+      if constexpr (HA || HB) {
+        if (h + LAST < h1) dma_wait_barrier<after_even>();
+        else dma_wait_barrier();
+        fill(h, false);
+      }
+      read(qa, qb, 1, a1, b1);
       multiply(a0, b0);
-      // stage s + 1 has landed, and every wave has stage s in registers
-      dma_wait_barrier();
-      if (s + 2 < s1) stage(s + 2);
-      if (s + 1 < s1) read(s + 1, 0, a0, b0);
+      pa = qa, pb = qb;
+      qa = next(pa, G::kPieceA, RA), qb = next(pb, G::kPieceB, RB);
+      if (h + LAST < h1) dma_wait_barrier<after_odd>();
+      else dma_wait_barrier();
+      fill(h + 1, true);
+      if (h + 2 < h1) read(qa, qb, 0, a0, b0);
       multiply(a1, b1);
+      pa = qa, pb = qb;
     }
   }
 
@@ -273,7 +328,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
       bias[1][v] = T::load1(a.bias, a.N + min(n + v, a.N - 1));
     }
   }
-  char* st = smem + w * ((int)G::kSmem / G::kWaves);
+  char* st = smem + w * G::kShare;
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < G::WROWS / ER; ++e) {

@@ -132,8 +132,9 @@ _native = None
 
 class _NoCalls:
     """In place of _calls.so where it cannot be loaded: every form is left to the Python path."""
-    layer_norm = layer_norm_backward = quantize_rows = layer_norm_q8 = linear_q8 = staticmethod(
-        lambda *args: None)
+    layer_norm = layer_norm_backward = quantize_rows = layer_norm_q8 = linear_q8 = gated_linear = \
+        linear_backward = gated_linear_backward = residual_norm = residual_norm_backward = staticmethod(
+            lambda *args: None)
 
 
 def _calls():
@@ -622,6 +623,10 @@ def gated_linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = N
     """h[..., F] = act(g) * u with [g | u] = x W^T + bias over the last axis, W [2F, K]
     (gl_gated_linear).  keep: return (h, pre), pre [..., 2F] the products that
     gated_linear_backward takes.  The outputs are detached."""
+    if stream is None and out is None and ws is None:
+        r = (_native or _calls()).gated_linear(x, W, bias, act, keep)
+        if r is not None:
+            return r
     R, K, N = _layer("gated_linear", x, W)
     F = _halves("gated_linear", W)
     _like("bias", bias, (N,), x.dtype, x)
@@ -666,6 +671,10 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, need=(Tr
     gradient dy [..., Cout] (gl_linear_backward); dW in x's type, dbias a float32 sum over
     all rows.  need: which of the three to compute (None for the others).  ws: the call's
     workspace (allocated here when not given)."""
+    if stream is None and ws is None and any(need):
+        r = (_native or _calls()).linear_backward(dy, x, W, *need)
+        if r is not None:
+            return r
     R, K, N = _layer("linear_backward", x, W)
     _matrix("dy", dy, x.shape[:-1] + (N,), x)
     dt = _dt(x)
@@ -683,6 +692,10 @@ def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pr
     """(dx, dW, dbias) of gated_linear from its output's gradient dh [..., F], its input and
     weight, and the products that it kept (gl_gated_linear_backward); dW in x's type,
     dbias [2F] a float32 sum over all rows.  need and ws as in linear_backward."""
+    if stream is None and ws is None and any(need):
+        r = (_native or _calls()).gated_linear_backward(dh, x, W, pre, act, *need)
+        if r is not None:
+            return r
     R, K, N = _layer("gated_linear_backward", x, W)
     F = _halves("gated_linear_backward", W)
     _matrix("dh", dh, x.shape[:-1] + (F,), x)
@@ -745,6 +758,10 @@ def residual_norm(x: torch.Tensor, b: torch.Tensor, post=None, scale: torch.Tens
     row's).  kind: GL_NORM_LAYER or GL_NORM_RMS.  x and b may be slices of wider rows.
     stats: return (s, y, ResidualStats), which residual_norm_backward takes.  The outputs
     are detached."""
+    if stream is None:
+        r = (_native or _calls()).residual_norm(x, b, post, scale, gate, norm, kind, eps, stats)
+        if r is not None:
+            return (r[0], r[1], ResidualStats(*r[2])) if stats else r
     R, C, ldx = _rows(x)
     Rb, Cb, ldb = _rows(b)
     if b.shape != x.shape or b.dtype != x.dtype or b.get_device() != x.get_device():
@@ -781,6 +798,10 @@ def residual_norm_backward(ds: torch.Tensor | None, dy: torch.Tensor | None, b: 
     """The gradients of residual_norm, from those of its outputs (either may be None), what
     it was given and returned, and its ResidualStats (gl_residual_norm_backward).  ws: the
     call's workspace (allocated here when not given)."""
+    if stream is None and ws is None:
+        r = (_native or _calls()).residual_norm_backward(ds, dy, b, s, stats, post, scale, gate, norm, kind)
+        if r is not None:
+            return ResidualGrads(*r)
     R, C, ldb = _rows(b)
     if ds is None and dy is None:
         raise ValueError("ds or dy is required")

@@ -97,10 +97,10 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
 
 template <int DT>
 hipError_t launch_tiles(const ProductArgs& a, hipStream_t stream) {
-  auto tiles = [&](int b) { return ((long long)(a.M + b - 1) / b) * ((2LL * a.N + b - 1) / b); };
+  const int tile = product_cut(a.M, 2LL * a.N, a.K, DT, false).tile;
   if constexpr (DT == 1)
-    if (tiles(256) >= 200) return launch_product<ProductCfg<1, false, false, 256, 256, 2, 4>, kProductGated>(a, stream);
-  if (tiles(128) >= 200) return launch_product<ProductCfg<DT, false, false, 128, 128, 2, 2>, kProductGated>(a, stream);
+    if (tile == 256) return launch_product<ProductCfg<1, false, false, 256, 256, 2, 4>, kProductGated>(a, stream);
+  if (tile == 128) return launch_product<ProductCfg<DT, false, false, 128, 128, 2, 2>, kProductGated>(a, stream);
   return launch_product<ProductCfg<DT, false, false, 64, 64, 2, 2>, kProductGated>(a, stream);
 }
 

@@ -171,26 +171,7 @@ __global__ __launch_bounds__(1024) void sum_groups_kernel(const float* part, int
   if (w == 0 && c < cols) out[c] = sums[0][t];
 }
 
-// How a product is cut: the tile, and the parts of its contraction.
-struct Cut {
-  int tile, parts;
-};
-
-Cut cut(long long M, long long N, long long K, int dt_bf16) {
-  const long long stages = (K + (dt_bf16 ? 63 : 31)) / (dt_bf16 ? 64 : 32);
-  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  const int tile = dt_bf16 && tiles(256) * std::max<long long>(1, stages / 16) >= 200 ? 256
-                   : tiles(128) * std::max<long long>(1, stages / 8) >= 200         ? 128
-                                                                                    : 64;
-  const long long want = tile == 256 ? 256 : tile == 128 ? 512 : 1024, have = tiles(tile);
-  const long long most = std::max<long long>(1, stages / 4);
-  long long parts = have >= want * 3 / 4 ? 1 : std::min(most, want / have);
-  // the parts' sums stay within 256 MiB
-  parts = std::max<long long>(1, std::min<long long>(parts, (256LL << 20) / (M * N * 4)));
-  return Cut{tile, (int)std::min<long long>(parts, 64)};
-}
-
-size_t part_bytes(const Cut& c, long long M, long long N) { return c.parts > 1 ? (size_t)c.parts * M * N * 4 : 0; }
+size_t part_bytes(const ProductCut& c, long long M, long long N) { return c.parts > 1 ? (size_t)c.parts * M * N * 4 : 0; }
 
 template <int DT, bool KA, bool KB, int EPI>
 hipError_t launch_cut(const ProductArgs& a, int tile, hipStream_t stream) {
@@ -202,7 +183,7 @@ hipError_t launch_cut(const ProductArgs& a, int tile, hipStream_t stream) {
 
 template <int DT, bool KA, bool KB>
 hipError_t product(ProductArgs a, float* part, hipStream_t stream) {
-  const Cut c = cut(a.M, a.N, a.K, DT);
+  const ProductCut c = product_cut(a.M, a.N, a.K, DT, true);
   if (c.parts == 1) return launch_cut<DT, KA, KB, kProductStore>(a, c.tile, stream);
   a.parts = c.parts;
   a.part = part;
@@ -245,7 +226,8 @@ GradPlan plan(int R, int K, int N, int dt_bf16, bool gated) {
   if (p.pack_dy) p.dy = take(R * packed_row(N, dt_bf16));
   p.groups = sum_groups(R, gated ? N / 2 : N, dt_bf16);
   p.sums = take(p.groups > 1 ? (size_t)p.groups * N * 4 : 0);
-  p.part = take(std::max(part_bytes(cut(R, K, N, dt_bf16), R, K), part_bytes(cut(N, K, R, dt_bf16), N, K)));
+  p.part = take(std::max(part_bytes(product_cut(R, K, N, dt_bf16, true), R, K),
+                         part_bytes(product_cut(N, K, R, dt_bf16, true), N, K)));
   p.bytes = at;
   return p;
 }

@@ -24,6 +24,8 @@
 // each part writes its sums in fp32 to the workspace, and product_join adds them in order.
 #pragma once
 
+#include <algorithm>
+
 #include "act_device.h"
 #include "gl_kernels.h"
 #include "row_device.h"
@@ -39,7 +41,7 @@ struct ProductArgs {
   int cols_a, cols_b;  // 16-byte places of a row, where the contraction goes down the columns
   void* out;           // [M, N], or h [M, N] of the gated layer, whose B has 2 N rows
   float* part;         // [parts, M, N]
-  int parts;           // workgroups in z, each with its part of the stages
+  int parts;           // of the contraction, whole stages each
   const void* bias;    // [2 N] or null (gated)
   void* pre;           // [M, 2 N] or null (gated)
   int act;             // gl_act (gated)
@@ -188,7 +190,11 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
   constexpr int OUT = EPI == kProductGated ? BN / 2 : BN;  // output columns of a tile
   const int ntm = (a.M + BM - 1) / BM, ntn = (a.N + OUT - 1) / OUT;
   // tiles by bands of eight rows of them, so that what an XCD's workgroups share is in its L2
-  const int blk = xcd_remap(blockIdx.x, gridDim.x);
+  int blk = xcd_remap(blockIdx.x, gridDim.x), part = 0;
+  if (EPI == kProductPart) {
+    part = blk / (ntm * ntn);
+    blk -= part * ntm * ntn;
+  }
   constexpr int BAND = 8;
   const int band = blk / (BAND * ntn), in = blk - band * BAND * ntn, high = min(BAND, ntm - band * BAND);
   const int nt = in / high, mt = band * BAND + in - nt * high;
@@ -201,8 +207,8 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
   const long long stages = (a.K + 2 * G::HALF - 1) / (2 * G::HALF);
   int h0 = 0, h1 = 2 * (int)stages;
   if (EPI == kProductPart) {
-    h0 = 2 * (int)(stages * blockIdx.y / a.parts);
-    h1 = 2 * (int)(stages * (blockIdx.y + 1) / a.parts);
+    h0 = 2 * (int)(stages * part / a.parts);
+    h1 = 2 * (int)(stages * (part + 1) / a.parts);
   }
 
   Staged<DT, G::KA, BM, G::kWaves> la;
@@ -367,7 +373,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
       if (EPI == kProductStore) {
         put(a.out, (size_t)row * a.N + n, y);
       } else if (EPI == kProductPart) {
-        float* o = a.part + ((size_t)blockIdx.y * a.M + row) * a.N + n;
+        float* o = a.part + ((size_t)part * a.M + row) * a.N + n;
         if (n + E <= a.N) {
           Chunk<0>::store(o, 0, y);
         } else {
@@ -401,10 +407,54 @@ __global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 template <class G, int EPI>
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
   constexpr int OUT = EPI == kProductGated ? G::BN / 2 : G::BN;
-  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + OUT - 1) / OUT);
+  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + OUT - 1) / OUT) * (EPI == kProductPart ? a.parts : 1);
   if (tiles > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
-  return launch_with_smem((const void*)&product_kernel<G, EPI>, dim3((unsigned)tiles, EPI == kProductPart ? a.parts : 1),
+  return launch_with_smem((const void*)&product_kernel<G, EPI>, dim3((unsigned)tiles),
                           dim3(G::kThreads), G::kSmem, stream, nullptr, nullptr, a);
+}
+
+// How a product is cut: the tile (256, 128 or 64 outputs each way) and the parts of its
+// contraction, by an estimate of its time in us.  Workgroups of 128 and 64 lie two and four
+// to a CU: a stage takes them a + b n, n of them, and a round of workgroups 1 to 4.5 us more
+// (its first stage's trip, its stores); parts cost a launch and their sums' way through
+// memory.  Measured, us (tile, parts; * taken), bf16:
+//                                  256        128        128, parts  64
+//   dx 16384 x 2048 x 8192         481 *      491                    1136
+//   dW 16384 x 2048 x 8192         462 *      565        612, 2      1541
+//   dx 12544 x 640 x 5120          122        77.2 *     98.1, 2     126
+//   dW 12544 x 640 x 5120          143, 4     145        98.5, 5 *   164, 2
+//   dx 12544 x 2560 x 640          46.4 *     50.8                   68.3
+//   dW 12544 x 2560 x 640          82.5, 8    68.1, 3    52.4, 5 *   79.5, 5
+//   dx 2000 x 4096 x 1024          33.2       22.0 *     42.6, 2     31.3
+struct ProductCut {
+  int tile, parts;
+};
+
+inline ProductCut product_cut(long long M, long long N, long long K, int dt_bf16, bool parts) {
+  struct Tile {
+    int size, per_cu;
+    double a, b, round;
+  };
+  constexpr Tile kBf16[] = {{256, 1, 0.0, 1.85, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}};
+  constexpr Tile kF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.15, 0.5, 1.5}};
+  const long long stages = (K + (dt_bf16 ? 63 : 31)) / (dt_bf16 ? 64 : 32);
+  ProductCut best{64, 1};
+  double least = 1e300;
+  for (int i = 0; i < (dt_bf16 ? 3 : 2); ++i) {
+    const Tile& t = dt_bf16 ? kBf16[i] : kF32[i];
+    const long long tiles = ((M + t.size - 1) / t.size) * ((N + t.size - 1) / t.size);
+    // (at least four stages a part; the parts' sums stay within 256 MiB)
+    const long long most = !parts ? 1 : std::max<long long>(1, std::min<long long>({64, stages / 4, (64LL << 20) / (M * N)}));
+    for (long long p = 1; p <= most; ++p) {
+      const long long all = tiles * p, slots = 256LL * t.per_cu, rest = all % slots;
+      const double n = (double)((stages + p - 1) / p);
+      double us = (double)(all / slots) * (n * (t.a + t.b * t.per_cu) + t.round);
+      if (rest) us += n * (t.a + t.b * (double)((rest + 255) / 256)) + t.round;
+      if (p > 1) us += 5.0 + (double)(8 * p + 4) * (double)(M * N) / 5.5e6;
+      if (us < least) least = us, best = ProductCut{t.size, (int)p};
+    }
+  }
+  return best;
 }
 
 }  // namespace gl

@@ -37,7 +37,7 @@ __device__ __forceinline__ float join_sum(float v, uint32_t* slot) {
 
 // LPR lanes hold a row, VPL chunks each; LPR 0: a workgroup of any number of waves does.
 template <int DT, int LPR, int VPL, bool POST>
-__global__ __launch_bounds__(LPR ? 256 : 1024) void residual_kernel(ResidualArgs a) {
+__global__ __launch_bounds__(LPR ? 256 : 512) void residual_kernel(ResidualArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, GROUPS = LPR ? 256 / (LPR ? LPR : 1) : 1;
   __shared__ uint32_t slots[2][4][16];
@@ -232,9 +232,18 @@ hipError_t launch_rows(const ResidualArgs& a, hipStream_t stream) {
     if (n <= 32 && a.R >= 4096) return go((const void*)&residual_kernel<DT, 16, 2, POST>, 16, 256, 16);
   }
   if (n <= 64) return go((const void*)&residual_kernel<DT, 64, 1, POST>, 4, 256, 16);
-  if (n <= 128) return go((const void*)&residual_kernel<DT, 64, 2, POST>, 4, 256, 16);
-  if (n <= 1024) return go((const void*)&residual_kernel<DT, 0, 1, POST>, 1, (n + 63) / 64 * 64, std::max(1, 2048 / n));
-  return go((const void*)&residual_kernel<DT, 0, 2, POST>, 1, (n + 127) / 128 * 64, 2);
+  if (n > 96 && n <= 128) return go((const void*)&residual_kernel<DT, 64, 2, POST>, 4, 256, 16);
+  if (n > 128 && n <= 192) return go((const void*)&residual_kernel<DT, 64, 3, POST>, 4, 256, 3);
+  // A row a workgroup: three or two chunks a lane, whichever leaves fewer lanes idle (fewer
+  // waves meet for a row's sums: 32768 x 2560 bf16, 3 x 2 waves 134 us, 2 x 3 waves 146, 1 x
+  // 5 waves 183 with as many workgroups as fit); as many workgroups as are resident together.
+  const int vpl = n <= 96 ? 1 : n > 1024 ? 4 : (n + 191) / 192 * 3 <= (n + 127) / 128 * 2 ? 3 : 2;
+  const int waves = (n + 64 * vpl - 1) / (64 * vpl), resident = vpl == 1 ? 24 : vpl == 2 ? (DT ? 16 : 12) : vpl == 3 ? 12 : 8;
+  return go(vpl == 1   ? (const void*)&residual_kernel<DT, 0, 1, POST>
+            : vpl == 2 ? (const void*)&residual_kernel<DT, 0, 2, POST>
+            : vpl == 3 ? (const void*)&residual_kernel<DT, 0, 3, POST>
+                       : (const void*)&residual_kernel<DT, 0, 4, POST>,
+            1, 64 * waves, std::max(vpl == 2 ? 2 : 1, resident / waves));
 }
 
 }  // namespace

@@ -246,24 +246,42 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
   }
 }
 
-// The groups' sums, and the vectors' gradients from them: 32 columns a workgroup, 32 groups
-// at a time, in the same order always.
+// The groups' sums and the vectors' gradients from them: 32 columns a workgroup, 32 groups
+// at a time and eight of those under way, in the same order always.  Workgroups past
+// `vectors` sum the gates' rows, a wave or (many rows) a workgroup each.
+constexpr int kGateWave = 512;
 template <int DT>
-__global__ __launch_bounds__(1024) void residual_vectors_kernel(ResidualGradArgs a, int G) {
+__global__ __launch_bounds__(1024) void residual_vectors_kernel(ResidualGradArgs a, int G, int vectors) {
   using T = Chunk<DT>;
-  constexpr int COLS = 32, ROWS = 1024 / COLS;
+  constexpr int COLS = 32, ROWS = 1024 / COLS, U = 8;
   __shared__ float sums[4][ROWS][COLS + 1];
+  if ((int)blockIdx.x >= vectors) {
+    const long long gates = ((long long)a.R + a.per_gate - 1) / a.per_gate;
+    const bool wide = a.per_gate > kGateWave;
+    const int id = blockIdx.x - vectors, lanes = wide ? 1024 : 64, lane = threadIdx.x & (lanes - 1);
+    const long long step = ((long long)gridDim.x - vectors) * (1024 / lanes);
+    for (long long gate = (long long)id * (1024 / lanes) + threadIdx.x / lanes; gate < gates; gate += step) {
+      const long long first = gate * a.per_gate, end = min(first + a.per_gate, (long long)a.R);
+      float s = 0.f;
+      for (long long r = first + lane; r < end; r += lanes) s += a.dots[r];
+      s = wide ? sum_row<1024>(s, reinterpret_cast<uint32_t*>(sums)) : sum_row<64>(s, nullptr);
+      if (lane == 0) a.dgate[gate] = s;
+      if (wide) __syncthreads();  // the words of sums are free again
+    }
+    return;
+  }
   const int t = threadIdx.x % COLS, w = threadIdx.x / COLS, C = a.C;
-  const int c = blockIdx.x * COLS + t, col = min(c, C - 1);
+  for (int c0 = blockIdx.x * COLS; c0 < C; c0 += vectors * COLS) {
+  const int c = c0 + t, col = min(c, C - 1);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int g0 = w; g0 < G; g0 += 2 * ROWS) {
-    float v[2][4];
+  for (int g0 = w; g0 < G; g0 += U * ROWS) {
+    float v[U][4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[u][q] = a.part[((size_t)min(g0 + u * ROWS, G - 1) * 4 + q) * C + col];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q) s[q] += g0 + u * ROWS < G ? v[u][q] : 0.f;
   }
@@ -276,25 +294,18 @@ __global__ __launch_bounds__(1024) void residual_vectors_kernel(ResidualGradArgs
 #pragma unroll
       for (int q = 0; q < 4; ++q) sums[q][w][t] += sums[q][w + h][t];
   }
-  if (w || c >= C) return;
-  const float S1 = sums[0][0][t], S0 = sums[1][0][t];
-  const float sc = a.scale ? T::load1(a.scale, c) : 1.f;
-  if (a.dscale)
-    a.dscale[c] = a.post ? fmaf(a.gamma1 ? T::load1(a.gamma1, c) : 1.f, S1, a.beta1 ? T::load1(a.beta1, c) * S0 : 0.f) : S1;
-  if (a.dgamma1) a.dgamma1[c] = sc * S1;
-  if (a.dbeta1) a.dbeta1[c] = sc * S0;
-  if (a.dgamma2) a.dgamma2[c] = sums[2][0][t];
-  if (a.dbeta2) a.dbeta2[c] = sums[3][0][t];
-}
-
-// A gate's rows, a workgroup each.
-__global__ __launch_bounds__(256) void residual_gate_kernel(const float* dots, int R, int per_gate, float* dgate) {
-  __shared__ uint32_t slots[4];
-  const long long first = (long long)blockIdx.x * per_gate, end = min(first + per_gate, (long long)R);
-  float s = 0.f;
-  for (long long r = first + threadIdx.x; r < end; r += 256) s += dots[r];
-  s = sum_row<256>(s, slots);
-  if (threadIdx.x == 0) dgate[blockIdx.x] = s;
+  if (!w && c < C) {
+    const float S1 = sums[0][0][t], S0 = sums[1][0][t];
+    const float sc = a.scale ? T::load1(a.scale, c) : 1.f;
+    if (a.dscale)
+      a.dscale[c] = a.post ? fmaf(a.gamma1 ? T::load1(a.gamma1, c) : 1.f, S1, a.beta1 ? T::load1(a.beta1, c) * S0 : 0.f) : S1;
+    if (a.dgamma1) a.dgamma1[c] = sc * S1;
+    if (a.dbeta1) a.dbeta1[c] = sc * S0;
+    if (a.dgamma2) a.dgamma2[c] = sums[2][0][t];
+    if (a.dbeta2) a.dbeta2[c] = sums[3][0][t];
+  }
+  __syncthreads();  // sums is free again
+  }
 }
 
 // Rows shorter than a chunk or longer than the largest tile: dx and db a workgroup a row,
@@ -412,8 +423,13 @@ Plan plan(int R, int C, bool near) {
   }
   if (n <= 64) return make(64, 1, 512, 512);
   if (n <= 128) return make(64, 2, 512, 256);
-  if (n <= 512) return make(0, 1, (n + 63) / 64 * 64, std::max(256, std::min(1024, 256 * (1024 / n))));
-  return make(0, 2, (n + 127) / 128 * 64, 256);
+  // A row a workgroup, as many of them as are resident together.  us, chunks a lane x waves:
+  //   bf16 32768 x 2560  2 x 3 266, 1 x 5 342      8192 x 4096  2 x 4 98, 1 x 8 120
+  //        20000 x 1536  1 x 3 88, 2 x 2 99
+  //   fp32 32768 x 2560  3 x 4 381, 2 x 5 439      8192 x 4096  3 x 6 168, 2 x 8 164
+  //        20000 x 1536  1 x 6 140, 3 x 2 145
+  const int vpl = n <= (DT ? 256 : 512) ? 1 : DT || n > 1536 ? 2 : 3, waves = (n + 64 * vpl - 1) / (64 * vpl);
+  return make(0, vpl, 64 * waves, 256 * std::max(1, (vpl == 1 ? 12 : 8) / waves));
 }
 
 size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -447,16 +463,15 @@ hipError_t launch_rows(ResidualGradArgs a, void* ws, hipStream_t stream) {
     e = go(p.vpl == 1 ? (const void*)&residual_grad_kernel<DT, 64, 1, POST> : (const void*)&residual_grad_kernel<DT, 64, 2, POST>);
   } else {
     e = go(p.vpl == 1                 ? (const void*)&residual_grad_kernel<DT, 0, 1, POST>
+           : p.vpl == 3               ? (const void*)&residual_grad_kernel<DT, 0, DT ? 2 : 3, POST>
            : DT || p.threads <= 512 ? (const void*)&residual_grad_kernel<DT, 0, 2, POST>
                                     : (const void*)&residual_grad_kernel<DT, 0, 2, POST, DT ? 512 : 1024>);
   }
-  if (e == hipSuccess && sums) {
-    residual_vectors_kernel<DT><<<(a.C + 31) / 32, 1024, 0, stream>>>(a, p.grid);
-    e = hipGetLastError();
-  }
-  if (e == hipSuccess && a.dgate && a.per_gate > 1) {
-    const int gates = (a.R + a.per_gate - 1) / a.per_gate;
-    residual_gate_kernel<<<gates, 256, 0, stream>>>(a.dots, a.R, a.per_gate, a.dgate);
+  const int vectors = sums ? std::min((a.C + 31) / 32, 1 << 16) : 0;
+  long long gates = a.dgate && a.per_gate > 1 ? ((long long)a.R + a.per_gate - 1) / a.per_gate : 0;
+  gates = std::min<long long>(a.per_gate > kGateWave ? gates : (gates + 15) / 16, 1 << 16);
+  if (e == hipSuccess && vectors + gates) {
+    residual_vectors_kernel<DT><<<(unsigned)(vectors + gates), 1024, 0, stream>>>(a, p.grid, vectors);
     e = hipGetLastError();
   }
   return e;

@@ -310,7 +310,9 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
       if (h + LAST < h1) dma_wait_barrier<after_odd>();
       else dma_wait_barrier();
       fill(h + 1, true);
-      if (h + 2 < h1) read(qa, qb, 0, a0, b0);
+      // (after the last half too, of whatever lies there: behind a branch the compiler would
+      // not know how many reads are under way, and wait for these before it multiplies)
+      read(qa, qb, 0, a0, b0);
       multiply(a1, b1);
       pa = qa, pb = qb;
     }

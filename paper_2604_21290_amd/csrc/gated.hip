@@ -82,10 +82,6 @@ __global__ __launch_bounds__(512) void gated_few_kernel(ProductArgs a) {
 
 constexpr int kFewRows = 64;
 
-// bytes of a row brought to whole 16-byte vectors
-size_t packed_row(int C, int dt_bf16) { return ((size_t)C * (dt_bf16 ? 2 : 4) + 15) & ~(size_t)15; }
-size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
-
 template <int DT>
 hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
   const void* fn = a.M <= 16   ? (const void*)&gated_few_kernel<DT, 1>
@@ -95,13 +91,21 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
   return hipLaunchKernel(fn, dim3((a.N + 15) / 16), dim3(512), argv, 0, stream);
 }
 
+template <class G>
+hipError_t launch_tile(const ProductArgs& a, hipStream_t stream) {
+  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + G::BN / 2 - 1) / (G::BN / 2));
+  if (tiles > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
+  return launch_with_smem((const void*)&product_gated_kernel<G>, dim3((unsigned)tiles), dim3(G::kThreads), G::kSmem, stream,
+                          nullptr, nullptr, a);
+}
+
 template <int DT>
 hipError_t launch_tiles(const ProductArgs& a, hipStream_t stream) {
-  const int tile = product_cut(a.M, 2LL * a.N, a.K, DT, false).tile;
+  const int tile = product_cut({a.M, 2LL * a.N, a.K}, DT, false).tile;
   if constexpr (DT == 1)
-    if (tile == 256) return launch_product<ProductCfg<1, false, false, 256, 256, 2, 4>, kProductGated>(a, stream);
-  if (tile == 128) return launch_product<ProductCfg<DT, false, false, 128, 128, 2, 2>, kProductGated>(a, stream);
-  return launch_product<ProductCfg<DT, false, false, 64, 64, 2, 2>, kProductGated>(a, stream);
+    if (tile == 256) return launch_tile<ProductCfg<1, false, false, 256, 256, 2, 4>>(a, stream);
+  if (tile == 128) return launch_tile<ProductCfg<DT, false, false, 128, 128, 2, 2>>(a, stream);
+  return launch_tile<ProductCfg<DT, false, false, 64, 64, 2, 2>>(a, stream);
 }
 
 }  // namespace
@@ -129,8 +133,7 @@ hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream) {
   if (g.K % (16 / es)) {  // rows of whole vectors in the workspace
     const size_t row = packed_row(g.K, dt_bf16);
     char *x = static_cast<char*>(g.ws), *W = x + whole256(g.R * row);
-    hipError_t e = launch_pack_rows(g.x, g.R, g.K, x, dt_bf16, stream);
-    if (e == hipSuccess) e = launch_pack_rows(g.W, 2 * g.F, g.K, W, dt_bf16, stream);
+    hipError_t e = launch_pack_rows(PackPair{{{g.x, x, g.R, g.K}, {g.W, W, 2 * g.F, g.K}}}, dt_bf16, stream);
     if (e != hipSuccess) return e;
     a.A = x;
     a.B = W;

@@ -279,6 +279,17 @@ hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream);
 size_t linear_grad_ws_bytes(int R, int K, int N, int dt_bf16, bool gated);
 hipError_t launch_linear_grad(const LinearGradArgs& g, int dt_bf16, hipStream_t stream);
 // rows [R, C] to rows of whole 16-byte vectors, zeros at their ends
-hipError_t launch_pack_rows(const void* src, int R, int C, void* dst, int dt_bf16, hipStream_t stream);
+struct PackRows {
+  const void* src;
+  void* dst;
+  int R, C;
+};
+struct PackPair {
+  PackRows t[2];  // src null: none
+};
+hipError_t launch_pack_rows(const PackPair& p, int dt_bf16, hipStream_t stream);
+// bytes of such a row
+inline size_t packed_row(int C, int dt_bf16) { return ((size_t)C * (dt_bf16 ? 2 : 4) + 15) & ~(size_t)15; }
+inline size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace gl

@@ -12,19 +12,17 @@ namespace {
 
 constexpr int kSumGroups = 256;  // most groups of rows whose sums are kept apart
 
-size_t packed_row(int C, int dt_bf16) { return ((size_t)C * (dt_bf16 ? 2 : 4) + 15) & ~(size_t)15; }
-size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// rows [R, C] to rows of `row` bytes, whole 16-byte vectors with zeros at their ends: 64
-// vectors of four rows a workgroup and turn
+// rows [R, C] to rows of whole 16-byte vectors with zeros at their ends: 64 vectors of four
+// rows a workgroup and turn, workgroup `id` of `count`
 template <int DT>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const void* src, int R, int C, char* dst, int row) {
+__device__ __forceinline__ void pack_rows(const PackRows& a, int id, int count) {
   using T = Chunk<DT>;
   constexpr int ES = DT ? 2 : 4, E = T::E;
-  const int v = blockIdx.x * 64 + (threadIdx.x & 63), c = v * E;
+  const int C = a.C, row = (C * ES + 15) & ~15, across = (row / 16 + 63) / 64;
+  const int y = id / across, v = (id - y * across) * 64 + (threadIdx.x & 63), c = v * E;
   if (v * 16 >= row) return;
-  for (long long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < R; r += 4LL * gridDim.y) {
-    const char* p = static_cast<const char*>(src) + r * C * ES;
+  for (long long r = y * 4 + (threadIdx.x >> 6); r < a.R; r += 4LL * (count / across)) {
+    const char* p = static_cast<const char*>(a.src) + r * C * ES;
     uint4 q;
     if (c + E <= C) {
       q = T::raw(p, c);
@@ -38,26 +36,51 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const void* src, int R, 
         }
       q = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    *reinterpret_cast<uint4*>(dst + r * row + v * 16) = q;
+    *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + r * row + v * 16) = q;
   }
 }
+// workgroups for it, whole rows of them
+int pack_count(const PackRows& a, int dt_bf16) {
+  if (!a.src) return 0;
+  const int across = (int)((packed_row(a.C, dt_bf16) / 16 + 63) / 64);
+  return across * std::min((a.R + 3) / 4, std::max(1, 4096 / across));
+}
 
-struct GateGradArgs {
-  const void *dh, *pre;  // [R, F], [R, 2 F]
-  char* dpre;            // rows of `row` bytes: dpre, then zeros
-  float* part;           // [gridDim.y, 2 F]: the groups' sums of dpre, or null
+template <int DT>
+__global__ __launch_bounds__(256) void pack_rows_kernel(PackPair p, int first) {
+  if ((int)blockIdx.x < first) pack_rows<DT>(p.t[0], blockIdx.x, first);
+  else pack_rows<DT>(p.t[1], blockIdx.x - first, gridDim.x - first);
+}
+
+// What comes before the products, in one launch: dpre and its sums over groups of rows
+// (GATED), or the sums of dy and, where its rows are no whole vectors, their copy; and the
+// copies of x and W.
+struct PrepareArgs {
+  const void *dy, *pre;  // [R, F] (GATED: dh), [R, 2 F]
+  char* out;             // rows of `row` bytes: dpre or dy, then zeros; null: not wanted
+  float* part;           // [groups, 2 F or F]: the groups' sums, or null
   int R, F, row, act;
+  int across, groups;    // workgroups: by columns, by groups of rows
+  PackPair pack;
+  int pack_first;        // workgroups of the first copy
 };
 
 // 32 lanes take 32 chunks of columns, eight rows a turn.
-// dpre and its groups' sums (GATED), or the sums of rows dh alone.
 template <int DT, bool GATED>
-__global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs a) {
+__global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   using T = Chunk<DT>;
   constexpr int E = T::E, ES = DT ? 2 : 4, CL = 32, RL = 256 / CL, NS = GATED ? 2 : 1;
   __shared__ float sums[RL][CL * E + 4];
+  int id = blockIdx.x;
+  if (id >= a.across * a.groups) {
+    id -= a.across * a.groups;
+    if (id < a.pack_first) pack_rows<DT>(a.pack.t[0], id, a.pack_first);
+    else pack_rows<DT>(a.pack.t[1], id - a.pack_first, gridDim.x - a.across * a.groups - a.pack_first);
+    return;
+  }
+  const int group = id / a.across, block = id - group * a.across;
   const int lane = threadIdx.x % CL, rl = threadIdx.x / CL;
-  const int F = a.F, c = (blockIdx.x * CL + lane) * E;
+  const int F = a.F, c = (block * CL + lane) * E;
   const bool on = c < F, whole = c + E <= F;
   auto load = [&](const void* p, size_t at, float* f) {
     if (whole) {
@@ -77,33 +100,36 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs a) {
     }
   };
   float s[NS][E] = {};
-  const long long step = (long long)RL * gridDim.y;
+  const long long step = (long long)RL * a.groups;
   if (on)
-    for (long long r = (long long)blockIdx.y * RL + rl; r < a.R; r += step) {
+    for (long long r = (long long)group * RL + rl; r < a.R; r += step) {
       float d[E];
-      load(a.dh, (size_t)r * F + c, d);
-      if (!GATED) {
+      load(a.dy, (size_t)r * F + c, d);
+      char* o = a.out + (size_t)r * a.row;
+      if (GATED) {
+        float p[E], u[E];
+        load(a.pre, (size_t)r * 2 * F + c, p);
+        load(a.pre, (size_t)r * 2 * F + F + c, u);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          float da;
+          const float act = gate_act_grad(a.act, p[j], &da);
+          p[j] = d[j] * u[j] * da;
+          u[j] = d[j] * act;
+          s[0][j] += p[j];
+          s[NS - 1][j] += u[j];
+        }
+        if (a.out) {
+          put(o, c, p);
+          put(o, F + c, u);
+        }
+      } else {
 #pragma unroll
         for (int j = 0; j < E; ++j) s[0][j] += d[j];
-        continue;
+        if (a.out) put(o, c, d);
       }
-      float p[E], u[E];
-      load(a.pre, (size_t)r * 2 * F + c, p);
-      load(a.pre, (size_t)r * 2 * F + F + c, u);
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        float da;
-        const float act = gate_act_grad(a.act, p[j], &da);
-        p[j] = d[j] * u[j] * da;
-        u[j] = d[j] * act;
-        s[0][j] += p[j];
-        s[NS - 1][j] += u[j];
-      }
-      char* o = a.dpre + (size_t)r * a.row;
-      put(o, c, p);
-      put(o, F + c, u);
-      if (!whole || c + E == F)  // the row's last chunk
-        for (int k = 2 * F; k < a.row / ES; ++k) T::store1(o, k, 0.f);
+      if (a.out && c + E >= F)  // the row's last chunk
+        for (int k = NS * F; k < a.row / ES; ++k) T::store1(o, k, 0.f);
     }
   if (!a.part) return;
 #pragma unroll
@@ -113,54 +139,79 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs a) {
     for (int j = 0; j < E; ++j) sums[rl][lane * E + j] = s[h][j];
     __syncthreads();
     for (int i = threadIdx.x; i < CL * E; i += 256) {
-      const int col = blockIdx.x * CL * E + i;
+      const int col = block * CL * E + i;
       float v = sums[0][i];
 #pragma unroll
       for (int q = 1; q < RL; ++q) v += sums[q][i];
-      if (col < F) a.part[(size_t)blockIdx.y * NS * F + h * F + col] = v;
+      if (col < F) a.part[(size_t)group * NS * F + h * F + col] = v;
     }
   }
 }
 
-// out[i] = sum over p of part[p, i], i < n, in the order of the parts
+// What comes after the products, in one launch: the parts of dx and of dW added in order, and
+// the groups' sums of db.
+struct FinishArgs {
+  const float* part[2];
+  void* out[2];
+  long long n[2];
+  int parts[2], count[2];  // workgroups; 0: not parted
+  const float* sums;       // [groups, cols], or null
+  float* db;
+  int groups, cols;
+};
+
 template <int DT>
-__global__ __launch_bounds__(256) void product_join_kernel(const float* part, int parts, long long n, void* out) {
-  for (long long i = (blockIdx.x * 256LL + threadIdx.x) * 4; i < n; i += 1024LL * gridDim.x) {
-    const int m = (int)min(4LL, n - i);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (m == 4) {
-      for (int p = 0; p < parts; ++p) {
-        float f[4];
-        Chunk<0>::unpack(Chunk<0>::raw_at(reinterpret_cast<const char*>(part + p * n + i), 0), f);
+__global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
+  int id = blockIdx.x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] += f[j];
+  for (int k = 0; k < 2; ++k) {
+    if (id < a.count[k]) {
+      const float* part = a.part[k];
+      const long long n = a.n[k];
+      for (long long i = (id * 256LL + threadIdx.x) * 4; i < n; i += 1024LL * a.count[k]) {
+        const int m = (int)min(4LL, n - i);
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (m == 4) {
+          // (eight loads under way at a time)
+          for (int p0 = 0; p0 < a.parts[k]; p0 += 8) {
+            uint4 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              v[u] = Chunk<0>::raw_at(reinterpret_cast<const char*>(part + min(p0 + u, a.parts[k] - 1) * n + i), 0);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              float f[4];
+              Chunk<0>::unpack(v[u], f);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) s[j] += p0 + u < a.parts[k] ? f[j] : 0.f;
+            }
+          }
+          if (DT) store8_any(static_cast<uint16_t*>(a.out[k]) + i,
+                             make_uint2(f32x2_to_bf16x2_bits(s[0], s[1]), f32x2_to_bf16x2_bits(s[2], s[3])));
+          else Chunk<0>::store(a.out[k], i, s);
+        } else {
+          for (int j = 0; j < m; ++j) {
+            float v = 0.f;
+            for (int p = 0; p < a.parts[k]; ++p) v += part[p * n + i + j];
+            Chunk<DT>::store1(a.out[k], i + j, v);
+          }
+        }
       }
-      if (DT) store8_any(static_cast<uint16_t*>(out) + i,
-                         make_uint2(f32x2_to_bf16x2_bits(s[0], s[1]), f32x2_to_bf16x2_bits(s[2], s[3])));
-      else Chunk<0>::store(out, i, s);
-    } else {
-      for (int j = 0; j < m; ++j) {
-        for (int p = 0; p < parts; ++p) s[0] += part[p * n + i + j];
-        Chunk<DT>::store1(out, i + j, s[0]);
-        s[0] = 0.f;
-      }
+      return;
     }
+    id -= a.count[k];
   }
-}
-
-// out[c] = sum over the G rows of part [G, cols]: 32 columns a workgroup, 32 rows at a time,
-// in the same order always (a thread a column took 62 us for 256 x 1536).
-__global__ __launch_bounds__(1024) void sum_groups_kernel(const float* part, int G, int cols, float* out) {
-  constexpr int COLS = 32, ROWS = 1024 / COLS;
+  // 32 columns a workgroup, eight groups at a time and eight of those under way
+  constexpr int COLS = 32, ROWS = 256 / COLS;
   __shared__ float sums[ROWS][COLS + 1];
-  const int t = threadIdx.x % COLS, w = threadIdx.x / COLS, c = blockIdx.x * COLS + t;
+  const int t = threadIdx.x % COLS, w = threadIdx.x / COLS, c = id * COLS + t;
   float s = 0.f;
-  for (int g0 = w; g0 < G; g0 += 8 * ROWS) {
+  for (int g0 = w; g0 < a.groups; g0 += 8 * ROWS) {
     float v[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = part[(size_t)min(g0 + u * ROWS, G - 1) * cols + min(c, cols - 1)];
+    for (int u = 0; u < 8; ++u) v[u] = a.sums[(size_t)min(g0 + u * ROWS, a.groups - 1) * a.cols + min(c, a.cols - 1)];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) s += g0 + u * ROWS < G ? v[u] : 0.f;
+    for (int u = 0; u < 8; ++u) s += g0 + u * ROWS < a.groups ? v[u] : 0.f;
   }
   sums[w][t] = s;
 #pragma unroll
@@ -168,30 +219,32 @@ __global__ __launch_bounds__(1024) void sum_groups_kernel(const float* part, int
     __syncthreads();
     if (w < h) sums[w][t] += sums[w + h][t];
   }
-  if (w == 0 && c < cols) out[c] = sums[0][t];
+  if (w == 0 && c < a.cols) a.db[c] = sums[0][t];
 }
 
-size_t part_bytes(const ProductCut& c, long long M, long long N) { return c.parts > 1 ? (size_t)c.parts * M * N * 4 : 0; }
+size_t part_bytes(int parts, const ProductSize& s) { return parts > 1 ? whole256((size_t)parts * s.M * s.N * 4) : 0; }
 
-template <int DT, bool KA, bool KB, int EPI>
-hipError_t launch_cut(const ProductArgs& a, int tile, hipStream_t stream) {
+template <int DT, int TILE>
+hipError_t launch_pair(ProductPair p, hipStream_t stream) {
+  using G = typename PairCfg<DT, TILE>::X;
+  auto count = [](const ProductArgs& a) {
+    return a.out ? ((long long)(a.M + TILE - 1) / TILE) * ((a.N + TILE - 1) / TILE) * a.parts : 0;
+  };
+  const long long x = count(p.dx), w = count(p.dW);
+  if (x + w + 8 > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
+  p.dx_count = (int)x;
+  p.dW_count = (int)w;
+  p.dW_first = (long long)p.dW.K / std::max(1, p.dW.parts) > (long long)p.dx.K / std::max(1, p.dx.parts);
+  const long long all = (((p.dW_first ? w : x) + 7) & ~7LL) + (p.dW_first ? x : w);
+  return launch_with_smem((const void*)&product_pair_kernel<PairCfg<DT, TILE>>, dim3((unsigned)all), dim3(G::kThreads), G::kSmem, stream,
+                          nullptr, nullptr, p);
+}
+
+template <int DT>
+hipError_t launch_tile(const ProductPair& p, int tile, hipStream_t stream) {
   if constexpr (DT == 1)
-    if (tile == 256) return launch_product<ProductCfg<1, KA, KB, 256, 256, 2, 4>, EPI>(a, stream);
-  if (tile == 128) return launch_product<ProductCfg<DT, KA, KB, 128, 128, 2, 2>, EPI>(a, stream);
-  return launch_product<ProductCfg<DT, KA, KB, 64, 64, 2, 2>, EPI>(a, stream);
-}
-
-template <int DT, bool KA, bool KB>
-hipError_t product(ProductArgs a, float* part, hipStream_t stream) {
-  const ProductCut c = product_cut(a.M, a.N, a.K, DT, true);
-  if (c.parts == 1) return launch_cut<DT, KA, KB, kProductStore>(a, c.tile, stream);
-  a.parts = c.parts;
-  a.part = part;
-  hipError_t e = launch_cut<DT, KA, KB, kProductPart>(a, c.tile, stream);
-  if (e != hipSuccess) return e;
-  const long long n = (long long)a.M * a.N;
-  product_join_kernel<DT><<<(unsigned)std::min<long long>((n + 1023) / 1024, 4096), 256, 0, stream>>>(part, c.parts, n, a.out);
-  return hipGetLastError();
+    if (tile == 256) return launch_pair<DT, 256>(p, stream);
+  return tile == 128 ? launch_pair<DT, 128>(p, stream) : launch_pair<DT, 64>(p, stream);
 }
 
 // Groups of rows of the sums over rows.
@@ -203,13 +256,14 @@ int sum_groups(int R, int F, int dt_bf16) {
 
 // The workspace of a backward pass, its pieces 256 bytes apart.
 struct GradPlan {
-  size_t x = 0, dy = 0, W = 0, sums = 0, part = 0, bytes = 0;  // offsets; W, x, dy: packed rows
+  size_t x = 0, dy = 0, W = 0, sums = 0, part_x = 0, part_W = 0, bytes = 0;  // offsets; W, x, dy: packed rows
   bool pack_x, pack_dy;
   int groups;
+  ProductCuts cuts;
 };
 
-GradPlan plan(int R, int K, int N, int dt_bf16, bool gated) {
-  GradPlan p;
+GradPlan make_plan(int R, int K, int N, int dt_bf16, bool gated) {
+  GradPlan p{};
   const int e = dt_bf16 ? 8 : 4;
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -226,81 +280,113 @@ GradPlan plan(int R, int K, int N, int dt_bf16, bool gated) {
   if (p.pack_dy) p.dy = take(R * packed_row(N, dt_bf16));
   p.groups = sum_groups(R, gated ? N / 2 : N, dt_bf16);
   p.sums = take(p.groups > 1 ? (size_t)p.groups * N * 4 : 0);
-  p.part = take(std::max(part_bytes(product_cut(R, K, N, dt_bf16, true), R, K),
-                         part_bytes(product_cut(N, K, R, dt_bf16, true), N, K)));
+  const ProductSize x{R, K, N}, W{N, K, R};
+  p.cuts = product_cuts(x, W, dt_bf16);
+  p.part_x = take(part_bytes(p.cuts.x.parts, x));
+  p.part_W = take(part_bytes(p.cuts.W.parts, W));
   p.bytes = at;
   return p;
+}
+
+// A call asks three times: for the workspace's size, its check and the launch.
+const GradPlan& plan(int R, int K, int N, int dt_bf16, bool gated) {
+  thread_local int key[5] = {};
+  thread_local GradPlan last;
+  const int now[5] = {R, K, N, dt_bf16, gated};
+  if (!std::equal(key, key + 5, now)) {
+    last = make_plan(R, K, N, dt_bf16, gated);
+    std::copy(now, now + 5, key);
+  }
+  return last;
 }
 
 template <int DT>
 hipError_t launch_grad(const LinearGradArgs& g, hipStream_t stream) {
   constexpr int es = DT ? 2 : 4, E = 16 / es;
-  const bool gated = g.pre != nullptr;
+  const bool gated = g.pre != nullptr, products = g.dx || g.dW;
   const GradPlan p = plan(g.R, g.K, g.N, DT, gated);
   char* ws = static_cast<char*>(g.ws);
-  const void *x = g.x, *W = g.W, *dy = g.dy;
   const int F = gated ? g.N / 2 : g.N;
   hipError_t e = hipSuccess;
-  if (p.pack_x) {
-    if (g.dW) e = launch_pack_rows(g.x, g.R, g.K, ws + p.x, DT, stream);
-    if (e == hipSuccess && g.dx) e = launch_pack_rows(g.W, g.N, g.K, ws + p.W, DT, stream);
-    x = ws + p.x;
-    W = ws + p.W;
-  }
-  if (e != hipSuccess) return e;
-  GateGradArgs s{};
-  s.dh = g.dy;
+
+  PrepareArgs s{};
+  s.dy = g.dy;
   s.pre = g.pre;
   s.R = g.R;
   s.F = F;
   s.act = g.act;
   s.row = (int)packed_row(g.N, DT);
-  s.dpre = ws + p.dy;
+  s.out = products && p.pack_dy ? ws + p.dy : nullptr;
   s.part = !g.db ? nullptr : p.groups > 1 ? reinterpret_cast<float*>(ws + p.sums) : g.db;
-  const dim3 grid((F + 32 * E - 1) / (32 * E), p.groups);
-  if (gated) gate_grad_kernel<DT, true><<<grid, 256, 0, stream>>>(s);
-  else if (g.db) gate_grad_kernel<DT, false><<<grid, 256, 0, stream>>>(s);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (g.db && p.groups > 1) {
-    sum_groups_kernel<<<(g.N + 31) / 32, 1024, 0, stream>>>(reinterpret_cast<float*>(ws + p.sums), p.groups, g.N, g.db);
+  s.across = (F + 32 * E - 1) / (32 * E);
+  s.groups = s.out || s.part ? p.groups : 0;
+  if (p.pack_x && g.dW) s.pack.t[0] = {g.x, ws + p.x, g.R, g.K};
+  if (p.pack_x && g.dx) s.pack.t[1] = {g.W, ws + p.W, g.N, g.K};
+  s.pack_first = pack_count(s.pack.t[0], DT);
+  const int before = s.across * s.groups + s.pack_first + pack_count(s.pack.t[1], DT);
+  if (before) {
+    if (gated) prepare_kernel<DT, true><<<before, 256, 0, stream>>>(s);
+    else prepare_kernel<DT, false><<<before, 256, 0, stream>>>(s);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (!gated && p.pack_dy && (g.dx || g.dW)) e = launch_pack_rows(g.dy, g.R, g.N, ws + p.dy, DT, stream);
-  if (p.pack_dy) dy = ws + p.dy;
-  if (e != hipSuccess) return e;
+
+  ProductPair q{};
   ProductArgs a{};
   const long long krow = (long long)packed_row(g.K, DT), nrow = (long long)packed_row(g.N, DT);
-  float* part = reinterpret_cast<float*>(ws + p.part);
-  a.A = dy;
+  a.A = p.pack_dy ? ws + p.dy : g.dy;
   a.lda = nrow;
   a.ldb = krow;
   a.N = g.K;
   a.cols_a = (int)(nrow / 16);
   a.cols_b = (int)(krow / 16);
-  if (g.dx) {
-    a.B = W;
-    a.M = g.R;
-    a.K = g.N;
-    a.out = g.dx;
-    if ((e = product<DT, false, true>(a, part, stream)) != hipSuccess) return e;
+  q.dx = q.dW = a;
+  q.dx.B = p.pack_x ? ws + p.W : g.W;
+  q.dx.M = g.R;
+  q.dx.K = g.N;
+  q.dx.out = g.dx;
+  q.dx.parts = p.cuts.x.parts;
+  q.dx.part = reinterpret_cast<float*>(ws + p.part_x);
+  q.dW.B = p.pack_x ? ws + p.x : g.x;
+  q.dW.M = g.N;
+  q.dW.K = g.R;
+  q.dW.out = g.dW;
+  q.dW.parts = p.cuts.W.parts;
+  q.dW.part = reinterpret_cast<float*>(ws + p.part_W);
+  if (products && p.cuts.together) {
+    e = launch_tile<DT>(q, p.cuts.x.tile, stream);
+  } else {
+    ProductPair x = q, W = q;
+    x.dW.out = W.dx.out = nullptr;
+    if (g.dx) e = launch_tile<DT>(x, p.cuts.x.tile, stream);
+    if (g.dW && e == hipSuccess) e = launch_tile<DT>(W, p.cuts.W.tile, stream);
   }
-  if (g.dW) {
-    a.B = x;
-    a.M = g.N;
-    a.K = g.R;
-    a.out = g.dW;
-    e = product<DT, true, true>(a, part, stream);
+  if (e != hipSuccess) return e;
+
+  FinishArgs f{};
+  const ProductArgs* both[2] = {&q.dx, &q.dW};
+  for (int k = 0; k < 2; ++k) {
+    f.part[k] = both[k]->part;
+    f.out[k] = both[k]->out;
+    f.n[k] = (long long)both[k]->M * both[k]->N;
+    f.parts[k] = both[k]->parts;
+    f.count[k] = both[k]->out && both[k]->parts > 1 ? (int)std::min<long long>((f.n[k] + 1023) / 1024, 4096) : 0;
   }
-  return e;
+  const bool sums = g.db && p.groups > 1;
+  f.sums = reinterpret_cast<const float*>(ws + p.sums);
+  f.db = g.db;
+  f.groups = p.groups;
+  f.cols = g.N;
+  const int after = f.count[0] + f.count[1] + (sums ? (g.N + 31) / 32 : 0);
+  if (after) finish_kernel<DT><<<after, 256, 0, stream>>>(f);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_pack_rows(const void* src, int R, int C, void* dst, int dt_bf16, hipStream_t stream) {
-  const int row = (int)packed_row(C, dt_bf16);
-  const dim3 grid((row / 16 + 63) / 64, std::min((R + 3) / 4, 4096));
-  if (dt_bf16) pack_rows_kernel<1><<<grid, 256, 0, stream>>>(src, R, C, static_cast<char*>(dst), row);
-  else pack_rows_kernel<0><<<grid, 256, 0, stream>>>(src, R, C, static_cast<char*>(dst), row);
+hipError_t launch_pack_rows(const PackPair& p, int dt_bf16, hipStream_t stream) {
+  const int first = pack_count(p.t[0], dt_bf16), all = first + pack_count(p.t[1], dt_bf16);
+  if (dt_bf16) pack_rows_kernel<1><<<all, 256, 0, stream>>>(p, first);
+  else pack_rows_kernel<0><<<all, 256, 0, stream>>>(p, first);
   return hipGetLastError();
 }
 

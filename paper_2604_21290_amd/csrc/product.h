@@ -32,7 +32,7 @@
 
 namespace gl {
 
-enum { kProductStore = 0, kProductPart = 1, kProductGated = 2 };
+enum { kProductStore = 0, kProductPart = 1, kProductGated = 2 };  // what becomes of the sums
 
 struct ProductArgs {
   const void *A, *B;
@@ -184,14 +184,104 @@ __device__ __forceinline__ f32x4 product_mma(const uint4& b, const uint4& a, f32
   return mfma_f32(__uint_as_float(b.w), __uint_as_float(a.w), acc);
 }
 
+// Lane (g, t) of MFMA tile (i, j) holds columns 4g .. 4g+3 of row t.  ER rows at a time the
+// wave writes its tile to its own part of LDS in fp32 (16-byte places permuted by the row) and
+// reads it back in rows, 16 bytes of output a lane.
 template <class G, int EPI>
-__device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
+__device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* smem, const f32x4 (&acc)[G::TM][G::TN], int m0,
+                                                 int n0, int part) {
+  constexpr int DT = G::DT, TN = G::TN;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, t = lane & 15, wm = w / G::WC, wn = w % G::WC;
+  using T = Chunk<DT>;
+  constexpr int E = EPI == kProductPart ? 4 : T::E;
+  constexpr int COLS = EPI == kProductGated ? G::WCOLS / 2 : G::WCOLS;
+  constexpr int LPR = COLS / E, RPP = 64 / LPR, ER = G::ER, CSW = G::WCOLS / 4 < 16 ? G::WCOLS / 4 - 1 : 15;
+  static_assert(ER % RPP == 0, "whole passes");
+  const int cq = lane % LPR, rq = lane / LPR;
+  const int n = n0 + wn * COLS + cq * E;
+  float bias[2][EPI == kProductGated ? E : 1] = {};
+  if (EPI == kProductGated && a.bias) {
+#pragma unroll
+    for (int v = 0; v < E; ++v) {
+      bias[0][v] = T::load1(a.bias, min(n + v, a.N - 1));
+      bias[1][v] = T::load1(a.bias, a.N + min(n + v, a.N - 1));
+    }
+  }
+  char* st = smem + w * G::kShare;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < G::WROWS / ER; ++e) {
+    if (e) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront"), __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < ER / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        *reinterpret_cast<f32x4*>(st + (i * 16 + t) * (G::WCOLS * 4) + (((j * 4 + g) ^ (t & CSW)) * 16)) =
+            acc[e * (ER / 16) + i][j];
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < ER / RPP; ++p) {
+      const int r = p * RPP + rq, row = m0 + wm * G::WROWS + e * ER + r;
+      const char* sr = st + r * (G::WCOLS * 4);
+      auto from = [&](int col, float* y) {  // E sums from column `col` of the wave's tile
+#pragma unroll
+        for (int v = 0; v < E; v += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(sr + (((col + v) / 4) ^ (r & CSW)) * 16);
+          y[v] = x[0], y[v + 1] = x[1], y[v + 2] = x[2], y[v + 3] = x[3];
+        }
+      };
+      auto put = [&](void* out, size_t at, const float* y) {
+        if (n + E <= a.N) {
+          T::store(out, at, y);
+        } else {
+#pragma unroll
+          for (int v = 0; v < E; ++v)
+            if (n + v < a.N) T::store1(out, at + v, y[v]);
+        }
+      };
+      if (row >= a.M || n >= a.N) continue;
+      float y[E];
+      from(cq * E, y);
+      if (EPI == kProductStore) {
+        put(a.out, (size_t)row * a.N + n, y);
+      } else if (EPI == kProductPart) {
+        float* o = a.part + ((size_t)part * a.M + row) * a.N + n;
+        if (n + E <= a.N) {
+          Chunk<0>::store(o, 0, y);
+        } else {
+#pragma unroll
+          for (int v = 0; v < E; ++v)
+            if (n + v < a.N) o[v] = y[v];
+        }
+      } else {
+        float u[E];
+        from(COLS + cq * E, u);
+#pragma unroll
+        for (int v = 0; v < E; ++v) y[v] += bias[0][v], u[v] += bias[1][v];
+        if (a.pre) {
+          put(a.pre, (size_t)row * 2 * a.N + n, y);
+          put(a.pre, (size_t)row * 2 * a.N + a.N + n, u);
+        }
+#pragma unroll
+        for (int v = 0; v < E; ++v) y[v] = gate_act<DT>(a.act, y[v]) * u[v];
+        put(a.out, (size_t)row * a.N + n, y);
+      }
+    }
+  }
+}
+
+// Workgroup `id` of `count` of a product.  EPI: kProductGated or kProductStore, which writes
+// parts where there are several.
+template <class G, int EPI>
+__device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, int id, int count) {
   constexpr int DT = G::DT, ES = G::ES, TM = G::TM, TN = G::TN, BM = G::BM, BN = G::BN;
   constexpr int OUT = EPI == kProductGated ? BN / 2 : BN;  // output columns of a tile
   const int ntm = (a.M + BM - 1) / BM, ntn = (a.N + OUT - 1) / OUT;
   // tiles by bands of eight rows of them, so that what an XCD's workgroups share is in its L2
-  int blk = xcd_remap(blockIdx.x, gridDim.x), part = 0;
-  if (EPI == kProductPart) {
+  int blk = xcd_remap(id, count), part = 0;
+  if (EPI != kProductGated && a.parts > 1) {
     part = blk / (ntm * ntn);
     blk -= part * ntm * ntn;
   }
@@ -206,7 +296,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
   // halves h0 .. h1 of the contraction, whole stages (the last half may be all zeros)
   const long long stages = (a.K + 2 * G::HALF - 1) / (2 * G::HALF);
   int h0 = 0, h1 = 2 * (int)stages;
-  if (EPI == kProductPart) {
+  if (EPI != kProductGated && a.parts > 1) {
     h0 = 2 * (int)(stages * part / a.parts);
     h1 = 2 * (int)(stages * (part + 1) / a.parts);
   }
@@ -318,142 +408,141 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem) {
     }
   }
 
-  // -- epilogue: lane (g, t) of MFMA tile (i, j) holds columns 4g .. 4g+3 of row t.  ER
-  //    rows at a time the wave writes its tile to its own part of LDS in fp32 (16-byte
-  //    places permuted by the row) and reads it back in rows, 16 bytes of output a lane
-  using T = Chunk<DT>;
-  constexpr int E = EPI == kProductPart ? 4 : T::E;
-  constexpr int COLS = EPI == kProductGated ? G::WCOLS / 2 : G::WCOLS;
-  constexpr int LPR = COLS / E, RPP = 64 / LPR, ER = G::ER, CSW = G::WCOLS / 4 < 16 ? G::WCOLS / 4 - 1 : 15;
-  static_assert(ER % RPP == 0, "whole passes");
-  const int cq = lane % LPR, rq = lane / LPR;
-  const int n = n0 + wn * COLS + cq * E;
-  float bias[2][EPI == kProductGated ? E : 1] = {};
-  if (EPI == kProductGated && a.bias) {
-#pragma unroll
-    for (int v = 0; v < E; ++v) {
-      bias[0][v] = T::load1(a.bias, min(n + v, a.N - 1));
-      bias[1][v] = T::load1(a.bias, a.N + min(n + v, a.N - 1));
-    }
-  }
-  char* st = smem + w * G::kShare;
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < G::WROWS / ER; ++e) {
-    if (e) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront"), __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < ER / 16; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-        *reinterpret_cast<f32x4*>(st + (i * 16 + t) * (G::WCOLS * 4) + (((j * 4 + g) ^ (t & CSW)) * 16)) =
-            acc[e * (ER / 16) + i][j];
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int p = 0; p < ER / RPP; ++p) {
-      const int r = p * RPP + rq, row = m0 + wm * G::WROWS + e * ER + r;
-      const char* sr = st + r * (G::WCOLS * 4);
-      auto from = [&](int col, float* y) {  // E sums from column `col` of the wave's tile
-#pragma unroll
-        for (int v = 0; v < E; v += 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(sr + (((col + v) / 4) ^ (r & CSW)) * 16);
-          y[v] = x[0], y[v + 1] = x[1], y[v + 2] = x[2], y[v + 3] = x[3];
-        }
-      };
-      auto put = [&](void* out, size_t at, const float* y) {
-        if (n + E <= a.N) {
-          T::store(out, at, y);
-        } else {
-#pragma unroll
-          for (int v = 0; v < E; ++v)
-            if (n + v < a.N) T::store1(out, at + v, y[v]);
-        }
-      };
-      if (row >= a.M || n >= a.N) continue;
-      float y[E];
-      from(cq * E, y);
-      if (EPI == kProductStore) {
-        put(a.out, (size_t)row * a.N + n, y);
-      } else if (EPI == kProductPart) {
-        float* o = a.part + ((size_t)part * a.M + row) * a.N + n;
-        if (n + E <= a.N) {
-          Chunk<0>::store(o, 0, y);
-        } else {
-#pragma unroll
-          for (int v = 0; v < E; ++v)
-            if (n + v < a.N) o[v] = y[v];
-        }
-      } else {
-        float u[E];
-        from(COLS + cq * E, u);
-#pragma unroll
-        for (int v = 0; v < E; ++v) y[v] += bias[0][v], u[v] += bias[1][v];
-        if (a.pre) {
-          put(a.pre, (size_t)row * 2 * a.N + n, y);
-          put(a.pre, (size_t)row * 2 * a.N + a.N + n, u);
-        }
-#pragma unroll
-        for (int v = 0; v < E; ++v) y[v] = gate_act<DT>(a.act, y[v]) * u[v];
-        put(a.out, (size_t)row * a.N + n, y);
-      }
-    }
-  }
+  if (EPI == kProductGated) product_epilogue<G, kProductGated>(a, smem, acc, m0, n0, 0);
+  else if (a.parts > 1) product_epilogue<G, kProductPart>(a, smem, acc, m0, n0, part);
+  else product_epilogue<G, kProductStore>(a, smem, acc, m0, n0, 0);
 }
 
-template <class G, int EPI>
-__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
-  extern __shared__ __align__(16) char smem[];
-  product_tile<G, EPI>(a, smem);
-}
-
-template <class G, int EPI>
-hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
-  constexpr int OUT = EPI == kProductGated ? G::BN / 2 : G::BN;
-  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + OUT - 1) / OUT) * (EPI == kProductPart ? a.parts : 1);
-  if (tiles > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
-  return launch_with_smem((const void*)&product_kernel<G, EPI>, dim3((unsigned)tiles),
-                          dim3(G::kThreads), G::kSmem, stream, nullptr, nullptr, a);
-}
-
-// How a product is cut: the tile (256, 128 or 64 outputs each way) and the parts of its
-// contraction, by an estimate of its time in us.  Workgroups of 128 and 64 lie two and four
-// to a CU: a stage takes them a + b n, n of them, and a round of workgroups 1 to 4.5 us more
-// (its first stage's trip, its stores); parts cost a launch and their sums' way through
-// memory.  Measured, us (tile, parts; * taken), bf16:
-//                                  256        128        128, parts  64
-//   dx 16384 x 2048 x 8192         481 *      491                    1136
-//   dW 16384 x 2048 x 8192         462 *      565        612, 2      1541
-//   dx 12544 x 640 x 5120          122        77.2 *     98.1, 2     126
-//   dW 12544 x 640 x 5120          143, 4     145        98.5, 5 *   164, 2
-//   dx 12544 x 2560 x 640          46.4 *     50.8                   68.3
-//   dW 12544 x 2560 x 640          82.5, 8    68.1, 3    52.4, 5 *   79.5, 5
-//   dx 2000 x 4096 x 1024          33.2       22.0 *     42.6, 2     31.3
-struct ProductCut {
-  int tile, parts;
+// Two products in one launch, of which either may be missing: x's gradient, whose first
+// operand lies along the contraction, and the weight's, whose both lie across it.  They need
+// nothing of each other, and fill the chip together where neither does alone.
+struct ProductPair {
+  ProductArgs dx, dW;
+  int dx_count, dW_count;  // workgroups
+  int dW_first;            // the one with the longer workgroups goes first
 };
 
-inline ProductCut product_cut(long long M, long long N, long long K, int dt_bf16, bool parts) {
-  struct Tile {
-    int size, per_cu;
-    double a, b, round;
-  };
-  constexpr Tile kBf16[] = {{256, 1, 0.0, 1.85, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}};
-  constexpr Tile kF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.15, 0.5, 1.5}};
-  const long long stages = (K + (dt_bf16 ? 63 : 31)) / (dt_bf16 ? 64 : 32);
-  ProductCut best{64, 1};
-  double least = 1e300;
+template <int DT, int TILE>
+struct PairCfg {
+  static constexpr int WR = 2, WC = TILE == 256 ? 4 : 2;
+  using X = ProductCfg<DT, false, true, TILE, TILE, WR, WC>;
+  using W = ProductCfg<DT, true, true, TILE, TILE, WR, WC>;
+  static constexpr int kThreads = X::kThreads;
+  static_assert(X::kSmem == W::kSmem && kThreads == W::kThreads, "one launch");
+};
+
+template <class P>
+__global__ __launch_bounds__(P::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductPair p) {
+  extern __shared__ __align__(16) char smem[];
+  // (the second one's workgroups begin with a whole round of the XCDs)
+  const int before = ((p.dW_first ? p.dW_count : p.dx_count) + 7) & ~7, id = blockIdx.x;
+  const bool second = id >= before;
+  if (second == (p.dW_first != 0)) {
+    const int i = second ? id - before : id;
+    if (i < p.dx_count) product_tile<typename P::X, kProductStore>(p.dx, smem, i, p.dx_count);
+  } else {
+    const int i = second ? id - before : id;
+    if (i < p.dW_count) product_tile<typename P::W, kProductStore>(p.dW, smem, i, p.dW_count);
+  }
+}
+
+template <class G>
+__global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void product_gated_kernel(ProductArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  product_tile<G, kProductGated>(a, smem, blockIdx.x, gridDim.x);
+}
+
+// How products are cut: the tile (256, 128 or 64 outputs each way) and the parts of their
+// contractions, by an estimate of the time in us.  Workgroups of 128 and 64 lie two and four
+// to a CU: a stage takes them a + b n, n of them, and a round of workgroups 1 to 4.5 us more
+// (its first stage's trip, its stores); parts cost a launch and their sums' way through
+// memory.  Measured, us (tile, parts), bf16:
+//                                  256        128        128, parts  64
+//   dx 16384 x 2048 x 8192         428        502                    1200
+//   dW 16384 x 2048 x 8192         426        565        608, 2      1572
+//   dx 12544 x 640 x 5120          118        78.5       102, 2      127
+//   dW 12544 x 640 x 5120          99.3, 4    133        97.4, 2     164, 2
+//   dx 12544 x 2560 x 640          45.8       50.9                   68.8
+//   dW 12544 x 2560 x 640          77.6, 5    68.1, 3    52.3, 5     80.5, 5
+//   dx 2000 x 4096 x 1024          33.2       22.0       42.6, 2     31.3
+struct ProductTile {
+  int size, per_cu;
+  double a, b, round;
+};
+constexpr ProductTile kTilesBf16[] = {{256, 1, 0.0, 1.66, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}};
+constexpr ProductTile kTilesF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.4, 0.45, 1.5}};
+
+struct ProductSize {
+  long long M, N, K;
+  long long tiles(int size) const { return ((M + size - 1) / size) * ((N + size - 1) / size); }
+  long long stages(int dt_bf16) const { return (K + (dt_bf16 ? 63 : 31)) / (dt_bf16 ? 64 : 32); }
+};
+
+struct ProductCut {
+  int tile, parts;
+  double us;
+};
+
+// One product alone.
+inline ProductCut product_cut(const ProductSize& s, int dt_bf16, bool may_part) {
+  ProductCut best{64, 1, 1e300};
+  const long long stages = s.stages(dt_bf16);
+  // (at least four stages a part; the parts' sums stay within 256 MiB)
+  const long long most = !may_part ? 1 : std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
   for (int i = 0; i < (dt_bf16 ? 3 : 2); ++i) {
-    const Tile& t = dt_bf16 ? kBf16[i] : kF32[i];
-    const long long tiles = ((M + t.size - 1) / t.size) * ((N + t.size - 1) / t.size);
-    // (at least four stages a part; the parts' sums stay within 256 MiB)
-    const long long most = !parts ? 1 : std::max<long long>(1, std::min<long long>({64, stages / 4, (64LL << 20) / (M * N)}));
-    for (long long p = 1; p <= most; ++p) {
-      const long long all = tiles * p, slots = 256LL * t.per_cu, rest = all % slots;
+    const ProductTile& t = dt_bf16 ? kTilesBf16[i] : kTilesF32[i];
+    const long long tiles = s.tiles(t.size), slots = 256LL * t.per_cu;
+    for (const int p : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (p > most || (p > 1 && tiles * p > 3 * slots)) break;
+      const long long all = tiles * p, rest = all % slots;
       const double n = (double)((stages + p - 1) / p);
       double us = (double)(all / slots) * (n * (t.a + t.b * t.per_cu) + t.round);
       if (rest) us += n * (t.a + t.b * (double)((rest + 255) / 256)) + t.round;
-      if (p > 1) us += 5.0 + (double)(8 * p + 4) * (double)(M * N) / 5.5e6;
-      if (us < least) least = us, best = ProductCut{t.size, (int)p};
+      if (p > 1) us += 5.0 + (double)(8 * p + 4) * (double)(s.M * s.N) / 5.5e6;
+      if (us < best.us) best = ProductCut{t.size, p, us};
+    }
+  }
+  return best;
+}
+
+// Two, in one launch with a tile and parts that suit both, or one after the other.  In one
+// launch against one after the other, us, bf16: 6272 x 192 x 1536 28 (38), 3008 x 1008 x 336
+// 23 (28), 784 x 640 x 5120 29 (41), 12544 x 2560 x 640 103 (110).
+struct ProductCuts {
+  ProductCut x, W;
+  bool together;
+};
+
+inline ProductCuts product_cuts(const ProductSize& x, const ProductSize& w, int dt_bf16) {
+  ProductCuts best{product_cut(x, dt_bf16, true), product_cut(w, dt_bf16, true), false};
+  double least = best.x.us + best.W.us + 8.0;
+  const long long sx = x.stages(dt_bf16), sw = w.stages(dt_bf16);
+  auto most = [](const ProductSize& s, long long stages) {
+    return std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
+  };
+  auto join = [](const ProductSize& s, int p) { return p > 1 ? (double)(8 * p + 4) * (double)(s.M * s.N) / 5.5e6 : 0.0; };
+  const long long mx = most(x, sx), mw = most(w, sw);
+  for (int i = 0; i < (dt_bf16 ? 3 : 2); ++i) {
+    const ProductTile& t = dt_bf16 ? kTilesBf16[i] : kTilesF32[i];
+    const long long slots = 256LL * t.per_cu, tx = x.tiles(t.size), tw = w.tiles(t.size);
+    const double full = t.a + t.b * t.per_cu;
+    for (const int px : {1, 2, 4, 8, 16}) {
+      if (px > mx || (px > 1 && tx * px > slots)) break;
+      const double nx = (double)((sx + px - 1) / px), x1 = nx * full + t.round, cx = (double)(tx * px);
+      for (const int pw : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48}) {
+        if (pw > mw || (pw > 1 && tw * pw > 2 * slots)) break;
+        const double nw = (double)((sw + pw - 1) / pw), cw = (double)(tw * pw), all = cx + cw;
+        double us;
+        if (all <= (double)slots) {
+          us = std::max(nx, nw) * (t.a + t.b * std::max(1.0, all / 256)) + t.round;
+        } else {
+          // the workgroups' time shared out, and half of one at the end; one takes its time at least
+          const double w1 = nw * full + t.round;
+          us = std::max((cx * x1 + cw * w1) / (double)slots + std::min(x1, w1) / 2, std::max(x1, w1));
+        }
+        us += join(x, px) + join(w, pw) + (px > 1 || pw > 1 ? 5.0 : 0.0);
+        if (us < least) least = us, best = ProductCuts{{t.size, px, us}, {t.size, pw, us}, true};
+      }
     }
   }
   return best;

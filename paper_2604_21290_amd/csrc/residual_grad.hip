@@ -432,7 +432,6 @@ Plan plan(int R, int C, bool near) {
   return make(0, vpl, 64 * waves, 256 * std::max(1, (vpl == 1 ? 12 : 8) / waves));
 }
 
-size_t whole256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 template <int DT, bool POST>
 hipError_t launch_rows(ResidualGradArgs a, void* ws, hipStream_t stream) {

@@ -369,6 +369,16 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
 #pragma unroll
     for (int i = 0; i < TM; ++i) af[i] = FA::read(smem + qa, abase, aswap, ablk + i, kk, g, t);
   };
+  // a half's reads among the multiplications before it, not ahead of them all
+  auto mix = [&] {
+    constexpr int reads = TM * (HA ? (DT ? 2 : 4) : 1) + TN * (HB ? (DT ? 2 : 4) : 1), mmas = TM * TN * (DT ? 1 : 4);
+    constexpr int each = mmas / reads > 0 ? mmas / reads : 1, n = reads < mmas ? reads : mmas;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, (reads + n - 1) / n, 0);
+    }
+  };
   uint4 a0[TM], b0[TN], a1[TM], b1[TN];
   if (h0 < h1) {
     // the rings' first filling, in the order of the turns that would have made it
@@ -395,6 +405,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
       }
       read(qa, qb, 1, a1, b1);
       multiply(a0, b0);
+      mix();
       pa = qa, pb = qb;
       qa = next(pa, G::kPieceA, RA), qb = next(pb, G::kPieceB, RB);
       if (h + LAST < h1) dma_wait_barrier<after_odd>();
@@ -404,6 +415,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
       // not know how many reads are under way, and wait for these before it multiplies)
       read(qa, qb, 0, a0, b0);
       multiply(a1, b1);
+      mix();
       pa = qa, pb = qb;
     }
   }

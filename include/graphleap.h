@@ -536,8 +536,8 @@ gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const 
  * their elements' alignment.  Sums are fp32, in an order that depends on the
  * sizes alone: a call repeats its bits.  dW is rounded once to dt; the sums
  * over rows (dbias, the norms' and the scale's gradients) are fp32.
- * Limits of the layers: 1 <= R <= 2^28; 1 <= K, Cout, 2 F <= 2^20; R times each
- * of them <= 2^36.  No output may overlap an input, the workspace or another.
+ * Limits of the layers: 1 <= R <= 2^28; 1 <= K, Cout, 2 F <= 2^20; no matrix of
+ * more than 2^36 elements.  No output may overlap an input, the workspace or another.
  * ========================================================================= */
 
 /* ---------------------------------------------------------------------------

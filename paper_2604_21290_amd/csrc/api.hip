@@ -1422,7 +1422,8 @@ namespace {
 
 bool layer_sizes_ok(int R, int K, long long N) {
   constexpr long long most = 1LL << 36;
-  return R >= 1 && K >= 1 && N >= 1 && R <= 1 << 28 && K <= 1 << 20 && N <= 1 << 20 && R * (long long)K <= most && R * N <= most;
+  return R >= 1 && K >= 1 && N >= 1 && R <= 1 << 28 && K <= 1 << 20 && N <= 1 << 20 && R * (long long)K <= most && R * N <= most &&
+         K * N <= most;
 }
 
 // Every tensor of a call as bytes from its start: those that are written, then the rest.

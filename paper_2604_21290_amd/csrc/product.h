@@ -197,7 +197,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
   constexpr int E = EPI == kProductPart ? 4 : T::E;
   constexpr int COLS = EPI == kProductGated ? G::WCOLS / 2 : G::WCOLS;
   constexpr int LPR = COLS / E, RPP = 64 / LPR, ER = G::ER, CSW = G::WCOLS / 4 < 16 ? G::WCOLS / 4 - 1 : 15;
-  static_assert(ER % RPP == 0, "whole passes");
+  static_assert(ER % RPP == 0 || RPP % ER == 0, "whole passes, or one");
   const int cq = lane % LPR, rq = lane / LPR;
   const int n = n0 + wn * COLS + cq * E;
   float bias[2][EPI == kProductGated ? E : 1] = {};
@@ -222,8 +222,8 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int p = 0; p < ER / RPP; ++p) {
-      const int r = p * RPP + rq, row = m0 + wm * G::WROWS + e * ER + r;
+    for (int p = 0; p < (ER + RPP - 1) / RPP; ++p) {
+      const int r = p * RPP + (RPP > ER ? rq % ER : rq), row = m0 + wm * G::WROWS + e * ER + r;
       const char* sr = st + r * (G::WCOLS * 4);
       auto from = [&](int col, float* y) {  // E sums from column `col` of the wave's tile
 #pragma unroll
@@ -241,7 +241,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
             if (n + v < a.N) T::store1(out, at + v, y[v]);
         }
       };
-      if (row >= a.M || n >= a.N) continue;
+      if (row >= a.M || n >= a.N || (RPP > ER && rq >= ER)) continue;
       float y[E];
       from(cq * E, y);
       if (EPI == kProductStore) {
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(G::kThreads) __attribute__((amdgpu_waves_per_eu(2))
   product_tile<G, kProductGated>(a, smem, blockIdx.x, gridDim.x);
 }
 
-// How products are cut: the tile (256, 128 or 64 outputs each way) and the parts of their
+// How products are cut: the tile (256, 128, 64 or 32 outputs each way) and the parts of their
 // contractions, by an estimate of the time in us.  Workgroups of 128 and 64 lie two and four
 // to a CU: a stage takes them a + b n, n of them, and a round of workgroups 1 to 4.5 us more
 // (its first stage's trip, its stores); parts cost a launch and their sums' way through
@@ -481,8 +481,9 @@ struct ProductTile {
   int size, per_cu;
   double a, b, round;
 };
-constexpr ProductTile kTilesBf16[] = {{256, 1, 0.0, 1.66, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}};
-constexpr ProductTile kTilesF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.4, 0.45, 1.5}};
+// (the tile of 32 is the gated layer's alone: 777 x 501 x 333 fp32 fills the chip with it)
+constexpr ProductTile kTilesBf16[] = {{256, 1, 0.0, 1.66, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}, {32, 8, 0.25, 0.06, 1.0}};
+constexpr ProductTile kTilesF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.4, 0.45, 1.5}, {32, 8, 0.25, 0.15, 1.0}};
 
 struct ProductSize {
   long long M, N, K;
@@ -495,15 +496,16 @@ struct ProductCut {
   double us;
 };
 
-// One product alone.
-inline ProductCut product_cut(const ProductSize& s, int dt_bf16, bool may_part) {
+// One product alone; the gated layer's is not parted.
+inline ProductCut product_cut(const ProductSize& s, int dt_bf16, bool gated) {
   ProductCut best{64, 1, 1e300};
   const long long stages = s.stages(dt_bf16);
   // (at least four stages a part; the parts' sums stay within 256 MiB)
-  const long long most = !may_part ? 1 : std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
-  for (int i = 0; i < (dt_bf16 ? 3 : 2); ++i) {
+  const long long most = gated ? 1 : std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
+  for (int i = 0; i < (dt_bf16 ? 3 : 2) + (gated ? 1 : 0); ++i) {
     const ProductTile& t = dt_bf16 ? kTilesBf16[i] : kTilesF32[i];
     const long long tiles = s.tiles(t.size), slots = 256LL * t.per_cu;
+    if (i && tiles > 1 << 22) break;  // (fewer than 2^31 threads a launch)
     for (const int p : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
       if (p > most || (p > 1 && tiles * p > 3 * slots)) break;
       const long long all = tiles * p, rest = all % slots;
@@ -526,7 +528,7 @@ struct ProductCuts {
 };
 
 inline ProductCuts product_cuts(const ProductSize& x, const ProductSize& w, int dt_bf16) {
-  ProductCuts best{product_cut(x, dt_bf16, true), product_cut(w, dt_bf16, true), false};
+  ProductCuts best{product_cut(x, dt_bf16, false), product_cut(w, dt_bf16, false), false};
   double least = best.x.us + best.W.us + 8.0;
   const long long sx = x.stages(dt_bf16), sw = w.stages(dt_bf16);
   auto most = [](const ProductSize& s, long long stages) {
@@ -537,6 +539,7 @@ inline ProductCuts product_cuts(const ProductSize& x, const ProductSize& w, int 
   for (int i = 0; i < (dt_bf16 ? 3 : 2); ++i) {
     const ProductTile& t = dt_bf16 ? kTilesBf16[i] : kTilesF32[i];
     const long long slots = 256LL * t.per_cu, tx = x.tiles(t.size), tw = w.tiles(t.size);
+    if (i && tx + tw > 1 << 22) break;
     const double full = t.a + t.b * t.per_cu;
     for (const int px : {1, 2, 4, 8, 16}) {
       if (px > mx || (px > 1 && tx * px > slots)) break;

@@ -83,6 +83,49 @@ __global__ __launch_bounds__(512) void gated_few_kernel(ProductArgs a) {
 // (32 x 640 x 2560 bf16 5.3 us, by tiles 5.5; 64 x 512 x 2048 fp32 would take 10.6 for 8.0)
 constexpr int kFewRows = 32;
 
+// Where the contraction is parted: the parts' sums added in order, four columns of the gate and
+// of the other product a thread, then the layer's end.
+template <int DT>
+__global__ __launch_bounds__(256) void gated_join_kernel(ProductArgs a) {
+  using T = Chunk<DT>;
+  const int N = a.N, across = (N + 3) / 4;
+  const long long n = (long long)a.M * across;
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += 256LL * gridDim.x) {
+    const long long row = i / across;
+    const int c = (int)(i - row * across) * 4, m = min(4, N - c);
+    const float* p = a.part + row * 2 * N + c;
+    const size_t step = (size_t)a.M * 2 * N;
+    float g[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+    if (m == 4) {
+#pragma unroll 4
+      for (int q = 0; q < a.parts; ++q) {
+        float f[4];
+        Chunk<0>::unpack(Chunk<0>::raw_at(reinterpret_cast<const char*>(p + q * step), 0), f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) g[j] += f[j];
+        Chunk<0>::unpack(Chunk<0>::raw_at(reinterpret_cast<const char*>(p + q * step + N), 0), f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] += f[j];
+      }
+    } else {
+      for (int q = 0; q < a.parts; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < m) g[j] += p[q * step + j], u[j] += p[q * step + N + j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j >= m) break;
+      if (a.bias) g[j] += T::load1(a.bias, c + j), u[j] += T::load1(a.bias, (size_t)N + c + j);
+      if (a.pre) {
+        T::store1(a.pre, row * 2 * N + c + j, g[j]);
+        T::store1(a.pre, row * 2 * N + N + c + j, u[j]);
+      }
+      T::store1(a.out, row * N + c + j, gate_act<DT>(a.act, g[j]) * u[j]);
+    }
+  }
+}
+
 template <int DT>
 hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
   const void* fn = a.M <= 16 ? (const void*)&gated_few_kernel<DT, 1> : (const void*)&gated_few_kernel<DT, 2>;
@@ -92,15 +135,14 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t stream) {
 
 template <class G>
 hipError_t launch_tile(const ProductArgs& a, hipStream_t stream) {
-  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + G::BN / 2 - 1) / (G::BN / 2));
+  const long long tiles = ((long long)(a.M + G::BM - 1) / G::BM) * ((a.N + G::BN / 2 - 1) / (G::BN / 2)) * a.parts;
   if (tiles > INT32_MAX / G::kThreads) return hipErrorInvalidConfiguration;
   return launch_with_smem((const void*)&product_gated_kernel<G>, dim3((unsigned)tiles), dim3(G::kThreads), G::kSmem, stream,
                           nullptr, nullptr, a);
 }
 
 template <int DT>
-hipError_t launch_tiles(const ProductArgs& a, hipStream_t stream) {
-  const int tile = product_cut({a.M, 2LL * a.N, a.K}, DT, true).tile;
+hipError_t launch_tiles(const ProductArgs& a, int tile, hipStream_t stream) {
   if constexpr (DT == 1)
     if (tile == 256) return launch_tile<ProductCfg<1, false, false, 256, 256, 2, 4>>(a, stream);
   if (tile == 128) return launch_tile<ProductCfg<DT, false, false, 128, 128, 2, 2>>(a, stream);
@@ -108,20 +150,47 @@ hipError_t launch_tiles(const ProductArgs& a, hipStream_t stream) {
   return launch_tile<ProductCfg<DT, false, false, 32, 32, 2, 2>>(a, stream);
 }
 
-}  // namespace
+// The workspace: rows of x and W brought to whole vectors, the parts' sums.
+struct GatedPlan {
+  size_t W = 0, part = 0, bytes = 0;  // offsets
+  bool pack;
+  ProductCut cut;
+};
 
-size_t gated_ws_bytes(int R, int K, int F, int dt_bf16) {
-  if (R <= kFewRows || K % (dt_bf16 ? 8 : 4) == 0) return 0;
-  const size_t row = packed_row(K, dt_bf16);
-  return whole256(R * row) + 2 * (size_t)F * row;
+GatedPlan make_plan(int R, int K, int F, int dt_bf16) {
+  GatedPlan p{};
+  if (R <= kFewRows) return p;
+  p.pack = K % (dt_bf16 ? 8 : 4) != 0;
+  if (p.pack) {
+    p.W = whole256(R * packed_row(K, dt_bf16));
+    p.part = p.W + whole256(2 * (size_t)F * packed_row(K, dt_bf16));
+  }
+  p.cut = product_cut({R, 2LL * F, K}, dt_bf16, true);
+  p.bytes = p.part + (p.cut.parts > 1 ? (size_t)p.cut.parts * R * 2 * F * 4 : 0);
+  return p;
 }
 
+// A call asks three times: for the workspace's size, its check and the launch.
+const GatedPlan& plan(int R, int K, int F, int dt_bf16) {
+  thread_local int key[4] = {};
+  thread_local GatedPlan last;
+  const int now[4] = {R, K, F, dt_bf16};
+  if (!std::equal(key, key + 4, now)) {
+    last = make_plan(R, K, F, dt_bf16);
+    std::copy(now, now + 4, key);
+  }
+  return last;
+}
+
+}  // namespace
+
+size_t gated_ws_bytes(int R, int K, int F, int dt_bf16) { return plan(R, K, F, dt_bf16).bytes; }
+
 hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream) {
-  const int es = dt_bf16 ? 2 : 4;
   ProductArgs a{};
   a.A = g.x;
   a.B = g.W;
-  a.lda = a.ldb = (long long)g.K * es;
+  a.lda = a.ldb = (long long)g.K * (dt_bf16 ? 2 : 4);
   a.M = g.R;
   a.N = g.F;
   a.K = g.K;
@@ -130,16 +199,23 @@ hipError_t launch_gated(const GatedArgs& g, int dt_bf16, hipStream_t stream) {
   a.pre = g.pre;
   a.act = g.act;
   if (g.R <= kFewRows) return dt_bf16 ? launch_few<1>(a, stream) : launch_few<0>(a, stream);
-  if (g.K % (16 / es)) {  // rows of whole vectors in the workspace
-    const size_t row = packed_row(g.K, dt_bf16);
-    char *x = static_cast<char*>(g.ws), *W = x + whole256(g.R * row);
-    hipError_t e = launch_pack_rows(PackPair{{{g.x, x, g.R, g.K}, {g.W, W, 2 * g.F, g.K}}}, dt_bf16, stream);
+  const GatedPlan& p = plan(g.R, g.K, g.F, dt_bf16);
+  char* ws = static_cast<char*>(g.ws);
+  if (p.pack) {
+    hipError_t e = launch_pack_rows(PackPair{{{g.x, ws, g.R, g.K}, {g.W, ws + p.W, 2 * g.F, g.K}}}, dt_bf16, stream);
     if (e != hipSuccess) return e;
-    a.A = x;
-    a.B = W;
-    a.lda = a.ldb = (long long)row;
+    a.A = ws;
+    a.B = ws + p.W;
+    a.lda = a.ldb = (long long)packed_row(g.K, dt_bf16);
   }
-  return dt_bf16 ? launch_tiles<1>(a, stream) : launch_tiles<0>(a, stream);
+  a.parts = p.cut.parts;
+  a.part = reinterpret_cast<float*>(ws + p.part);
+  hipError_t e = dt_bf16 ? launch_tiles<1>(a, p.cut.tile, stream) : launch_tiles<0>(a, p.cut.tile, stream);
+  if (e != hipSuccess || a.parts == 1) return e;
+  const unsigned grid = (unsigned)std::min<long long>(((long long)g.R * ((g.F + 3) / 4) + 255) / 256, 8192);
+  if (dt_bf16) gated_join_kernel<1><<<grid, 256, 0, stream>>>(a);
+  else gated_join_kernel<0><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace gl

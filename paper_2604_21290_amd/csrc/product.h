@@ -32,7 +32,7 @@
 
 namespace gl {
 
-enum { kProductStore = 0, kProductPart = 1, kProductGated = 2 };  // what becomes of the sums
+enum { kProductStore = 0, kProductPart = 1, kProductGated = 2, kProductGatedPart = 3 };  // what becomes of the sums
 
 struct ProductArgs {
   const void *A, *B;
@@ -40,7 +40,7 @@ struct ProductArgs {
   int M, N, K;         // K: of the contraction, in elements; whole 16 bytes where it lies along rows
   int cols_a, cols_b;  // 16-byte places of a row, where the contraction goes down the columns
   void* out;           // [M, N], or h [M, N] of the gated layer, whose B has 2 N rows
-  float* part;         // [parts, M, N]
+  float* part;         // [parts, M, N], gated [parts, M, 2 N]
   int parts;           // of the contraction, whole stages each
   const void* bias;    // [2 N] or null (gated)
   void* pre;           // [M, 2 N] or null (gated)
@@ -194,8 +194,9 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, t = lane & 15, wm = w / G::WC, wn = w % G::WC;
   using T = Chunk<DT>;
-  constexpr int E = EPI == kProductPart ? 4 : T::E;
-  constexpr int COLS = EPI == kProductGated ? G::WCOLS / 2 : G::WCOLS;
+  constexpr bool GATED = EPI == kProductGated || EPI == kProductGatedPart;
+  constexpr int E = EPI == kProductPart || EPI == kProductGatedPart ? 4 : T::E;
+  constexpr int COLS = GATED ? G::WCOLS / 2 : G::WCOLS;
   constexpr int LPR = COLS / E, RPP = 64 / LPR, ER = G::ER, CSW = G::WCOLS / 4 < 16 ? G::WCOLS / 4 - 1 : 15;
   static_assert(ER % RPP == 0 || RPP % ER == 0, "whole passes, or one");
   const int cq = lane % LPR, rq = lane / LPR;
@@ -246,14 +247,21 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
       from(cq * E, y);
       if (EPI == kProductStore) {
         put(a.out, (size_t)row * a.N + n, y);
-      } else if (EPI == kProductPart) {
-        float* o = a.part + ((size_t)part * a.M + row) * a.N + n;
-        if (n + E <= a.N) {
-          Chunk<0>::store(o, 0, y);
-        } else {
+      } else if (EPI == kProductPart || EPI == kProductGatedPart) {
+        auto sums = [&](float* o) {
+          if (n + E <= a.N) {
+            Chunk<0>::store(o, 0, y);
+          } else {
 #pragma unroll
-          for (int v = 0; v < E; ++v)
-            if (n + v < a.N) o[v] = y[v];
+            for (int v = 0; v < E; ++v)
+              if (n + v < a.N) o[v] = y[v];
+          }
+        };
+        float* o = a.part + ((size_t)part * a.M + row) * (GATED ? 2 * (size_t)a.N : a.N) + n;
+        sums(o);
+        if (GATED) {
+          from(COLS + cq * E, y);
+          sums(o + a.N);
         }
       } else {
         float u[E];
@@ -272,7 +280,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
   }
 }
 
-// Workgroup `id` of `count` of a product.  EPI: kProductGated or kProductStore, which writes
+// Workgroup `id` of `count` of a product.  EPI: kProductGated or kProductStore, which write
 // parts where there are several.
 template <class G, int EPI>
 __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, int id, int count) {
@@ -281,7 +289,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
   const int ntm = (a.M + BM - 1) / BM, ntn = (a.N + OUT - 1) / OUT;
   // tiles by bands of eight rows of them, so that what an XCD's workgroups share is in its L2
   int blk = xcd_remap(id, count), part = 0;
-  if (EPI != kProductGated && a.parts > 1) {
+  if (a.parts > 1) {
     part = blk / (ntm * ntn);
     blk -= part * ntm * ntn;
   }
@@ -296,7 +304,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
   // halves h0 .. h1 of the contraction, whole stages (the last half may be all zeros)
   const long long stages = (a.K + 2 * G::HALF - 1) / (2 * G::HALF);
   int h0 = 0, h1 = 2 * (int)stages;
-  if (EPI != kProductGated && a.parts > 1) {
+  if (a.parts > 1) {
     h0 = 2 * (int)(stages * part / a.parts);
     h1 = 2 * (int)(stages * (part + 1) / a.parts);
   }
@@ -420,9 +428,13 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
     }
   }
 
-  if (EPI == kProductGated) product_epilogue<G, kProductGated>(a, smem, acc, m0, n0, 0);
-  else if (a.parts > 1) product_epilogue<G, kProductPart>(a, smem, acc, m0, n0, part);
-  else product_epilogue<G, kProductStore>(a, smem, acc, m0, n0, 0);
+  if (EPI == kProductGated) {
+    if (a.parts > 1) product_epilogue<G, kProductGatedPart>(a, smem, acc, m0, n0, part);
+    else product_epilogue<G, kProductGated>(a, smem, acc, m0, n0, 0);
+  } else if (a.parts > 1)
+    product_epilogue<G, kProductPart>(a, smem, acc, m0, n0, part);
+  else
+    product_epilogue<G, kProductStore>(a, smem, acc, m0, n0, 0);
 }
 
 // Two products in one launch, of which either may be missing: x's gradient, whose first
@@ -481,7 +493,10 @@ struct ProductTile {
   int size, per_cu;
   double a, b, round;
 };
-// (the tile of 32 is the gated layer's alone: 777 x 501 x 333 fp32 fills the chip with it)
+// (the tile of 32 is the gated layer's alone: 777 x 501 x 333 fp32 fills the chip with it.  Its
+// activations and its rows of pre and h make a round longer: 12544 x 640 x 2560 117 us with
+// 256, 125 with 128, 162 with 64; 100352 x 80 x 320 69, 58, 58; 6272 x 192 x 768 18.8, 18.0, 15.5)
+constexpr double kGatedRound[] = {12.5, 6.2, 2.6, 2.4};
 constexpr ProductTile kTilesBf16[] = {{256, 1, 0.0, 1.66, 4.5}, {128, 2, 0.5, 0.22, 3.3}, {64, 4, 0.2, 0.15, 1.0}, {32, 8, 0.25, 0.06, 1.0}};
 constexpr ProductTile kTilesF32[] = {{128, 2, 0.5, 1.75, 4.0}, {64, 4, 0.4, 0.45, 1.5}, {32, 8, 0.25, 0.15, 1.0}};
 
@@ -496,12 +511,12 @@ struct ProductCut {
   double us;
 };
 
-// One product alone; the gated layer's is not parted.
+// One product alone.
 inline ProductCut product_cut(const ProductSize& s, int dt_bf16, bool gated) {
   ProductCut best{64, 1, 1e300};
   const long long stages = s.stages(dt_bf16);
   // (at least four stages a part; the parts' sums stay within 256 MiB)
-  const long long most = gated ? 1 : std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
+  const long long most = std::max<long long>(1, std::min<long long>(stages / 4, (64LL << 20) / (s.M * s.N)));
   for (int i = 0; i < (dt_bf16 ? 3 : 2) + (gated ? 1 : 0); ++i) {
     const ProductTile& t = dt_bf16 ? kTilesBf16[i] : kTilesF32[i];
     const long long tiles = s.tiles(t.size), slots = 256LL * t.per_cu;
@@ -509,9 +524,9 @@ inline ProductCut product_cut(const ProductSize& s, int dt_bf16, bool gated) {
     for (const int p : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
       if (p > most || (p > 1 && tiles * p > 3 * slots)) break;
       const long long all = tiles * p, rest = all % slots;
-      const double n = (double)((stages + p - 1) / p);
-      double us = (double)(all / slots) * (n * (t.a + t.b * t.per_cu) + t.round);
-      if (rest) us += n * (t.a + t.b * (double)((rest + 255) / 256)) + t.round;
+      const double n = (double)((stages + p - 1) / p), round = gated && p == 1 ? kGatedRound[i + !dt_bf16] : t.round;
+      double us = (double)(all / slots) * (n * (t.a + t.b * t.per_cu) + round);
+      if (rest) us += n * (t.a + t.b * (double)((rest + 255) / 256)) + round;
       if (p > 1) us += 5.0 + (double)(8 * p + 4) * (double)(s.M * s.N) / 5.5e6;
       if (us < best.us) best = ProductCut{t.size, p, us};
     }

@@ -30,7 +30,8 @@ def _weight(seed, N, K, dtype):
 # one row to the largest tiles; whole vectors and odd sizes; contractions shorter than a
 # stage, of whole stages and past them
 GATED = [(1, 8, 8), (1, 640, 2560), (1, 37, 5), (3, 1, 1), (16, 200, 24), (17, 100, 33), (64, 129, 40), (65, 129, 40),
-         (65, 8, 3), (100, 192, 96), (196, 192, 768), (300, 64, 700), (777, 501, 333), (1500, 72, 1100), (2600, 648, 2560)]
+         (65, 8, 3), (100, 192, 96), (196, 192, 768), (300, 64, 700), (777, 501, 333), (1500, 72, 1100), (2600, 648, 2560),
+         (278, 2912, 112), (70, 4001, 33), (40, 3000, 7), (32, 1030, 50)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -10,7 +10,7 @@ namespace gl {
 
 namespace {
 
-constexpr int kSumGroups = 256;  // most groups of rows whose sums are kept apart
+constexpr int kSumGroups = 512;  // most groups of rows whose sums are kept apart
 
 // rows [R, C] to rows of whole 16-byte vectors with zeros at their ends: 64 vectors of four
 // rows a workgroup and turn, workgroup `id` of `count`
@@ -21,29 +21,36 @@ __device__ __forceinline__ void pack_rows(const PackRows& a, int id, int count) 
   const int C = a.C, row = (C * ES + 15) & ~15, across = (row / 16 + 63) / 64;
   const int y = id / across, v = (id - y * across) * 64 + (threadIdx.x & 63), c = v * E;
   if (v * 16 >= row) return;
-  for (long long r = y * 4 + (threadIdx.x >> 6); r < a.R; r += 4LL * (count / across)) {
-    const char* p = static_cast<const char*>(a.src) + r * C * ES;
-    uint4 q;
-    if (c + E <= C) {
-      q = T::raw(p, c);
-    } else {
-      uint32_t w[4] = {0, 0, 0, 0};
+  const long long step = 4LL * (count / across);
+  constexpr int U = 4;  // rows under way
+  for (long long r = y * 4 + (threadIdx.x >> 6); r < a.R; r += U * step) {
+    uint4 q[U];
 #pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (c + j < C) {
-          if (DT) w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[c + j] << (j % 2 * 16);
-          else w[j] = reinterpret_cast<const uint32_t*>(p)[c + j];
-        }
-      q = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int u = 0; u < U; ++u) {
+      const char* p = static_cast<const char*>(a.src) + min(r + u * step, a.R - 1LL) * C * ES;
+      if (c + E <= C) {
+        q[u] = T::raw(p, c);
+      } else {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          if (c + j < C) {
+            if (DT) w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[c + j] << (j % 2 * 16);
+            else w[j] = reinterpret_cast<const uint32_t*>(p)[c + j];
+          }
+        q[u] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
-    *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + r * row + v * 16) = q;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r + u * step < a.R) *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + (r + u * step) * row + v * 16) = q[u];
   }
 }
 // workgroups for it, whole rows of them
 int pack_count(const PackRows& a, int dt_bf16) {
   if (!a.src) return 0;
   const int across = (int)((packed_row(a.C, dt_bf16) / 16 + 63) / 64);
-  return across * std::min((a.R + 3) / 4, std::max(1, 4096 / across));
+  return across * std::min((a.R + 15) / 16, std::max(1, 4096 / across));
 }
 
 template <int DT>
@@ -65,11 +72,11 @@ struct PrepareArgs {
   int pack_first;        // workgroups of the first copy
 };
 
-// 32 lanes take 32 chunks of columns, eight rows a turn.
-template <int DT, bool GATED>
+// CL lanes take as many chunks of columns, 256 / CL rows a turn and two turns' loads under way.
+template <int DT, bool GATED, int CL>
 __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   using T = Chunk<DT>;
-  constexpr int E = T::E, ES = DT ? 2 : 4, CL = 32, RL = 256 / CL, NS = GATED ? 2 : 1;
+  constexpr int E = T::E, ES = DT ? 2 : 4, RL = 256 / CL, NS = GATED ? 2 : 1, U = 2;
   __shared__ float sums[RL][CL * E + 4];
   int id = blockIdx.x;
   if (id >= a.across * a.groups) {
@@ -82,13 +89,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   const int lane = threadIdx.x % CL, rl = threadIdx.x / CL;
   const int F = a.F, c = (block * CL + lane) * E;
   const bool on = c < F, whole = c + E <= F;
-  auto load = [&](const void* p, size_t at, float* f) {
-    if (whole) {
-      T::unpack(T::raw(p, at), f);
-    } else {
+  auto load = [&](const void* p, size_t at) {
+    if (whole) return T::raw(p, at);
+    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < E; ++j) f[j] = c + j < F ? T::load1(p, at + j) : 0.f;
-    }
+    for (int j = 0; j < E; ++j)
+      if (c + j < F) {
+        if (DT) w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[at + j] << (j % 2 * 16);
+        else w[j] = static_cast<const uint32_t*>(p)[at + j];
+      }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   };
   auto put = [&](char* p, size_t at, const float* f) {
     if (whole) {
@@ -102,34 +112,49 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   float s[NS][E] = {};
   const long long step = (long long)RL * a.groups;
   if (on)
-    for (long long r = (long long)group * RL + rl; r < a.R; r += step) {
-      float d[E];
-      load(a.dy, (size_t)r * F + c, d);
-      char* o = a.out + (size_t)r * a.row;
-      if (GATED) {
-        float p[E], u[E];
-        load(a.pre, (size_t)r * 2 * F + c, p);
-        load(a.pre, (size_t)r * 2 * F + F + c, u);
+    for (long long r0 = (long long)group * RL + rl; r0 < a.R; r0 += U * step) {
+      uint4 rd[U], rp[U], ru[U];
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          float da;
-          const float act = gate_act_grad(a.act, p[j], &da);
-          p[j] = d[j] * u[j] * da;
-          u[j] = d[j] * act;
-          s[0][j] += p[j];
-          s[NS - 1][j] += u[j];
+      for (int k = 0; k < U; ++k) {
+        const long long r = min(r0 + k * step, a.R - 1LL);
+        rd[k] = load(a.dy, (size_t)r * F + c);
+        if (GATED) {
+          rp[k] = load(a.pre, (size_t)r * 2 * F + c);
+          ru[k] = load(a.pre, (size_t)r * 2 * F + F + c);
         }
-        if (a.out) {
-          put(o, c, p);
-          put(o, F + c, u);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < E; ++j) s[0][j] += d[j];
-        if (a.out) put(o, c, d);
       }
-      if (a.out && c + E >= F)  // the row's last chunk
-        for (int k = NS * F; k < a.row / ES; ++k) T::store1(o, k, 0.f);
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const long long r = r0 + k * step;
+        if (r >= a.R) break;
+        float d[E];
+        T::unpack(rd[k], d);
+        char* o = a.out + (size_t)r * a.row;
+        if (GATED) {
+          float p[E], u[E];
+          T::unpack(rp[k], p);
+          T::unpack(ru[k], u);
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            float da;
+            const float act = gate_act_grad(a.act, p[j], &da);
+            p[j] = d[j] * u[j] * da;
+            u[j] = d[j] * act;
+            s[0][j] += p[j];
+            s[NS - 1][j] += u[j];
+          }
+          if (a.out) {
+            put(o, c, p);
+            put(o, F + c, u);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) s[0][j] += d[j];
+          if (a.out) put(o, c, d);
+        }
+        if (a.out && c + E >= F)  // the row's last chunk
+          for (int q = NS * F; q < a.row / ES; ++q) T::store1(o, q, 0.f);
+      }
     }
   if (!a.part) return;
 #pragma unroll
@@ -247,11 +272,13 @@ hipError_t launch_tile(const ProductPair& p, int tile, hipStream_t stream) {
   return tile == 128 ? launch_pair<DT, 128>(p, stream) : launch_pair<DT, 64>(p, stream);
 }
 
-// Groups of rows of the sums over rows.
+// Lanes to a row of F columns (narrow rows would leave most of 32 idle), and groups of rows of
+// the sums over rows.
+int row_lanes(int F, int dt_bf16) { return F <= (dt_bf16 ? 64 : 32) ? 8 : 32; }
 int sum_groups(int R, int F, int dt_bf16) {
-  const long long cols = ((long long)F + (dt_bf16 ? 255 : 127)) / (dt_bf16 ? 256 : 128);
-  const long long rows = ((long long)R + 7) / 8;
-  return (int)std::max<long long>(1, std::min<long long>({rows, (2048 + cols - 1) / cols, kSumGroups}));
+  const int lanes = row_lanes(F, dt_bf16), e = dt_bf16 ? 8 : 4;
+  const long long cols = ((long long)F + lanes * e - 1) / (lanes * e), rows = ((long long)R + 256 / lanes - 1) / (256 / lanes);
+  return (int)std::max<long long>(1, std::min<long long>({(rows + 1) / 2, (2048 + cols - 1) / cols, kSumGroups}));
 }
 
 // The workspace of a backward pass, its pieces 256 bytes apart.
@@ -318,16 +345,18 @@ hipError_t launch_grad(const LinearGradArgs& g, hipStream_t stream) {
   s.row = (int)packed_row(g.N, DT);
   s.out = products && p.pack_dy ? ws + p.dy : nullptr;
   s.part = !g.db ? nullptr : p.groups > 1 ? reinterpret_cast<float*>(ws + p.sums) : g.db;
-  s.across = (F + 32 * E - 1) / (32 * E);
+  const int lanes = row_lanes(F, DT);
+  s.across = (F + lanes * E - 1) / (lanes * E);
   s.groups = s.out || s.part ? p.groups : 0;
   if (p.pack_x && g.dW) s.pack.t[0] = {g.x, ws + p.x, g.R, g.K};
   if (p.pack_x && g.dx) s.pack.t[1] = {g.W, ws + p.W, g.N, g.K};
   s.pack_first = pack_count(s.pack.t[0], DT);
   const int before = s.across * s.groups + s.pack_first + pack_count(s.pack.t[1], DT);
   if (before) {
-    if (gated) prepare_kernel<DT, true><<<before, 256, 0, stream>>>(s);
-    else prepare_kernel<DT, false><<<before, 256, 0, stream>>>(s);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    void* argv[] = {&s};
+    const void* fn = gated ? (lanes == 8 ? (const void*)&prepare_kernel<DT, true, 8> : (const void*)&prepare_kernel<DT, true, 32>)
+                           : (lanes == 8 ? (const void*)&prepare_kernel<DT, false, 8> : (const void*)&prepare_kernel<DT, false, 32>);
+    if ((e = hipLaunchKernel(fn, dim3(before), dim3(256), argv, 0, stream)) != hipSuccess) return e;
   }
 
   ProductPair q{};

@@ -53,27 +53,43 @@ __device__ __forceinline__ float sigmoid_f32(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
 }
 
-// The gate's activation (uniform `act`); x sigmoid(x) is 0 at -infinity.
-template <int DT>
-__device__ __forceinline__ float gate_act(int act, float x) {
-  if (act == kActGelu) return gelu_tail<DT>(x);
-  return act == kActSilu ? fmaxf(x, -3.4e38f) * sigmoid_f32(x) : x;
+// The gate's activation of N values (uniform `act`, asked once: behind a branch for each value
+// their chains of instructions would run one after the other); x sigmoid(x) is 0 at -infinity.
+template <int DT, int N>
+__device__ __forceinline__ void gate_acts(int act, float (&x)[N]) {
+  if (act == kActGelu) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = gelu_tail<DT>(x[j]);
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = fmaxf(x[j], -3.4e38f) * sigmoid_f32(x[j]);
+  }
 }
 
-// The activation and its derivative:
+// The activation, in place, and its derivative:
 //   GELU  Phi(x) + x e^(-x^2 / 2) / sqrt(2 pi)
 //   SiLU  s + x s (1 - s), s = sigmoid(x); 1 - s is sigmoid(-x), which keeps its bits
-__device__ __forceinline__ float gate_act_grad(int act, float x, float* da) {
-  if (act == kActNone) return *da = 1.f, x;
-  if (act == kActSilu) {
-    const float s = sigmoid_f32(x), c = fmaxf(fminf(x, 3.4e38f), -3.4e38f) * s;
-    *da = fmaf(c, sigmoid_f32(-x), s);
-    return fmaxf(x, -3.4e38f) * s;
+template <int N>
+__device__ __forceinline__ void gate_act_grads(int act, float (&x)[N], float (&da)[N]) {
+  if (act == kActGelu) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float a = fminf(fabsf(x[j]), 3.4e38f), e = gauss_exp(x[j]), tail = gauss_tail<0>(a) * e;
+      const float c = a * e * 0.3989422804014327f;
+      da[j] = x[j] < 0.f ? tail - c : 1.f - tail + c;
+      x[j] = fmaf(-a, tail, fmaxf(x[j], 0.f));
+    }
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float s = sigmoid_f32(x[j]), c = fmaxf(fminf(x[j], 3.4e38f), -3.4e38f) * s;
+      da[j] = fmaf(c, sigmoid_f32(-x[j]), s);
+      x[j] = fmaxf(x[j], -3.4e38f) * s;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) da[j] = 1.f;
   }
-  const float a = fminf(fabsf(x), 3.4e38f), e = gauss_exp(x), tail = gauss_tail<0>(a) * e;
-  const float c = a * e * 0.3989422804014327f;
-  *da = x < 0.f ? tail - c : 1.f - tail + c;
-  return fmaf(-a, tail, fmaxf(x, 0.f));
 }
 
 }  // namespace gl

@@ -76,7 +76,9 @@ __global__ __launch_bounds__(512) void gated_few_kernel(ProductArgs a) {
       T::store1(a.pre, (size_t)r * 2 * a.N + n, y);
       T::store1(a.pre, (size_t)r * 2 * a.N + a.N + n, u);
     }
-    T::store1(a.out, (size_t)r * a.N + n, gate_act<DT>(a.act, y) * u);
+    float g[1] = {y};
+    gate_acts<DT>(a.act, g);
+    T::store1(a.out, (size_t)r * a.N + n, g[0] * u);
   }
 }
 
@@ -121,8 +123,11 @@ __global__ __launch_bounds__(256) void gated_join_kernel(ProductArgs a) {
         T::store1(a.pre, row * 2 * N + c + j, g[j]);
         T::store1(a.pre, row * 2 * N + N + c + j, u[j]);
       }
-      T::store1(a.out, row * N + c + j, gate_act<DT>(a.act, g[j]) * u[j]);
     }
+    gate_acts<DT>(a.act, g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < m) T::store1(a.out, row * N + c + j, g[j] * u[j]);
   }
 }
 

@@ -131,15 +131,14 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
         T::unpack(rd[k], d);
         char* o = a.out + (size_t)r * a.row;
         if (GATED) {
-          float p[E], u[E];
-          T::unpack(rp[k], p);
+          float act[E], p[E], u[E];
+          T::unpack(rp[k], act);
           T::unpack(ru[k], u);
+          gate_act_grads(a.act, act, p);
 #pragma unroll
           for (int j = 0; j < E; ++j) {
-            float da;
-            const float act = gate_act_grad(a.act, p[j], &da);
-            p[j] = d[j] * u[j] * da;
-            u[j] = d[j] * act;
+            p[j] *= d[j] * u[j];
+            u[j] = d[j] * act[j];
             s[0][j] += p[j];
             s[NS - 1][j] += u[j];
           }

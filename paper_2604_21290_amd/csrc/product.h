@@ -272,8 +272,9 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& a, char* sme
           put(a.pre, (size_t)row * 2 * a.N + n, y);
           put(a.pre, (size_t)row * 2 * a.N + a.N + n, u);
         }
+        gate_acts<DT>(a.act, y);
 #pragma unroll
-        for (int v = 0; v < E; ++v) y[v] = gate_act<DT>(a.act, y[v]) * u[v];
+        for (int v = 0; v < E; ++v) y[v] *= u[v];
         put(a.out, (size_t)row * a.N + n, y);
       }
     }

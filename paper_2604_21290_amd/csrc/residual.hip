@@ -92,9 +92,14 @@ __global__ __launch_bounds__(LPR ? 256 : 512) void residual_kernel(ResidualArgs 
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
         float q = 0.f;
-        const int skip = ragged ? (lane + v * lanes) * E - at[v] : 0;
+        if (ragged) {
+          const int skip = (lane + v * lanes) * E - at[v];
 #pragma unroll
-        for (int j = 0; j < E; ++j) q = !ragged || j >= skip ? term(q, p[v][j]) : q;
+          for (int j = 0; j < E; ++j) q = j >= skip ? term(q, p[v][j]) : q;
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) q = term(q, p[v][j]);
+        }
         s += on(v) ? q : 0.f;
       }
       return join_sum<LPR>(s, slot);

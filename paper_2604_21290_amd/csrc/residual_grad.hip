@@ -61,7 +61,20 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
 #pragma unroll
   for (int v = 0; v < VPL; ++v) at[v] = min(min(lane + v * lanes, n - 1) * E, C - E);
   auto on = [&](int v) { return lane + v * lanes < n; };
-  auto counts = [&](int v, int j) { return on(v) && (!ragged || j >= (lane + v * lanes) * E - at[v]); };
+  // adds up what `term` makes of the chunk's values that count: not those that the chunk
+  // before it has too, and none of a lane past the row's end
+  auto add_up = [&](int v, float& sum, auto term) {
+    float q = 0.f;
+    if (ragged) {
+      const int skip = (lane + v * lanes) * E - at[v];
+#pragma unroll
+      for (int j = 0; j < E; ++j) q = j >= skip ? term(q, j) : q;
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) q = term(q, j);
+    }
+    sum += on(v) ? q : 0.f;
+  };
   uint4 raw_d[VPL], raw_y[VPL], raw_b[VPL], raw_s[VPL];
   float mb = 0.f, rb = 1.f, ms = 0.f, rs = 0.f, gate = 1.f;
   auto load = [&](long long r0) {
@@ -140,10 +153,9 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
           T1[v][j] = fmaf(h[v][j], x[v][j], T1[v][j]);
           T0[v][j] += h[v][j];
           h[v][j] *= w[j];
-          const float q = counts(v, j) ? h[v][j] : 0.f;
-          p[0] += q;
-          p[1] = fmaf(q, x[v][j], p[1]);
         }
+        if (!a.rms) add_up(v, p[0], [&](float q, int j) { return q + h[v][j]; });
+        add_up(v, p[1], [&](float q, int j) { return fmaf(h[v][j], x[v][j], q); });
       }
       sum_rows<LPR>(p, slots[turn]);
       const float s0 = a.rms ? 0.f : p[0] * a.inv_c * -rsr, s1 = p[1] * a.inv_c * -rsr;
@@ -171,17 +183,18 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const float dg = d[v][j] * gr, k = d[v][j] * (gr * sv[j]);
+        const float dg = d[v][j] * gr;
         if (POST) f[v][j] = (f[v][j] - mbr) * rbr;
         S1[v][j] = fmaf(dg, f[v][j], S1[v][j]);
         if (POST) S0[v][j] += dg;
-        h[v][j] = POST ? k * w[j] : k;
-        if (counts(v, j)) {
-          const float m = POST ? fmaf(f[v][j], w[j], c[j]) : f[v][j];
-          if (POST) p[0] += h[v][j], p[1] = fmaf(h[v][j], f[v][j], p[1]);
-          p[2] = fmaf(d[v][j] * sv[j], m, p[2]);
-        }
+        d[v][j] *= sv[j];
+        h[v][j] = POST ? d[v][j] * gr * w[j] : d[v][j] * gr;
       }
+      if (POST) {
+        if (!a.rms) add_up(v, p[0], [&](float q, int j) { return q + h[v][j]; });
+        add_up(v, p[1], [&](float q, int j) { return fmaf(h[v][j], f[v][j], q); });
+      }
+      if (a.dots) add_up(v, p[2], [&](float q, int j) { return fmaf(d[v][j], POST ? fmaf(f[v][j], w[j], c[j]) : f[v][j], q); });
     }
     if (POST || a.dots) sum_rows<LPR>(p, slots[turn] + 2);
     if (a.dots && mine && lane == 0) (a.dots + first)[rows.lane] = p[2];

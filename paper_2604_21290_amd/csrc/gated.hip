@@ -2,8 +2,11 @@
 //   pre = x W^T + b,  W [2 F, K];  h = act(pre[:, :F]) * pre[:, F:]
 // in one pass: a wave's tile holds as many columns of the gate as of the other product, the
 // same ones, so that both of an output's products end in the same lane's registers and only
-// h (and, for a backward pass, pre) is written.  Many rows: product.h.  Few rows (serving):
-// the kernel below, which reads W once straight into registers.
+// h (and, for a backward pass, pre) is written.  Many rows: product.h; us, GELU, with pre:
+// bf16 16384 x 2048 x 4096 494 (1.11 PFLOP/s), 12544 x 640 x 2560 117 (0.70: ten stages, then
+// the activations, for which the matrix cores wait), 6272 x 192 x 768 15.
+// Few rows (serving): the kernel below, which reads W once straight into registers; one row of
+// 640 x 2560 bf16 3.9 us (W's 6.6 MB from the last level of cache and a launch).
 #include "product.h"
 
 namespace gl {

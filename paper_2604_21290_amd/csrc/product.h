@@ -565,7 +565,7 @@ inline ProductCuts product_cuts(const ProductSize& x, const ProductSize& w, int 
         const double nw = (double)((sw + pw - 1) / pw), cw = (double)(tw * pw), all = cx + cw;
         double us;
         if (all <= (double)slots) {
-          us = std::max(nx, nw) * (t.a + t.b * std::max(1.0, all / 256)) + t.round;
+          us = std::max(nx, nw) * (t.a + t.b * (double)(((long long)all + 255) / 256)) + t.round;
         } else {
           // the workgroups' time shared out, and half of one at the end; one takes its time at least
           const double w1 = nw * full + t.round;

@@ -17,11 +17,11 @@
 //     stages (their rows are whole cache lines), operands down it in a ring of halves, whose
 //     new rows at every half come from other pages and take the longer to arrive: with two
 //     whole stages, one under way, 8192 x 4096 x 4096 took 476 us for the weight's gradient
-//     and 249 for the input's, where the output took 200.
+//     and 249 for the input's (209 and 211 now, 1.3 PFLOP/s, the matrix cores 63 % busy).
 //   - Each wave has the next half's operands on their way to registers while it multiplies
 //     this one's; one barrier for each piece of a ring that is freed and filled again.
-// Contractions are cut by halves of stages where there are too few tiles to fill the chip:
-// each part writes its sums in fp32 to the workspace, and product_join adds them in order.
+// Contractions are cut in parts of whole stages where there are too few tiles to fill the chip:
+// each part writes its sums in fp32 to the workspace, and a last launch adds them in order.
 #pragma once
 
 #include <algorithm>

@@ -92,14 +92,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   const int lane = threadIdx.x % CL, rl = threadIdx.x / CL;
   const int F = a.F, c = (block * CL + lane) * E;
   const bool on = c < F, whole = c + E <= F;
-  auto load = [&](const void* p, size_t at) {
-    if (whole) return T::raw(p, at);
+  // the lane's columns of the row that begins `row` elements from p
+  auto load = [&](const void* p, size_t row) {
+    const char* q = static_cast<const char*>(p) + row * ES;
+    if (whole) return T::raw(q, c);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < E; ++j)
       if (c + j < F) {
-        if (DT) w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[at + j] << (j % 2 * 16);
-        else w[j] = static_cast<const uint32_t*>(p)[at + j];
+        if (DT) w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(q)[c + j] << (j % 2 * 16);
+        else w[j] = reinterpret_cast<const uint32_t*>(q)[c + j];
       }
     return make_uint4(w[0], w[1], w[2], w[3]);
   };
@@ -120,10 +122,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         const long long r = min(r0 + k * step, a.R - 1LL);
-        rd[k] = load(a.dy, (size_t)r * F + c);
+        rd[k] = load(a.dy, (size_t)r * F);
         if (GATED) {
-          rp[k] = load(a.pre, (size_t)r * 2 * F + c);
-          ru[k] = load(a.pre, (size_t)r * 2 * F + F + c);
+          rp[k] = load(a.pre, (size_t)r * 2 * F);
+          ru[k] = load(a.pre, (size_t)r * 2 * F + F);
         }
       }
 #pragma unroll

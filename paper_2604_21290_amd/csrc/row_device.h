@@ -14,6 +14,8 @@ namespace gl {
 // values, which the chunk before it has too, are left out of sums.  So every
 // access lies inside the row and no width or alignment needs a loop over single
 // values (rows shorter than one chunk aside).
+// raw's place is within a row, where 32 bits hold its bytes; a place in a whole matrix, of
+// any wider type, does not compile: the row's pointer is made in 64 bits first.
 // ---------------------------------------------------------------------------
 template <int DT>
 struct Chunk;  // DT 1: bf16, 0: fp32
@@ -24,9 +26,11 @@ template <>
 struct Chunk<1> {
   static constexpr int E = 8;
   static constexpr size_t kSize = 2;
-  __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
+  __device__ __forceinline__ static uint4 raw(const void* p, int i) {
     return load16_any(static_cast<const uint16_t*>(p) + i);
   }
+  template <class I>
+  static uint4 raw(const void* p, I i) = delete;
   __device__ __forceinline__ static uint4 raw_at(const char* p, uint32_t byte) { return load16_any(p + byte); }
   __device__ __forceinline__ static void store_at(char* p, uint32_t byte, const float* f) {
     store16_any(p + byte, pack_bf16x8(f));
@@ -58,9 +62,11 @@ template <>
 struct Chunk<0> {
   static constexpr int E = 4;
   static constexpr size_t kSize = 4;
-  __device__ __forceinline__ static uint4 raw(const void* p, size_t i) {
+  __device__ __forceinline__ static uint4 raw(const void* p, int i) {
     return raw_at(static_cast<const char*>(p), (uint32_t)i * 4);
   }
+  template <class I>
+  static uint4 raw(const void* p, I i) = delete;
   __device__ __forceinline__ static uint4 raw_at(const char* p, uint32_t byte) {
     return __builtin_bit_cast(uint4, *reinterpret_cast<const u32x4_any4*>(p + byte));
   }

@@ -455,15 +455,12 @@ PyObject* py_residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (PyErr_Occurred()) return nullptr;
     const float* st[4] = {};
     const bool means = kind == GL_NORM_LAYER, on[4] = {j.post && means, j.post, j.norm && means, j.norm};
-    PyObject* kept = PySequence_Fast(a[4], "");
-    if (!kept) {
-      PyErr_Clear();
-      return none();
-    }
-    bool ok = PySequence_Fast_GET_SIZE(kept) == 4;
+    // (an iterator's tensors would be gone, and their memory the outputs', before the kernel
+    // reads them: a tuple or a list holds what it is asked for)
+    if (!PyTuple_Check(a[4]) && !PyList_Check(a[4])) return none();
+    bool ok = PySequence_Fast_GET_SIZE(a[4]) == 4;
     for (int i = 0; ok && i < 4; ++i)
-      if (on[i]) ok = PySequence_Fast_GET_ITEM(kept, i) != Py_None && stats(PySequence_Fast_GET_ITEM(kept, i), dev, *b.t, &st[i]);
-    Py_DECREF(kept);
+      if (on[i]) ok = stats(PySequence_Fast_GET_ITEM(a[4], i), dev, *b.t, &st[i]);
     if (!ok) return none();
     const at::ScalarType type = b.t->scalar_type();
     at::Tensor dx = empty(b.t->sizes(), *b.t, type), db = empty(b.t->sizes(), *b.t, type), dgate, v[5], ws;

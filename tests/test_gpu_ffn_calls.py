@@ -1,0 +1,44 @@
+"""The operators that train a gated FFN, called as their documentation allows and rarely
+done: where the statistics come from, what the outputs share, values past 32 bits."""
+import pytest
+import torch
+
+from gpu_helpers import require_gpu
+from paper_2604_21290_amd import api
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def _rand(seed, *shape, dtype=torch.float32, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * size).to(dtype)
+
+
+def _end(R, C, dtype=torch.float32):
+    """(b, its block's end's keywords, s, statistics, ds, dy)"""
+    vec = [_rand(10 + i, C, dtype=dtype) for i in range(5)]
+    how = dict(post=(vec[0], vec[1]), scale=vec[2], gate=_rand(20, R), norm=(vec[3], vec[4]))
+    x, b, ds, dy = (_rand(i, R, C, dtype=dtype) for i in range(4))
+    s, _, st = api.residual_norm(x, b, stats=True, **how)
+    return b, how, s, st, ds, dy
+
+
+def flat(grads):
+    return [t for g in grads for t in (g if isinstance(g, tuple) else (g,))]
+
+
+@pytest.mark.parametrize("R,C", [(300, 72), (196, 1), (4096, 4)])
+def test_statistics_from_an_iterator(R, C):
+    """Whose tensors nobody else holds: they live until the kernel has read them."""
+    b, how, s, st, ds, dy = _end(R, C)
+    want = flat(api.residual_norm_backward(ds, dy, b, s, st, **how))
+    for kept in (list(st), (t.clone() for t in st), map(torch.clone, st), iter(st)):
+        got = flat(api.residual_norm_backward(ds, dy, b, s, kept, **how))
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    with pytest.raises(ValueError, match="mean_b"):
+        api.residual_norm_backward(ds, dy, b, s, (t[:-1].clone() for t in st), **how)

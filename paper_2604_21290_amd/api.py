@@ -353,6 +353,12 @@ def _count(name: str, *ns: int):
         raise GraphLeapError(name, 2, f"counts {ns} past 2^31 - 1")
 
 
+def _choice(name: str, value: int):
+    """An activation or a norm is 32 bits to the library too, which names an unknown one itself."""
+    if not -0x80000000 <= value <= 0x7fffffff:
+        raise GraphLeapError(name, 4, f"unknown choice {value}")
+
+
 def _rows(x: torch.Tensor):
     """(R, C, ld) of a device tensor whose leading axes are rows a uniform stride apart."""
     if not x.is_cuda or x.dim() < 1:
@@ -629,6 +635,7 @@ def gated_linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = N
             return r
     R, K, N = _layer("gated_linear", x, W)
     F = _halves("gated_linear", W)
+    _choice("gated_linear", act)
     _like("bias", bias, (N,), x.dtype, x)
     lead = x.shape[:-1]
     if out is None:
@@ -698,6 +705,7 @@ def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pr
             return r
     R, K, N = _layer("gated_linear_backward", x, W)
     F = _halves("gated_linear_backward", W)
+    _choice("gated_linear_backward", act)
     _matrix("dh", dh, x.shape[:-1] + (F,), x)
     _matrix("pre", pre, x.shape[:-1] + (N,), x)
     dt = _dt(x)
@@ -764,6 +772,7 @@ def residual_norm(x: torch.Tensor, b: torch.Tensor, post=None, scale: torch.Tens
             return (r[0], r[1], ResidualStats(*r[2])) if stats else r
     R, C, ldx = _rows(x)
     Rb, Cb, ldb = _rows(b)
+    _choice("residual_norm", kind)
     if b.shape != x.shape or b.dtype != x.dtype or b.get_device() != x.get_device():
         raise ValueError(f"b {b.dtype} {tuple(b.shape)} does not match x {x.dtype} {tuple(x.shape)}")
     g1, b1 = _norm_pair("post", post, C, x)
@@ -803,6 +812,7 @@ def residual_norm_backward(ds: torch.Tensor | None, dy: torch.Tensor | None, b: 
         if r is not None:
             return ResidualGrads(*r)
     R, C, ldb = _rows(b)
+    _choice("residual_norm_backward", kind)
     if ds is None and dy is None:
         raise ValueError("ds or dy is required")
     if (dy is None) != (norm is None):

@@ -134,6 +134,9 @@ PyObject* guarded(F f) {
 
 PyObject* none() { Py_RETURN_NONE; }
 
+// An activation or a norm: what does not fit 32 bits is not cut short to one that there is.
+bool choice(long v) { return v == (int)v; }
+
 // layer_norm(x, gamma, beta, eps, stats) -> out or (out, mean, rstd)
 PyObject* py_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -325,6 +328,7 @@ PyObject* py_gated_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const long act = PyLong_AsLong(a[3]);
     const int keep = PyObject_IsTrue(a[4]), F = l.N / 2;
     if (PyErr_Occurred()) return nullptr;
+    if (!choice(act)) return none();
     const size_t bytes = p_gated_linear_ws(l.R, l.K, F, l.dt);
     at::Tensor h = empty(with_last(*l.x, F), *l.x, l.x->scalar_type()), pre, ws;
     if (keep) pre = empty(with_last(*l.x, l.N), *l.x, l.x->scalar_type());
@@ -352,6 +356,7 @@ PyObject* layer_backward(PyObject* const* a, bool gated) {
   PyObject* const* need = a + (gated ? 5 : 3);
   const int wx = PyObject_IsTrue(need[0]), ww = PyObject_IsTrue(need[1]), wb = PyObject_IsTrue(need[2]);
   if (PyErr_Occurred()) return nullptr;
+  if (!choice(act)) return none();
   const size_t bytes = gated ? p_gated_linear_backward_ws(l.R, l.K, F, l.dt) : p_linear_backward_ws(l.R, l.K, F, l.dt);
   at::Tensor dx, dW, db, ws;
   if (wx) dx = empty(l.x->sizes(), *l.x, type);
@@ -421,6 +426,7 @@ PyObject* py_residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const double eps = PyFloat_AsDouble(a[7]);
     const int want = PyObject_IsTrue(a[8]);
     if (PyErr_Occurred()) return nullptr;
+    if (!choice(kind)) return none();
     const at::ScalarType type = x.t->scalar_type();
     at::Tensor s = empty(x.t->sizes(), *x.t, type), y, st[4];
     if (j.norm) y = empty(x.t->sizes(), *x.t, type);
@@ -453,6 +459,7 @@ PyObject* py_residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
       return none();
     const long kind = PyLong_AsLong(a[9]);
     if (PyErr_Occurred()) return nullptr;
+    if (!choice(kind)) return none();
     const float* st[4] = {};
     const bool means = kind == GL_NORM_LAYER, on[4] = {j.post && means, j.post, j.norm && means, j.norm};
     // (an iterator's tensors would be gone, and their memory the outputs', before the kernel

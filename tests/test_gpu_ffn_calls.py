@@ -42,3 +42,18 @@ def test_statistics_from_an_iterator(R, C):
         assert all(torch.equal(g, w) for g, w in zip(got, want))
     with pytest.raises(ValueError, match="mean_b"):
         api.residual_norm_backward(ds, dy, b, s, (t[:-1].clone() for t in st), **how)
+
+
+def test_choices_past_32_bits_are_refused():
+    """By the native marshalling too, which would cast 2^32 + 1 to the GELU."""
+    x, W = _rand(1, 40, 8), _rand(2, 8, 8)
+    h, pre = api.gated_linear(x, W, keep=True)
+    b, how, s, st, ds, dy = _end(40, 8)
+    for off in (1 << 32, -(1 << 32)):
+        for call in (lambda: api.gated_linear(x, W, act=off + api.GL_ACT_GELU),
+                     lambda: api.gated_linear_backward(h, x, W, pre, act=off + api.GL_ACT_GELU),
+                     lambda: api.residual_norm(x, b, kind=off, **how),
+                     lambda: api.residual_norm_backward(ds, dy, b, s, st, kind=off + api.GL_NORM_RMS, **how)):
+            with pytest.raises(api.GraphLeapError) as e:
+                call()
+            assert api.STATUS[e.value.status] == "GL_ERR_UNSUPPORTED"

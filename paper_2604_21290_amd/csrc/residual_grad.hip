@@ -123,7 +123,9 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
   // every group of a workgroup makes the same number of turns
   for (; r0 < a.R; r0 += step, turn ^= 1) {
     const long long first = r0 + rows.wave;  // the wave's
-    const bool mine = first + rows.lane < a.R;
+    // a row past the last repeats it: nothing of it is stored, and the sums over rows leave it
+    // out, where 0 times its values would not be 0 for an infinity
+    const bool mine = !LPR || first + rows.lane < a.R;
     float d[VPL][E], h[VPL][E], f[VPL][E], x[VPL][E];
     if (!AHEAD) load(r0);
     const float mbr = mb, rbr = rb, msr = ms, rsr = rs, gr = gate;
@@ -135,11 +137,6 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
       T::unpack(raw_b[v], f[v]);
     }
     if (AHEAD && r0 + step < a.R) load(r0 + step);
-    if (!mine)  // rows past the last count for nothing
-#pragma unroll
-      for (int v = 0; v < VPL; ++v)
-#pragma unroll
-        for (int j = 0; j < E; ++j) d[v][j] = h[v][j] = 0.f;
     auto store = [&](void* out, int v, const float* y) {
       T::store_at(static_cast<char*>(out) + first * C * (long long)T::kSize,
                   (rows.lane * (uint32_t)C + at[v]) * (uint32_t)T::kSize, y);
@@ -152,12 +149,15 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
         if (VPL > 1) keep_packed(g2[v]);
         T::unpack(g2[v], w);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          x[v][j] = (x[v][j] - msr) * rsr;
-          T1[v][j] = fmaf(h[v][j], x[v][j], T1[v][j]);
-          T0[v][j] += h[v][j];
-          h[v][j] *= w[j];
-        }
+        for (int j = 0; j < E; ++j) x[v][j] = (x[v][j] - msr) * rsr;
+        if (mine)
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            T1[v][j] = fmaf(h[v][j], x[v][j], T1[v][j]);
+            T0[v][j] += h[v][j];
+          }
+#pragma unroll
+        for (int j = 0; j < E; ++j) h[v][j] *= w[j];
         if (!a.rms) add_up(v, p[0], [&](float q, int j) { return q + h[v][j]; });
         add_up(v, p[1], [&](float q, int j) { return fmaf(h[v][j], x[v][j], q); });
       }
@@ -168,11 +168,6 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
 #pragma unroll
         for (int j = 0; j < E; ++j) d[v][j] += fmaf(h[v][j], rsr, fmaf(x[v][j], s1, s0));
     }
-    if (!mine)
-#pragma unroll
-      for (int v = 0; v < VPL; ++v)
-#pragma unroll
-        for (int j = 0; j < E; ++j) d[v][j] = 0.f;
     // h: k from here on; p: the sums of k, of k xb and of dv scale n
     float p[3] = {0.f, 0.f, 0.f};
 #pragma unroll
@@ -185,12 +180,18 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(ResidualGradArgs a) {
         T::unpack(g1[v], w);
         T::unpack(b1[v], c);
       }
+      if (POST)
+#pragma unroll
+        for (int j = 0; j < E; ++j) f[v][j] = (f[v][j] - mbr) * rbr;
+      if (mine)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const float dg = d[v][j] * gr;
+          S1[v][j] = fmaf(dg, f[v][j], S1[v][j]);
+          if (POST) S0[v][j] += dg;
+        }
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const float dg = d[v][j] * gr;
-        if (POST) f[v][j] = (f[v][j] - mbr) * rbr;
-        S1[v][j] = fmaf(dg, f[v][j], S1[v][j]);
-        if (POST) S0[v][j] += dg;
         d[v][j] *= sv[j];
         h[v][j] = POST ? d[v][j] * gr * w[j] : d[v][j] * gr;
       }

@@ -57,3 +57,25 @@ def test_choices_past_32_bits_are_refused():
             with pytest.raises(api.GraphLeapError) as e:
                 call()
             assert api.STATUS[e.value.status] == "GL_ERR_UNSUPPORTED"
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("R,C", [(17001, 24), (101, 40), (5001, 80), (99, 250), (37, 500), (5, 5)])
+def test_an_infinity_in_the_last_row_counts_once(R, C, dtype):
+    """The last row's infinities (in b, then in its gate) are terms of the sums over rows once:
+    a workgroup's rows past the last, which repeat it, add no 0 x infinity."""
+    inf = float("inf")
+    b, dy = _rand(1, R, C, dtype=dtype), (1 + _rand(2, R, C).abs()).to(dtype)
+    scale, gate = (1 + _rand(3, C).abs()).to(dtype), 1 + _rand(4, R).abs()
+    b[-1, 1::2], b[-1, 0::4] = inf, -inf
+    g = api.residual_norm_backward(dy, None, b, None, (None,) * 4, scale=scale, gate=gate)
+    want = (dy.double() * gate.double()[:, None] * b.double()).sum(0)
+    special = ~b[-1].isfinite()
+    assert torch.equal(g.dscale[special].double(), want[special]) and want[special].isinf().all()
+    assert g.dscale[~special].isfinite().all()
+    b[-1], gate[-1] = 1.0, inf
+    g = api.residual_norm_backward(dy, None, b, None, (None,) * 4, scale=scale, gate=gate)
+    assert bool((g.dscale == inf).all())
+    st = api.residual_norm(b, b, post=(None, None), stats=True)[2]
+    g = api.residual_norm_backward(dy, None, b, None, st, post=(scale, scale), gate=gate)
+    assert bool((g.dpost[1] == inf).all())

@@ -79,3 +79,16 @@ def test_an_infinity_in_the_last_row_counts_once(R, C, dtype):
     st = api.residual_norm(b, b, post=(None, None), stats=True)[2]
     g = api.residual_norm_backward(dy, None, b, None, st, post=(scale, scale), gate=gate)
     assert bool((g.dpost[1] == inf).all())
+
+
+@pytest.mark.parametrize("C", [8, 72])
+def test_gradients_do_not_share_a_storage(C):
+    """Keeping or saving one keeps no other, and one that grows leaves the others alone."""
+    b, how, s, st, ds, dy = _end(300, C)
+    got = flat(api.residual_norm_backward(ds, dy, b, s, st, **how))
+    assert len({t.untyped_storage().data_ptr() for t in got}) == len(got) == 8
+    assert all(t.storage_offset() == 0 and t.untyped_storage().nbytes() == t.nbytes for t in got)
+    for i, t in enumerate(got):
+        others = [o.clone() for o in got]
+        t.resize_(t.numel() + 512)[-512:] = 9.0
+        assert all(torch.equal(o, g) for k, (o, g) in enumerate(zip(others, got)) if k != i)

@@ -19,6 +19,7 @@ import sys
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
@@ -46,6 +47,7 @@ class GatedFfn(torch.autograd.Function):
         return s, y
 
     @staticmethod
+    @once_differentiable  # the calls' results are detached
     def backward(ctx, ds, dy):
         x, gate, n, mean, rstd, z, pre, o, s, *rest = ctx.saved_tensors
         kept, (gamma, beta, W, bias, Wd, bd, pg, pb, scale, ng, nb) = rest[:4], rest[4:]

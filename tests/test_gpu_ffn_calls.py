@@ -1,5 +1,8 @@
 """The operators that train a gated FFN, called as their documentation allows and rarely
 done: where the statistics come from, what the outputs share, values past 32 bits."""
+import importlib.util
+import os
+
 import pytest
 import torch
 
@@ -17,6 +20,14 @@ def _gpu():
 def _rand(seed, *shape, dtype=torch.float32, size=1.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     return (torch.randn(*shape, generator=g, device="cuda") * size).to(dtype)
+
+
+def _example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "ffn_gated.py")
+    spec = importlib.util.spec_from_file_location("ffn_gated", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
 
 
 def _end(R, C, dtype=torch.float32):
@@ -92,3 +103,14 @@ def test_gradients_do_not_share_a_storage(C):
         others = [o.clone() for o in got]
         t.resize_(t.numel() + 512)[-512:] = 9.0
         assert all(torch.equal(o, g) for k, (o, g) in enumerate(zip(others, got)) if k != i)
+
+
+def test_the_example_has_first_derivatives_alone():
+    """Its gradients are detached: a penalty on them is refused, not left out of the slope."""
+    m = _example()
+    w = m.make_weights(12, 8, torch.float32)
+    x, gate = _rand(1, 2, 5, 12).requires_grad_(), torch.ones(2, device="cuda")
+    s, y = m.GatedFfn.apply(x, gate, *(w[k] for k in m.NAMES))
+    dx, = torch.autograd.grad((s * s).sum() + (y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        ((dx * dx).sum() + (x * x).sum()).backward()

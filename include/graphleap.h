@@ -549,8 +549,9 @@ gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const 
  *   pre [R, 2 F] or NULL: [g | u], what gl_gated_linear_backward needs.
  *   act: GL_ACT_GELU (g Phi(g)), GL_ACT_SILU (g sigmoid(g)) or GL_ACT_NONE; GELU and SiLU
  *   of infinities are their limits.
- *   workspace: gl_gated_linear_workspace_bytes(R, K, F, dt) bytes (0 for few rows, and for
- *   many of whole vectors), 16-byte aligned.
+ *   workspace: gl_gated_linear_workspace_bytes(R, K, F, dt) bytes, 16-byte aligned.  0 for
+ *   up to 32 rows; beyond, rows that are no whole vectors need some, and so do long
+ *   contractions of few outputs, which are cut in parts: ask for every layer.
  * Errors: GL_ERR_NULL_PTR, GL_ERR_UNSUPPORTED (dtype, activation), GL_ERR_BAD_SHAPE,
  * GL_ERR_ALIGNMENT, GL_ERR_ALIAS, GL_ERR_WORKSPACE, GL_ERR_HIP.
  * -------------------------------------------------------------------------*/

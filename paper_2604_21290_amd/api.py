@@ -618,7 +618,7 @@ def _halves(name: str, W: torch.Tensor) -> int:
 
 
 def gated_linear_workspace(x: torch.Tensor, W: torch.Tensor) -> Workspace:
-    """Workspace of gl_gated_linear for this layer (empty for most)."""
+    """Workspace of gl_gated_linear for this layer (empty for many, not for all of whole vectors)."""
     R, K, N = _layer("gated_linear", x, W)
     return Workspace(lib().gl_gated_linear_workspace_bytes(R, K, _halves("gated_linear", W), _dt(x)), x.device)
 

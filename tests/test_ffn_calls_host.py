@@ -39,3 +39,16 @@ def test_choices_past_32_bits_are_refused(off):
         with pytest.raises(api.GraphLeapError) as e:
             call()
         assert api.STATUS[e.value.status] == "GL_ERR_UNSUPPORTED", i
+
+
+@pytest.mark.parametrize("R,K,F,dt", [(278, 2912, 112, 0), (40, 8192, 16, 1), (33, 4096, 4, 0)])
+def test_a_parted_contraction_needs_a_workspace(R, K, F, dt):
+    """Though its rows are whole vectors, which the header promises nothing about."""
+    L, P = api.lib(), lambda i: i * FAR  # noqa: E731
+    need = L.gl_gated_linear_workspace_bytes(R, K, F, dt)
+    assert need >= 2 * R * 2 * F * 4
+    call = lambda ws, n: api.STATUS[L.gl_gated_linear(P(1), R, K, P(2), None, F, 1, dt, P(3), None, ws, n, None)]  # noqa: E731
+    assert call(None, 0) == call(P(4), need - 1) == "GL_ERR_WORKSPACE"
+    assert L.gl_gated_linear_workspace_bytes(32, K, F, dt) == 0
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "graphleap.h")).read()
+    assert "ask for every layer" in text and "many of whole vectors" not in text

@@ -28,6 +28,7 @@
 
 #include "act_device.h"
 #include "gl_kernels.h"
+#include "product_ring.h"
 #include "row_device.h"
 
 namespace gl {
@@ -56,7 +57,7 @@ struct ProductCfg {
   static constexpr bool KA = KA_, KB = KB_;
   static constexpr int ES = DT ? 2 : 4, HALF = 64 / ES;  // contraction of half a stage
   static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
-  static constexpr int RA = KA ? (KB ? 5 : 4) : KB ? 3 : 2, RB = KB ? (KA ? 5 : 4) : KA ? 3 : 2;
+  static constexpr int RA = product_ring_depth(KA, KB), RB = product_ring_depth(KB, KA);
   static constexpr int kPieceA = BM * (KA ? 64 : 128), kPieceB = BN * (KB ? 64 : 128);
   static constexpr int kPlaceB = RA * kPieceA;  // of the second operand's ring
   static constexpr int TM = BM / WR / 16, TN = BN / WC / 16;
@@ -343,35 +344,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = product_mma<DT>(bf[j], af[i], acc[i][j]);
   };
-  // -- the rings.  Half h is piece h of an operand of halves, and half h & 1 of piece h / 2 of
-  //    one of stages.  Once every wave has half h in registers, a piece that it was the last
-  //    of is filled with the one that comes a ring later.
-  constexpr bool HA = G::KA, HB = G::KB;  // by halves
-  constexpr int RA = G::RA, RB = G::RB, NA = decltype(la)::NL, NB = decltype(lb)::NL;
   const uint32_t lds0 = lds_offset(smem) + w * 1024;
-  uint32_t pa = 0, pb = 0;  // where half h's pieces lie in the rings
-  auto next = [](uint32_t at, int piece, int ring) { return at + piece == (uint32_t)(piece * ring) ? 0u : at + piece; };
-  // after half h (odd: of its stage)
-  auto fill = [&](int h, bool odd) {
-    if (!HA && odd && 2 * ((h >> 1) + RA) < h1) la.load((h >> 1) + RA, a.K, lds0 + pa);
-    if (!HB && odd && 2 * ((h >> 1) + RB) < h1) lb.load((h >> 1) + RB, a.K, lds0 + G::kPlaceB + pb);
-    if (HA && h + RA < h1) la.load(h + RA, a.K, lds0 + pa);
-    if (HB && h + RB < h1) lb.load(h + RB, a.K, lds0 + G::kPlaceB + pb);
-  };
-  // Loads that may be under way while half h + 1 must have landed: those issued after its own.
-  // Each turn issues the stages' (odd turns) and then the halves'.
-  //   halves: h + 1's went out in turn h + 1 - ring; the ring - 2 turns up to h - 1 follow, of
-  //     which half are odd (rounded up after an even h, as h - 1 is odd)
-  //   stages: that of h + 1 (h odd) in turn h + 2 - 2 ring; 2 ring - 2 turns' halves follow,
-  //     its own turn's among them, and ring - 2 stages
-  constexpr int per_stage = (HA ? 0 : NA) + (HB ? 0 : NB), per_half = (HA ? NA : 0) + (HB ? NB : 0);
-  constexpr int rh = HA ? RA : RB, rs = HA ? RB : RA;
-  constexpr int by_half_even = (rh - 2) * per_half + (rh - 1) / 2 * per_stage;
-  constexpr int by_half_odd = (rh - 2) * per_half + (rh - 2) / 2 * per_stage;
-  constexpr int by_stage = (rs - 2) * per_stage + (2 * rs - 2) * per_half;
-  constexpr int after_even = by_half_even;
-  constexpr int after_odd = HA && HB ? by_half_odd : HA || HB ? (by_half_odd < by_stage ? by_half_odd : by_stage) : by_stage;
-  constexpr int LAST = 2 * (RA > RB ? RA : RB);  // turns before the last whose loads all go out
   auto read = [&](uint32_t qa, uint32_t qb, int kk, uint4* af, uint4* bf) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) bf[j] = FB::read(smem + G::kPlaceB + qb, bbase, bswap, bblk + j, kk, g, t);
@@ -380,7 +353,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
   };
   // a half's reads among the multiplications before it, not ahead of them all
   auto mix = [&] {
-    constexpr int reads = TM * (HA ? (DT ? 2 : 4) : 1) + TN * (HB ? (DT ? 2 : 4) : 1), mmas = TM * TN * (DT ? 1 : 4);
+    constexpr int reads = TM * (G::KA ? (DT ? 2 : 4) : 1) + TN * (G::KB ? (DT ? 2 : 4) : 1), mmas = TM * TN * (DT ? 1 : 4);
     constexpr int each = mmas / reads > 0 ? mmas / reads : 1, n = reads < mmas ? reads : mmas;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
@@ -389,45 +362,20 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, char* smem, i
     }
   };
   uint4 a0[TM], b0[TN], a1[TM], b1[TN];
-  if (h0 < h1) {
-    // the rings' first filling, in the order of the turns that would have made it
-#pragma unroll
-    for (int o = 2 - LAST; o <= 0; ++o) {  // the turn before half h0 + o
-      const bool odd = (o & 1) == 0;
-      if (!HA && odd && o / 2 - 1 + RA >= 0 && h0 + 2 * (o / 2 - 1 + RA) < h1)
-        la.load(h0 / 2 + o / 2 - 1 + RA, a.K, lds0 + (o / 2 - 1 + RA) * G::kPieceA);
-      if (!HB && odd && o / 2 - 1 + RB >= 0 && h0 + 2 * (o / 2 - 1 + RB) < h1)
-        lb.load(h0 / 2 + o / 2 - 1 + RB, a.K, lds0 + G::kPlaceB + (o / 2 - 1 + RB) * G::kPieceB);
-      if (HA && o - 1 + RA >= 0 && h0 + o - 1 + RA < h1) la.load(h0 + o - 1 + RA, a.K, lds0 + (o - 1 + RA) * G::kPieceA);
-      if (HB && o - 1 + RB >= 0 && h0 + o - 1 + RB < h1)
-        lb.load(h0 + o - 1 + RB, a.K, lds0 + G::kPlaceB + (o - 1 + RB) * G::kPieceB);
-    }
-    if (h0 + LAST < h1) dma_wait_barrier<after_odd>();
-    else dma_wait_barrier();
-    read(0, 0, 0, a0, b0);
-    for (int h = h0; h < h1; h += 2) {
-      uint32_t qa = HA ? next(pa, G::kPieceA, RA) : pa, qb = HB ? next(pb, G::kPieceB, RB) : pb;
-      if constexpr (HA || HB) {
-        if (h + LAST < h1) dma_wait_barrier<after_even>();
-        else dma_wait_barrier();
-        fill(h, false);
-      }
-      read(qa, qb, 1, a1, b1);
-      multiply(a0, b0);
-      mix();
-      pa = qa, pb = qb;
-      qa = next(pa, G::kPieceA, RA), qb = next(pb, G::kPieceB, RB);
-      if (h + LAST < h1) dma_wait_barrier<after_odd>();
-      else dma_wait_barrier();
-      fill(h + 1, true);
-      // (after the last half too, of whatever lies there: behind a branch the compiler would
-      // not know how many reads are under way, and wait for these before it multiplies)
-      read(qa, qb, 0, a0, b0);
-      multiply(a1, b1);
-      mix();
-      pa = qa, pb = qb;
-    }
-  }
+  using Ring = ProductRing<G::KA, G::KB, decltype(la)::NL, decltype(lb)::NL, G::kPieceA, G::kPieceB>;
+  Ring::run(
+      h0, h1, [&](int piece, uint32_t at) { la.load(piece, a.K, lds0 + at); },
+      [&](int piece, uint32_t at) { lb.load(piece, a.K, lds0 + G::kPlaceB + at); },
+      [&](auto n) { dma_wait_barrier<decltype(n)::value>(); }, [&] { dma_wait_barrier(); },
+      [&](auto set, uint32_t qa, uint32_t qb) {
+        if constexpr (decltype(set)::value) read(qa, qb, 1, a1, b1);
+        else read(qa, qb, 0, a0, b0);
+      },
+      [&](auto set) {
+        if constexpr (decltype(set)::value) multiply(a1, b1);
+        else multiply(a0, b0);
+        mix();
+      });
 
   if (EPI == kProductGated) {
     if (a.parts > 1) product_epilogue<G, kProductGatedPart>(a, smem, acc, m0, n0, part);

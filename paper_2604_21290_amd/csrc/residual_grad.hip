@@ -290,39 +290,39 @@ __global__ __launch_bounds__(1024) void residual_vectors_kernel(ResidualGradArgs
   }
   const int t = threadIdx.x % COLS, w = threadIdx.x / COLS, C = a.C;
   for (int c0 = blockIdx.x * COLS; c0 < C; c0 += vectors * COLS) {
-  const int c = c0 + t, col = min(c, C - 1);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int g0 = w; g0 < G; g0 += U * ROWS) {
-    float v[U][4];
+    const int c = c0 + t, col = min(c, C - 1);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = w; g0 < G; g0 += U * ROWS) {
+      float v[U][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[u][q] = a.part[((size_t)min(g0 + u * ROWS, G - 1) * 4 + q) * C + col];
+        for (int q = 0; q < 4; ++q) v[u][q] = a.part[((size_t)min(g0 + u * ROWS, G - 1) * 4 + q) * C + col];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += g0 + u * ROWS < G ? v[u][q] : 0.f;
-  }
+        for (int q = 0; q < 4; ++q) s[q] += g0 + u * ROWS < G ? v[u][q] : 0.f;
+    }
 #pragma unroll
-  for (int q = 0; q < 4; ++q) sums[q][w][t] = s[q];
+    for (int q = 0; q < 4; ++q) sums[q][w][t] = s[q];
 #pragma unroll
-  for (int h = ROWS / 2; h >= 1; h /= 2) {
-    __syncthreads();
-    if (w < h)
+    for (int h = ROWS / 2; h >= 1; h /= 2) {
+      __syncthreads();
+      if (w < h)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sums[q][w][t] += sums[q][w + h][t];
-  }
-  if (!w && c < C) {
-    const float S1 = sums[0][0][t], S0 = sums[1][0][t];
-    const float sc = a.scale ? T::load1(a.scale, c) : 1.f;
-    if (a.dscale)
-      a.dscale[c] = a.post ? fmaf(a.gamma1 ? T::load1(a.gamma1, c) : 1.f, S1, a.beta1 ? T::load1(a.beta1, c) * S0 : 0.f) : S1;
-    if (a.dgamma1) a.dgamma1[c] = sc * S1;
-    if (a.dbeta1) a.dbeta1[c] = sc * S0;
-    if (a.dgamma2) a.dgamma2[c] = sums[2][0][t];
-    if (a.dbeta2) a.dbeta2[c] = sums[3][0][t];
-  }
-  __syncthreads();  // sums is free again
+        for (int q = 0; q < 4; ++q) sums[q][w][t] += sums[q][w + h][t];
+    }
+    if (!w && c < C) {
+      const float S1 = sums[0][0][t], S0 = sums[1][0][t];
+      const float sc = a.scale ? T::load1(a.scale, c) : 1.f;
+      if (a.dscale)
+        a.dscale[c] = a.post ? fmaf(a.gamma1 ? T::load1(a.gamma1, c) : 1.f, S1, a.beta1 ? T::load1(a.beta1, c) * S0 : 0.f) : S1;
+      if (a.dgamma1) a.dgamma1[c] = sc * S1;
+      if (a.dbeta1) a.dbeta1[c] = sc * S0;
+      if (a.dgamma2) a.dgamma2[c] = sums[2][0][t];
+      if (a.dbeta2) a.dbeta2[c] = sums[3][0][t];
+    }
+    __syncthreads();  // sums is free again
   }
 }
 

@@ -548,7 +548,7 @@ gl_status gl_linear_q8(const int8_t* q, const float* scale, int R, int K, const 
  *   x [R, K]; W [2 F, K]; bias [2 F] or NULL; h [R, F]
  *   pre [R, 2 F] or NULL: [g | u], what gl_gated_linear_backward needs.
  *   act: GL_ACT_GELU (g Phi(g)), GL_ACT_SILU (g sigmoid(g)) or GL_ACT_NONE; GELU and SiLU
- *   of infinities are their limits.
+ *   of infinities are their limits, and values of theirs under 2^-119 may be 0.
  *   workspace: gl_gated_linear_workspace_bytes(R, K, F, dt) bytes, 16-byte aligned.  0 for
  *   up to 32 rows; beyond, rows that are no whole vectors need some, and so do long
  *   contractions of few outputs, which are cut in parts: ask for every layer.

@@ -13,6 +13,9 @@ enum { kActNone = 0, kActGelu = 1, kActSilu = 2 };  // gl_act
 // that the tail's small results have their bits too:
 //   bf16  five terms, within 5.7e-7 e^(1.5 a), never more than 2.8e-3 (2^-8 is its rounding)
 //   fp32  eight terms, within 3.8e-8 (1 + a)
+// The three terms more would cost a bf16 gated layer up to 2.7 % (12544 x 640 x 2560 94.4 us for
+// 97.0 without pre, 16384 x 2048 x 4096 443 for 446, 6272 x 192 x 768 and single rows nothing);
+// down to -4, where the GELU is -1.3e-4, five are within a sixteenth of its type's rounding.
 template <int DT>
 __device__ __forceinline__ float gauss_tail(float a) {
   const float t = __builtin_amdgcn_rcpf(fmaf(DT ? 0.34400001f : 0.3f, a, 1.f));
@@ -48,7 +51,8 @@ __device__ __forceinline__ float gelu_tail(float x) {
   return fmaf(-fminf(a, 3.4e38f), tq * e, fmaxf(x, 0.f));
 }
 
-// 1 / (1 + e^-x); the division by a reciprocal of about one unit in the last place
+// 1 / (1 + e^-x); the division by a reciprocal of about one unit in the last place.  Below
+// 2^-126, x < -87.3, it is 0: the hardware's reciprocal gives no subnormals.
 __device__ __forceinline__ float sigmoid_f32(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
 }

@@ -5,7 +5,7 @@
 // which one pass over dh and pre writes to the workspace, rounded to the operands' type (a
 // product's operands are 16 bits; the sum db is of the values before that rounding).  Three
 // launches: before, both products, after.  us, bf16: gated 16384 x 2048 x 4096 976 (113 at
-// 5.2 TB/s, then 860: 1.28 PFLOP/s), 6272 x 192 x 768 36 (12.5, 21, 5); plain 12544 x 2560 x 640
+// 5.9 TB/s, then 860: 1.28 PFLOP/s), 6272 x 192 x 768 36 (12.5, 21, 5); plain 12544 x 2560 x 640
 // 112 (5, 100, 7).
 #include "product.h"
 

@@ -5,9 +5,9 @@
 // The norms are over a row's channels, with the mean taken out (layer norm) or not (rms).
 // A row's values stay in registers in fp32 from the loads to both stores: y is of the sum
 // before its rounding.  Memory bounds it: us a call (TB/s of the four rows; a copy of 1 GiB
-// reaches 5.2), with post and a gate for each row, bf16 32768 x 2560 131 (5.1), 8192 x 4096
-// 47 (5.7), 100352 x 320 53 (4.9), 100352 x 80 15.6 (4.3; 10 of 16 lanes hold a chunk); fp32
-// 32768 x 2560 230 (5.9).  196 x 192 takes a launch, 3 us.
+// reaches 5.2), with post and a gate for each row, bf16 32768 x 2560 130 (5.2), 8192 x 4096
+// 46 (5.8), 100352 x 320 47 (5.5), 100352 x 80 16.1 (4.0; 10 of 16 lanes hold a chunk), 4096 x
+// 16384 118 (4.6); fp32 32768 x 2560 229 (5.9).  196 x 192 takes a launch, 3 us.
 #include "gl_kernels.h"
 #include "row_device.h"
 

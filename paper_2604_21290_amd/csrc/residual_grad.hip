@@ -12,10 +12,13 @@
 // terms to sums of its own over all rows that it meets; a workgroup adds its lanes' and
 // writes them to the workspace, and a second kernel adds the workgroups' and makes the
 // vectors.  Memory bounds it where rows are many and wide, us (TB/s of the six rows), with post
-// and a gate for each row: bf16 32768 x 2560 261 (3.9; without post 213, 4.7), 8192 x 4096 99
-// (4.1), 16384 x 1024 47 (4.3), fp32 32768 x 2560 370 (5.5).  Four sums a channel and four
-// rows under way take the registers of all but two waves a SIMD, and the vector units are
-// busy half of the time; 100352 x 80 (27 us without post, 3.7 TB/s) keeps them busy 88 %.
+// and a gate for each row: bf16 32768 x 2560 259 (3.9; without post 212, 4.7), 8192 x 4096 100
+// (4.0), 16384 x 1024 48 (4.2), 8192 x 8192 196 (4.1), fp32 32768 x 2560 374 (5.4).  Four sums a
+// channel and four rows under way take the registers of all but two waves a SIMD, and the
+// vector units are busy half of the time; 100352 x 80 (28 us without post, 3.5 TB/s) keeps them
+// busy 90 %.  Rows wider than the largest tile, 8192 channels of either type, go value by value,
+// and eight (bf16) or three times (fp32) slower: bf16 8192 x 8200 1603 us (0.5), 4096 x 16384
+// 1416 (0.6), fp32 8192 x 8208 1237 (1.3).
 // Everything is fp32, added in an order that depends on the sizes alone.
 #include "gl_kernels.h"
 #include "row_device.h"

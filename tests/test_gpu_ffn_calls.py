@@ -114,3 +114,17 @@ def test_the_example_has_first_derivatives_alone():
     dx, = torch.autograd.grad((s * s).sum() + (y * y).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         ((dx * dx).sum() + (x * x).sum()).backward()
+
+
+def test_gradients_of_memory_that_torch_did_not_allocate():
+    """Such a tensor has no allocator of its own to make the small outputs by."""
+    b, how, s, st, ds, dy = _end(300, 72)
+    want = flat(api.residual_norm_backward(ds, dy, b, s, st, **how))
+    args = [torch.from_dlpack(t) for t in (ds, dy, b, s)]
+    assert args[2].data_ptr() == b.data_ptr()
+    got = flat(api.residual_norm_backward(*args, st, **how))
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+    got[3].resize_(1000).zero_()
+    with torch.inference_mode():
+        got = flat(api.residual_norm_backward(ds, dy, b, s, st, **how))
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
